@@ -288,6 +288,79 @@ vidax_status vidax_qkv_proj(const void* x, const void* w, const float* bias, con
                             int32_t H, int32_t d, int32_t C, const vidax_rope3d_desc* rope, hipStream_t stream);
 
 /*
+ * The step between two sublayers of a block (Section 3, "Supported Models":
+ * adaptive layer norm per sample or per token; the paper gives no formula):
+ * the sublayer's output y joins the residual stream x, and the sum is
+ * normalised and modulated for the next sublayer.  Per token, over C channels:
+ *
+ *   u  = post(y) * post_gain            post: none, layer norm or RMS norm
+ *   x' = alpha * x + gate * u
+ *   h  = norm(x') * gain * (1 + scale) + shift
+ *
+ * layer norm: (v - mean) / sqrt(mean((v - mean)^2) + eps), RMS norm: v /
+ * sqrt(mean(v^2) + eps).  Evaluated in fp32; x' and h are each rounded once (h
+ * is formed from x' before that is rounded).
+ */
+typedef struct vidax_block_mod {
+  const float* p;        /* fp32 device rows, 16-byte aligned, or NULL (gate 1, scale and shift 0) */
+  int64_t batch_stride;  /* elements between the rows of two batches and of two tokens: */
+  int64_t token_stride;  /* multiples of 4, >= 0; token_stride 0 = one row a batch */
+} vidax_block_mod;
+
+typedef struct vidax_block_norm_desc {
+  int32_t stream_fp32;  /* x, x' and their gradients: 0 bf16, 1 fp32 */
+  int32_t norm;         /* 1 layer norm, 2 RMS norm */
+  int32_t post;         /* 0 none, 1 layer norm, 2 RMS norm */
+  int32_t per_token;    /* backward: gradients of gate, scale and shift are [B, L, C]
+                           (1), or [B, C], summed over a batch's tokens (0, which
+                           requires token strides of 0).  The forward ignores it. */
+  float eps;            /* >= 0, finite */
+  float alpha;          /* finite */
+  const float* gain;      /* fp32 [C] on the device, 16-byte aligned, or NULL (1) */
+  const float* post_gain; /* likewise; requires post */
+  vidax_block_mod gate, scale, shift;
+} vidax_block_norm_desc;
+
+/*
+ * x: bf16 or fp32 [B, L, C]; y: bf16 [B, L, C] or NULL (no branch: gate, post
+ * and post_gain must then be absent); xo (x'): as x, may be x itself (in place),
+ * NULL allowed without a branch where alpha is 1 (x' is x); h: bf16 [B, L, C].
+ * All device pointers 16-byte aligned; outputs must not overlap each other or
+ * an input (x itself apart).  Requires C a multiple of 8 and C <= 16384
+ * (VIDAX_ERR_UNSUPPORTED otherwise); zero-sized calls are no-ops.  `desc` is a
+ * host pointer.  HBM-bound: x and y are read once, x' and h written once.
+ */
+vidax_status vidax_block_norm_fwd(const void* x, const void* y, void* xo, void* h, int32_t B, int32_t L, int32_t C,
+                                  const vidax_block_norm_desc* desc, hipStream_t stream);
+
+/* Gradients of the modulations and gains, fp32 device pointers, 16-byte
+ * aligned, each NULL where it is not wanted or (dgain ...) the operand is 1. */
+typedef struct vidax_block_norm_grads {
+  float *dgate, *dscale, *dshift; /* [B, C], or [B, L, C] with per_token */
+  float *dgain, *dpost_gain;      /* [C], summed over batches and tokens */
+} vidax_block_norm_grads;
+
+/*
+ * Gradient of vidax_block_norm_fwd at the stream xo (x') that it left:
+ *   dh  : bf16 [B, L, C], gradient of h;  dxo: as the stream, gradient of x'
+ *         from what reads it later, or NULL (none)
+ *   dx  : as the stream, gradient of x, may be dxo itself (in place)
+ *   dy  : bf16 [B, L, C], gradient of y (NULL exactly where y is)
+ * workspace: fp32 device memory, at least vidax_block_norm_bwd_workspace_floats
+ * (B, L, C) values, 16-byte aligned; not needed (NULL allowed) where no sum over
+ * tokens is asked for.  Sums over tokens are fp32, in an order that depends on
+ * the sizes alone (same call, same bits).  desc->shift is not read.  Other
+ * requirements as for the forward.
+ */
+vidax_status vidax_block_norm_bwd(const void* dh, const void* dxo, const void* xo, const void* y, void* dx, void* dy,
+                                  const vidax_block_norm_grads* grads, float* workspace, size_t workspace_floats,
+                                  int32_t B, int32_t L, int32_t C, const vidax_block_norm_desc* desc,
+                                  hipStream_t stream);
+
+/* fp32 values of that workspace; 0 for sizes that the backward refuses. */
+size_t vidax_block_norm_bwd_workspace_floats(int32_t B, int32_t L, int32_t C);
+
+/*
  * Same contract as vidax_attn_fwd, computed by a plain scalar fp32 kernel (one
  * thread per query row, rotation evaluated on the fly, no matrix cores).  It
  * exists as an independent second GPU implementation for cross-checks at

@@ -20,6 +20,9 @@ served models (per-head RMS normalisation with a learned gain);
 ``rope_transpose_ref`` carries a gradient back through the rotation, and
 ``na3d_ref`` is the 3D neighbourhood (windowed) attention of a VAE decoder,
 and ``qkv_proj_ref`` the Q/K/V projection followed by the Q/K prologue.
+``attn_mod_ref`` and ``attn_mod_bwd_ref`` are attention with capped, biased and
+masked scores and its gradient, ``block_norm_ref`` and ``block_norm_bwd_ref`` the
+step between two sublayers of a block.
 """
 
 from .bf16 import bf16_bits_to_f64, f64_to_bf16_bits
@@ -29,6 +32,8 @@ from .qknorm import qk_norm_ref
 from .attention_bwd import attn_bwd_ref, attn_bwd_ref_rows, rope_transpose_ref
 from .na3d import na3d_ref
 from .qkv import qkv_proj_ref
+from .attn_mod import ScoreSpec, attn_mod_ref, attn_mod_bwd_ref
+from .block_norm import block_norm_ref, block_norm_bwd_ref
 
 __all__ = [
     "bf16_bits_to_f64",
@@ -44,4 +49,9 @@ __all__ = [
     "rope_transpose_ref",
     "na3d_ref",
     "qkv_proj_ref",
+    "ScoreSpec",
+    "attn_mod_ref",
+    "attn_mod_bwd_ref",
+    "block_norm_ref",
+    "block_norm_bwd_ref",
 ]

@@ -29,6 +29,9 @@ EXPORTED_SYMBOLS = (
     "vidax_na3d_fwd",
     "vidax_qkv_proj",
     "vidax_qk_norm_rope",
+    "vidax_block_norm_fwd",
+    "vidax_block_norm_bwd",
+    "vidax_block_norm_bwd_workspace_floats",
     "vidax_attn_fwd",
     "vidax_attn_fwd_naive",
     "vidax_status_string",
@@ -72,6 +75,36 @@ class Rope:
         return RopeDesc(*self.grid, *self.dims, float(self.theta), int(self.pair_mode), int(self.keys_prerotated))
 
 
+class BlockMod(ctypes.Structure):
+    """Mirror of vidax_block_mod."""
+
+    _fields_ = [("p", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64)]
+
+
+class BlockNormDesc(ctypes.Structure):
+    """Mirror of vidax_block_norm_desc."""
+
+    _fields_ = [
+        ("stream_fp32", ctypes.c_int32),
+        ("norm", ctypes.c_int32),
+        ("post", ctypes.c_int32),
+        ("per_token", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("alpha", ctypes.c_float),
+        ("gain", ctypes.c_void_p),
+        ("post_gain", ctypes.c_void_p),
+        ("gate", BlockMod),
+        ("scale", BlockMod),
+        ("shift", BlockMod),
+    ]
+
+
+class BlockNormGrads(ctypes.Structure):
+    """Mirror of vidax_block_norm_grads."""
+
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dgate", "dscale", "dshift", "dgain", "dpost_gain")]
+
+
 _lib = None
 
 
@@ -102,6 +135,13 @@ def lib() -> ctypes.CDLL:
         L.vidax_qkv_proj.restype = i32
         L.vidax_qk_norm_rope.argtypes = [vp, vp, vp, f32, i32, i32, i32, i32, ctypes.POINTER(RopeDesc), vp]
         L.vidax_qk_norm_rope.restype = i32
+        L.vidax_block_norm_fwd.argtypes = [vp] * 4 + [i32] * 3 + [ctypes.POINTER(BlockNormDesc), vp]
+        L.vidax_block_norm_fwd.restype = i32
+        L.vidax_block_norm_bwd.argtypes = ([vp] * 6 + [ctypes.POINTER(BlockNormGrads), vp, ctypes.c_size_t]
+                                           + [i32] * 3 + [ctypes.POINTER(BlockNormDesc), vp])
+        L.vidax_block_norm_bwd.restype = i32
+        L.vidax_block_norm_bwd_workspace_floats.argtypes = [i32, i32, i32]
+        L.vidax_block_norm_bwd_workspace_floats.restype = ctypes.c_size_t
         for name in ("vidax_attn_fwd", "vidax_attn_fwd_naive"):
             fn = getattr(L, name)
             fn.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, f32, vp, ctypes.POINTER(RopeDesc), vp]
@@ -330,3 +370,139 @@ def attn_fwd_naive(q, k, v, scale=None, kv_valid_len=None, rope: Rope | None = N
                    stream=None):
     """Same contract on the scalar fp32 cross-check kernel (small sizes only)."""
     return _attn("vidax_attn_fwd_naive", q, k, v, scale, kv_valid_len, rope, return_lse, out, stream)
+
+
+# ------------------------------------------------------- block norm ----
+
+
+def _call(fn: str, device, stream, *args):
+    """fn(*args, stream) with the tensors' device current and, by default, on that device's current stream."""
+    import torch
+
+    s = torch.cuda.current_stream(device) if stream is None else stream
+    h = ctypes.c_void_p(s.cuda_stream)
+    if device.index == torch.cuda.current_device():
+        st = getattr(lib(), fn)(*args, h)
+    else:
+        with torch.cuda.device(device):
+            st = getattr(lib(), fn)(*args, h)
+    if st != VIDAX_OK:
+        raise VidaxError(fn, st)
+
+
+def _check_dense(name, t, dtype, shape, device):
+    if t.dtype != dtype or t.device != device or not t.is_contiguous() or t.shape != shape:
+        raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} tensor on {device}")
+
+
+_NORMS = {None: 0, "layer": 1, "rms": 2}
+
+
+def _block_mod(name, t, B, L, C, device):
+    """(BlockMod, one row a token?) of a modulation [B, C], [B, 1, C] or [B, L, C]."""
+    import torch
+
+    if t is None:
+        return BlockMod(None, 0, 0), None
+    if t.dtype != torch.float32 or t.device != device or (C > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name} must be a float32 tensor on {device} with dense channels")
+    if t.shape == (B, C):
+        return BlockMod(t.data_ptr(), t.stride(0) if B > 1 else 0, 0), False
+    if t.dim() != 3 or t.shape[0] != B or t.shape[1] not in (1, L) or t.shape[2] != C:
+        raise ValueError(f"{name} must be [B, C], [B, 1, C] or [B, L, C]")
+    token = t.shape[1] > 1
+    return BlockMod(t.data_ptr(), t.stride(0) if B > 1 else 0, t.stride(1) if token else 0), token
+
+
+def _block_desc(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha):
+    """(descriptor, gradients one row a token?)"""
+    import torch
+
+    if x.dim() != 3 or not x.is_cuda or x.dtype not in (torch.bfloat16, torch.float32) or not x.is_contiguous():
+        raise ValueError("x must be a contiguous bfloat16 or float32 [B, L, C] device tensor")
+    if norm not in ("layer", "rms") or post not in _NORMS:
+        raise ValueError("norm must be 'layer' or 'rms', post one of them or None")
+    B, L, C = x.shape
+    if y is not None:
+        _check_dense("y", y, torch.bfloat16, x.shape, x.device)
+    for n, t in (("gain", gain), ("post_gain", post_gain)):
+        if t is not None:
+            _check_dense(n, t, torch.float32, (C,), x.device)
+    mods = [_block_mod(n, t, B, L, C, x.device) for n, t in (("gate", gate), ("scale", scale), ("shift", shift))]
+    token = {f for _, f in mods if f is not None}
+    d = BlockNormDesc(x.dtype == torch.float32, _NORMS[norm], _NORMS[post], 0, float(eps), float(alpha),
+                      gain.data_ptr() if gain is not None else None,
+                      post_gain.data_ptr() if post_gain is not None else None, *(m for m, _ in mods))
+    return d, token
+
+
+def block_norm_fwd(x, y=None, gate=None, scale=None, shift=None, gain=None, post_gain=None, norm: str = "layer",
+                   post: str | None = None, eps: float = 1e-6, alpha: float = 1.0, out=None, stream=None):
+    """The step between two sublayers: (x', h) with x' = alpha x + gate post(y)
+    post_gain and h = norm(x') gain (1 + scale) + shift.
+
+    x: bf16 or fp32 [B, L, C], the residual stream; y: bf16, the sublayer's
+    output, or None (no branch; x' is then x itself where alpha is 1).  gate,
+    scale, shift: fp32 [B, C], [B, 1, C] or [B, L, C], rows of any strides that
+    are multiples of 4 (slices of one modulation table); gain, post_gain: fp32
+    [C].  norm: "layer" or "rms"; post: the norm on the branch, or None.  h is
+    bf16.  `out` = (x', h) tensors to write into; x' may be x (in place)."""
+    import torch
+
+    d, _ = _block_desc(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha)
+    same = y is None and alpha == 1.0
+    if out is None:
+        xo = None if same else torch.empty_like(x)
+        h = torch.empty_like(x, dtype=torch.bfloat16)
+    else:
+        xo, h = out
+        if xo is not None:
+            _check_dense("out[0]", xo, x.dtype, x.shape, x.device)
+        elif not same:
+            raise ValueError("out[0] may be None only where x' is x")
+        _check_dense("out[1]", h, torch.bfloat16, x.shape, x.device)
+    B, L, C = x.shape
+    _call("vidax_block_norm_fwd", x.device, stream, _ptr(x), _ptr(y), _ptr(xo), _ptr(h), B, L, C, ctypes.byref(d))
+    return (x if xo is None else xo), h
+
+
+def block_norm_bwd(dh, dx, x, y=None, gate=None, scale=None, shift=None, gain=None, post_gain=None,
+                   norm: str = "layer", post: str | None = None, eps: float = 1e-6, alpha: float = 1.0, workspace=None,
+                   stream=None):
+    """Gradients of block_norm_fwd, as a dict: "dx", "dy" (with a branch) and
+    "dgate", "dscale", "dshift", "dgain", "dpost_gain" for the operands given,
+    each in its operand's shape (fp32).
+
+    dh: gradient of h (bf16); dx: gradient of x' from what reads it later, in
+    the stream's type, or None; x: the x' that the forward returned; the rest as
+    for the forward (gate, scale and shift are all per sample or all per token).
+    `workspace`: a contiguous float32 device tensor of at least
+    vidax_block_norm_bwd_workspace_floats values (by default one is allocated)."""
+    import torch
+
+    d, token = _block_desc(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha)
+    if len(token) > 1:
+        raise ValueError("gate, scale and shift must all be per sample or all per token")
+    d.per_token = int(True in token)
+    B, L, C = x.shape
+    _check_dense("dh", dh, torch.bfloat16, x.shape, x.device)
+    if dx is not None:
+        _check_dense("dx", dx, x.dtype, x.shape, x.device)
+    got = {"dx": torch.empty_like(x)}
+    if y is not None:
+        got["dy"] = torch.empty_like(y)
+    for n, t in (("dgate", gate), ("dscale", scale), ("dshift", shift), ("dgain", gain), ("dpost_gain", post_gain)):
+        if t is not None:
+            got[n] = torch.empty(t.shape, dtype=torch.float32, device=x.device)
+    g = BlockNormGrads(*(got[n].data_ptr() if n in got else None for n, _ in BlockNormGrads._fields_))
+    sums = (not d.per_token and len(token) > 0) or gain is not None or post_gain is not None
+    if workspace is not None:
+        if (workspace.dtype != torch.float32 or workspace.device != x.device or not workspace.is_contiguous()):
+            raise ValueError(f"workspace must be a contiguous float32 tensor on {x.device}")
+    elif sums:
+        n = lib().vidax_block_norm_bwd_workspace_floats(B, L, C)
+        workspace = torch.empty((n,), dtype=torch.float32, device=x.device)
+    _call("vidax_block_norm_bwd", x.device, stream, _ptr(dh), _ptr(dx), _ptr(x), _ptr(y), _ptr(got["dx"]),
+          _ptr(got.get("dy")), ctypes.byref(g), _ptr(workspace), 0 if workspace is None else workspace.numel(), B, L, C,
+          ctypes.byref(d))
+    return got

@@ -7,6 +7,7 @@
 
 #include "../../include/vidax.h"
 #include "launch.hpp"
+#include "launch_block.hpp"
 
 static_assert(VIDAX_NOALLOC_MAX_ROWS == vidax::kNoAllocRows, "allocation-free scratch size");
 
@@ -199,6 +200,67 @@ vidax_status bwd_common(bool noalloc, const void* q, const void* k, const void* 
   return e == hipSuccess ? VIDAX_OK : VIDAX_ERR_LAUNCH;
 }
 
+// A buffer of a call, for the checks that all entry points below share.
+struct Buf {
+  const void* p;
+  uint64_t bytes;
+};
+
+// Outputs overlap each other or an input?  (`in_place`: this output may be
+// exactly this input.)
+template <int NO, int NI>
+bool any_overlap(const Buf (&outs)[NO], const Buf (&ins)[NI], int io_out = -1, int io_in = -1) {
+  for (int i = 0; i < NO; ++i) {
+    if (!outs[i].p) continue;
+    for (int j = 0; j < NI; ++j) {
+      if (!ins[j].p || (i == io_out && j == io_in && outs[i].p == ins[j].p)) continue;
+      if (overlaps(outs[i].p, outs[i].bytes, ins[j].p, ins[j].bytes)) return true;
+    }
+    for (int j = i + 1; j < NO; ++j)
+      if (outs[j].p && overlaps(outs[i].p, outs[i].bytes, outs[j].p, outs[j].bytes)) return true;
+  }
+  return false;
+}
+
+// Bytes from a modulation's first element to behind its last, or -1 if its
+// strides are not allowed.
+int64_t mod_bytes(const vidax_block_mod& m, int64_t B, int64_t L, int64_t C) {
+  if (!m.p) return 0;
+  if (m.batch_stride < 0 || m.token_stride < 0 || (m.batch_stride | m.token_stride) & 3) return -1;
+  const int64_t lim = INT64_C(1) << 58;
+  if ((m.batch_stride && B > lim / m.batch_stride) || (m.token_stride && L > lim / m.token_stride)) return -1;
+  return B && L ? ((B - 1) * m.batch_stride + (L - 1) * m.token_stride + C) * 4 : 0;
+}
+
+// The checks that the block norm's forward and backward share.
+vidax_status block_norm_common(int32_t B, int32_t L, int32_t C, const vidax_block_norm_desc* d, bool branch,
+                               vidax::BlockNorm* n, Buf (&mods)[5]) {
+  if (B < 0 || L < 0 || C < 0 || !d) return VIDAX_ERR_INVALID_ARG;
+  if (numel4(B, L, C, 4) < 0) return VIDAX_ERR_INVALID_ARG;
+  if ((d->stream_fp32 != 0 && d->stream_fp32 != 1) || (d->norm != 1 && d->norm != 2) || d->post < 0 || d->post > 2 ||
+      (d->per_token != 0 && d->per_token != 1))
+    return VIDAX_ERR_INVALID_ARG;
+  if (!(d->eps >= 0.0f) || !isfinite(d->eps) || !isfinite(d->alpha)) return VIDAX_ERR_INVALID_ARG;
+  const bool empty = B == 0 || L == 0 || C == 0;  // (the branch may then be NULL like any tensor)
+  if (!branch && !empty && (d->post || d->gate.p)) return VIDAX_ERR_INVALID_ARG;
+  if (!d->post && d->post_gain) return VIDAX_ERR_INVALID_ARG;
+  const vidax_block_mod* m[3] = {&d->gate, &d->scale, &d->shift};
+  for (int i = 0; i < 3; ++i) {
+    const int64_t bytes = mod_bytes(*m[i], B, L, C);
+    if (bytes < 0 || !aligned(m[i]->p, 16)) return VIDAX_ERR_INVALID_ARG;
+    mods[i] = Buf{m[i]->p, (uint64_t)bytes};
+  }
+  if (!aligned(d->gain, 16) || !aligned(d->post_gain, 16)) return VIDAX_ERR_INVALID_ARG;
+  mods[3] = Buf{d->gain, (uint64_t)C * 4};
+  mods[4] = Buf{d->post_gain, (uint64_t)C * 4};
+  if (C % 8 != 0 || C > vidax::kBlockMaxC) return VIDAX_ERR_UNSUPPORTED;
+  if ((int64_t)B * L > INT32_MAX) return VIDAX_ERR_UNSUPPORTED;  // workgroups
+  auto mod = [](const vidax_block_mod& x) { return vidax::BlockMod{x.p, x.batch_stride, x.token_stride}; };
+  *n = vidax::BlockNorm{B, L, C, d->stream_fp32, d->norm, d->post, d->eps, d->alpha, d->gain, d->post_gain,
+                        mod(d->gate), mod(d->scale), mod(d->shift)};
+  return VIDAX_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -344,6 +406,83 @@ vidax_status vidax_qkv_proj(const void* x, const void* w, const float* bias, con
   const hipError_t e = vidax::launch_qkv_proj((const uint16_t*)x, (const uint16_t*)w, bias, gain_q, gain_k, eps,
                                               (uint16_t*)q, (uint16_t*)k, (uint16_t*)v, B, L, H, C, rp, stream);
   return e == hipSuccess ? VIDAX_OK : VIDAX_ERR_LAUNCH;
+}
+
+vidax_status vidax_block_norm_fwd(const void* x, const void* y, void* xo, void* h, int32_t B, int32_t L, int32_t C,
+                                  const vidax_block_norm_desc* desc, hipStream_t stream) {
+  vidax::BlockNormFwd a;
+  Buf mods[5];
+  const vidax_status st = block_norm_common(B, L, C, desc, y != nullptr, &a.n, mods);
+  if (st == VIDAX_ERR_INVALID_ARG) return st;
+  const uint64_t n = (uint64_t)B * L * C, sb = n * (desc->stream_fp32 ? 4 : 2);
+  for (const void* p : {x, y, (const void*)xo, (const void*)h})
+    if (!aligned(p, 16)) return VIDAX_ERR_INVALID_ARG;
+  if (n > 0 && (!x || !h || (!xo && (y || desc->alpha != 1.0f)))) return VIDAX_ERR_INVALID_ARG;
+  const Buf outs[2] = {{xo, sb}, {h, n * 2}};
+  const Buf ins[7] = {{x, sb}, {y, n * 2}, mods[0], mods[1], mods[2], mods[3], mods[4]};
+  if (any_overlap(outs, ins, 0, 0)) return VIDAX_ERR_INVALID_ARG;
+  if (st != VIDAX_OK || n == 0) return st;
+  if (!vidax::launch_block_norm_fwd) return VIDAX_ERR_LAUNCH;
+  a.x = x;
+  a.y = (const uint16_t*)y;
+  a.xo = xo;
+  a.h = (uint16_t*)h;
+  return vidax::launch_block_norm_fwd(a, stream) == hipSuccess ? VIDAX_OK : VIDAX_ERR_LAUNCH;
+}
+
+size_t vidax_block_norm_bwd_workspace_floats(int32_t B, int32_t L, int32_t C) {
+  if (B < 0 || L < 0 || C < 0 || C % 8 != 0 || C > vidax::kBlockMaxC || (int64_t)B * L > INT32_MAX) return 0;
+  return B && L && C ? vidax::block_bwd_floats(B, L, C) : 0;
+}
+
+vidax_status vidax_block_norm_bwd(const void* dh, const void* dxo, const void* xo, const void* y, void* dx, void* dy,
+                                  const vidax_block_norm_grads* grads, float* workspace, size_t workspace_floats,
+                                  int32_t B, int32_t L, int32_t C, const vidax_block_norm_desc* desc,
+                                  hipStream_t stream) {
+  vidax::BlockNormBwd a;
+  Buf mods[5];
+  const vidax_status st = block_norm_common(B, L, C, desc, y != nullptr, &a.n, mods);
+  if (st == VIDAX_ERR_INVALID_ARG) return st;
+  if (!grads) return VIDAX_ERR_INVALID_ARG;
+  const bool per_token = desc->per_token != 0;
+  if (!per_token)
+    for (const vidax_block_mod* m : {&desc->gate, &desc->scale})
+      if (m->p && m->token_stride) return VIDAX_ERR_INVALID_ARG;
+  // dgate and dpost_gain need the branch; dpost_gain its norm
+  const uint64_t n = (uint64_t)B * L * C;
+  if ((grads->dgate && n > 0 && !y) || (grads->dpost_gain && (!desc->post || (n > 0 && !y)))) return VIDAX_ERR_INVALID_ARG;
+  const uint64_t sb = n * (desc->stream_fp32 ? 4 : 2);
+  const uint64_t mb = (per_token ? n : (uint64_t)B * C) * 4;
+  for (const void* p : {dh, dxo, xo, y, (const void*)dx, (const void*)dy, (const void*)grads->dgate,
+                        (const void*)grads->dscale, (const void*)grads->dshift, (const void*)grads->dgain,
+                        (const void*)grads->dpost_gain, (const void*)workspace})
+    if (!aligned(p, 16)) return VIDAX_ERR_INVALID_ARG;
+  if (n > 0 && (!dh || !xo || !dx || (y && !dy) || (!y && dy))) return VIDAX_ERR_INVALID_ARG;
+  if (workspace_floats > ((uint64_t)1 << 60)) return VIDAX_ERR_INVALID_ARG;
+  const bool sums = (!per_token && (grads->dgate || grads->dscale || grads->dshift)) || grads->dgain || grads->dpost_gain;
+  const Buf outs[8] = {{dx, sb}, {dy, n * 2}, {grads->dgate, mb}, {grads->dscale, mb}, {grads->dshift, mb},
+                       {grads->dgain, (uint64_t)C * 4}, {grads->dpost_gain, (uint64_t)C * 4},
+                       {workspace, (uint64_t)workspace_floats * 4}};
+  const Buf ins[8] = {{dxo, sb}, {dh, n * 2}, {xo, sb}, {y, n * 2}, mods[0], mods[1], mods[3], mods[4]};
+  if (any_overlap(outs, ins, 0, 0)) return VIDAX_ERR_INVALID_ARG;
+  if (st != VIDAX_OK) return st;
+  if (n > 0 && sums && (!workspace || workspace_floats < vidax::block_bwd_floats(B, L, C))) return VIDAX_ERR_INVALID_ARG;
+  if (C == 0 || (n == 0 && !sums)) return VIDAX_OK;  // (without tokens the sums are zero)
+  if (!vidax::launch_block_norm_bwd) return VIDAX_ERR_LAUNCH;
+  a.dh = (const uint16_t*)dh;
+  a.dxo = dxo;
+  a.xo = xo;
+  a.y = (const uint16_t*)y;
+  a.dx = dx;
+  a.dy = (uint16_t*)dy;
+  a.dgate = grads->dgate;
+  a.dscale = grads->dscale;
+  a.dshift = grads->dshift;
+  a.dgain = grads->dgain;
+  a.dpost_gain = grads->dpost_gain;
+  a.per_token = desc->per_token;
+  a.ws = workspace;
+  return vidax::launch_block_norm_bwd(a, stream) == hipSuccess ? VIDAX_OK : VIDAX_ERR_LAUNCH;
 }
 
 const char* vidax_status_string(int32_t status) {

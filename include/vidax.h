@@ -288,6 +288,68 @@ vidax_status vidax_qkv_proj(const void* x, const void* w, const float* bias, con
                             int32_t H, int32_t d, int32_t C, const vidax_rope3d_desc* rope, hipStream_t stream);
 
 /*
+ * What attention with score modifiers does to the scores, and which keys a
+ * query sees (porting-bug table, "Sharding, Parallelism & Custom Kernels":
+ * segment ids instead of a dense mask; Section 3: causal beside full attention).
+ * For batch b, query head h, query i at position p_i = q_start[b] + i and key j:
+ *
+ *   s_ij = scale <q_i, k_j>
+ *   s_ij = cap * tanh(s_ij / cap)             with a cap
+ *   s_ij = s_ij - slopes[h] * |p_i - j|       with slopes
+ *
+ * and key j takes part in the softmax of query i only if all of these hold:
+ *   j < kv_valid_len[b] (clamped to [0, Lk]),
+ *   q_doc[b, i] == k_doc[b, j] >= 0           with documents (ids in any order;
+ *                                             a negative id belongs to none),
+ *   j <= p_i  or  j < prefix_len[b]           with causal.
+ * A query that sees no key gives o = 0, lse = -inf and passes no gradient.
+ * All pointers are device pointers, 4-byte aligned, NULL where absent.
+ */
+typedef struct vidax_score_desc {
+  int32_t causal;               /* 0 or 1 */
+  float cap;                    /* > 0, or 0: none */
+  const float* slopes;          /* fp32 [H]; constants: they get no gradient */
+  const int32_t* q_doc;         /* int32 [B, Lq] and */
+  const int32_t* k_doc;         /* int32 [B, Lk]: both or neither */
+  const int32_t* kv_valid_len;  /* int32 [B]; NULL: Lk */
+  const int32_t* prefix_len;    /* int32 [B], requires causal; NULL: 0 */
+  const int32_t* q_start;       /* int32 [B], clamped to +-2^30; NULL: Lk - Lq (the
+                                   queries are the last tokens of the keys) */
+} vidax_score_desc;
+
+/*
+ * o_i = sum_j softmax_j(s_ij) v_j over the keys that query i sees.
+ *   q, o : bf16 [B, Lq, H, d];  k, v : bf16 [B, Lk, Hkv, d], Hkv a divisor of H:
+ *          query head h reads K/V head h / (H / Hkv).
+ *   lse  : fp32 [B, H, Lq], natural-log sum-exp of the seen scores, or NULL.
+ *   score: host pointer, or NULL (no modifier, all keys seen).
+ *   workspace: fp32 device memory, 16-byte aligned.  With documents at least
+ *          2 B (2 ceil(Lk / 64) + 2 ceil(Lq / 64)) values (VIDAX_ERR_INVALID_ARG
+ *          below); otherwise NULL is allowed.  With at least
+ *          vidax_attn_mod_fwd_workspace_floats(...) values, calls of few query
+ *          rows cut the keys into runs that work side by side; with fewer they
+ *          take the runs that fit.  The result differs by fp32 rounding only.
+ * What lies in k and v where no query of the call can see it (past
+ * kv_valid_len, behind the last query's position, at keys of negative documents)
+ * never reaches an output, whatever it holds; k and v of the other keys must be
+ * finite, also for queries that do not see them.
+ * Products on bf16 inputs with fp32 accumulation, softmax in fp32, the weights
+ * rounded to bf16 before the product with v.  Requires d == 128; device pointers
+ * 16-byte aligned; outputs and workspace must not overlap each other or an
+ * input.  One batch of q, Lq * H * d * 2 bytes, and 64 tokens of k must stay
+ * below 2 GiB - 4 KiB (VIDAX_ERR_UNSUPPORTED beyond).  scale finite.
+ */
+vidax_status vidax_attn_mod_fwd(const void* q, const void* k, const void* v, void* o, float* lse, int32_t B, int32_t H,
+                                int32_t Hkv, int32_t Lq, int32_t Lk, int32_t d, float scale,
+                                const vidax_score_desc* score, float* workspace, size_t workspace_floats,
+                                hipStream_t stream);
+
+/* fp32 values of that workspace on the current device (docs: 1 with documents);
+ * 0 for invalid arguments or where none is needed. */
+size_t vidax_attn_mod_fwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, int32_t Lq, int32_t Lk, int32_t d,
+                                           int32_t docs);
+
+/*
  * The step between two sublayers of a block (Section 3, "Supported Models":
  * adaptive layer norm per sample or per token; the paper gives no formula):
  * the sublayer's output y joins the residual stream x, and the sum is

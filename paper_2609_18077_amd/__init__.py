@@ -29,6 +29,8 @@ EXPORTED_SYMBOLS = (
     "vidax_na3d_fwd",
     "vidax_qkv_proj",
     "vidax_qk_norm_rope",
+    "vidax_attn_mod_fwd",
+    "vidax_attn_mod_fwd_workspace_floats",
     "vidax_block_norm_fwd",
     "vidax_block_norm_bwd",
     "vidax_block_norm_bwd_workspace_floats",
@@ -73,6 +75,34 @@ class Rope:
 
     def desc(self) -> RopeDesc:
         return RopeDesc(*self.grid, *self.dims, float(self.theta), int(self.pair_mode), int(self.keys_prerotated))
+
+
+class ScoreDesc(ctypes.Structure):
+    """Mirror of vidax_score_desc."""
+
+    _fields_ = [("causal", ctypes.c_int32), ("cap", ctypes.c_float)] + [
+        (n, ctypes.c_void_p) for n in ("slopes", "q_doc", "k_doc", "kv_valid_len", "prefix_len", "q_start")]
+
+
+@dataclass(frozen=True)
+class Score:
+    """What attention does to its scores and which keys a query sees.
+
+    causal: key j only up to the query's position, or j < prefix_len[b]; cap:
+    scores become cap * tanh(score / cap) (0: none); slopes: float32 [H], slope *
+    |position - j| is subtracted; q_doc, k_doc: int32 [B, Lq] and [B, Lk], only
+    keys of the query's own document are seen (a negative id belongs to none);
+    kv_valid_len, prefix_len: int32 [B]; q_start: int32 [B], the position of
+    query 0 (default: Lk - Lq).  All tensors are device tensors."""
+
+    causal: bool = False
+    cap: float = 0.0
+    slopes: object = None
+    q_doc: object = None
+    k_doc: object = None
+    kv_valid_len: object = None
+    prefix_len: object = None
+    q_start: object = None
 
 
 class BlockMod(ctypes.Structure):
@@ -135,6 +165,10 @@ def lib() -> ctypes.CDLL:
         L.vidax_qkv_proj.restype = i32
         L.vidax_qk_norm_rope.argtypes = [vp, vp, vp, f32, i32, i32, i32, i32, ctypes.POINTER(RopeDesc), vp]
         L.vidax_qk_norm_rope.restype = i32
+        L.vidax_attn_mod_fwd.argtypes = ([vp] * 5 + [i32] * 6 + [f32, ctypes.POINTER(ScoreDesc), vp, ctypes.c_size_t, vp])
+        L.vidax_attn_mod_fwd.restype = i32
+        L.vidax_attn_mod_fwd_workspace_floats.argtypes = [i32] * 7
+        L.vidax_attn_mod_fwd_workspace_floats.restype = ctypes.c_size_t
         L.vidax_block_norm_fwd.argtypes = [vp] * 4 + [i32] * 3 + [ctypes.POINTER(BlockNormDesc), vp]
         L.vidax_block_norm_fwd.restype = i32
         L.vidax_block_norm_bwd.argtypes = ([vp] * 6 + [ctypes.POINTER(BlockNormGrads), vp, ctypes.c_size_t]
@@ -372,7 +406,14 @@ def attn_fwd_naive(q, k, v, scale=None, kv_valid_len=None, rope: Rope | None = N
     return _attn("vidax_attn_fwd_naive", q, k, v, scale, kv_valid_len, rope, return_lse, out, stream)
 
 
-# ------------------------------------------------------- block norm ----
+def _on(device, fn, *args):
+    """fn(*args) with that device current."""
+    import torch
+
+    if device.index == torch.cuda.current_device():
+        return fn(*args)
+    with torch.cuda.device(device):
+        return fn(*args)
 
 
 def _call(fn: str, device, stream, *args):
@@ -380,12 +421,7 @@ def _call(fn: str, device, stream, *args):
     import torch
 
     s = torch.cuda.current_stream(device) if stream is None else stream
-    h = ctypes.c_void_p(s.cuda_stream)
-    if device.index == torch.cuda.current_device():
-        st = getattr(lib(), fn)(*args, h)
-    else:
-        with torch.cuda.device(device):
-            st = getattr(lib(), fn)(*args, h)
+    st = _on(device, getattr(lib(), fn), *args, ctypes.c_void_p(s.cuda_stream))
     if st != VIDAX_OK:
         raise VidaxError(fn, st)
 
@@ -394,6 +430,78 @@ def _check_dense(name, t, dtype, shape, device):
     if t.dtype != dtype or t.device != device or not t.is_contiguous() or t.shape != shape:
         raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} tensor on {device}")
 
+
+# ------------------------------------- attention with score modifiers ----
+
+_SCALE_128 = 0.08838834764831845  # 1 / sqrt(128), rounded to fp32 at the call
+
+
+def _score_desc(score, q, Lk):
+    """Descriptor of a Score for queries q [B, Lq, H, d] against Lk keys."""
+    import torch
+
+    s = Score() if score is None else score
+    B, Lq, H, _ = q.shape
+    if (s.q_doc is None) != (s.k_doc is None):
+        raise ValueError("q_doc and k_doc come together")
+    if s.slopes is not None:
+        _check_dense("slopes", s.slopes, torch.float32, (H,), q.device)
+    for n, shape in (("q_doc", (B, Lq)), ("k_doc", (B, Lk)), ("kv_valid_len", (B,)), ("prefix_len", (B,)),
+                     ("q_start", (B,))):
+        t = getattr(s, n)
+        if t is not None:
+            _check_dense(n, t, torch.int32, shape, q.device)
+    return ScoreDesc(int(s.causal), float(s.cap), *(None if t is None else t.data_ptr() for t in (
+        s.slopes, s.q_doc, s.k_doc, s.kv_valid_len, s.prefix_len, s.q_start)))
+
+
+def _check_mod_qkv(q, k, v):
+    for n, t in (("q", q), ("k", k), ("v", v)):
+        _check_bshd(n, t)
+    if k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
+        raise ValueError("k and v must be [B, Lk, Hkv, d] matching q's B and d")
+    if k.device != q.device or v.device != q.device:
+        raise ValueError("q, k and v must be on one device")
+
+
+def _workspace(workspace, need, device):
+    """The caller's float32 workspace, checked, or a new one of `need` values (None for 0)."""
+    import torch
+
+    if workspace is None:
+        return torch.empty((need,), dtype=torch.float32, device=device) if need else None
+    if workspace.dtype != torch.float32 or workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous float32 tensor on {device}")
+    return workspace
+
+
+def attn_mod_fwd(q, k, v, score: Score | None = None, scale=None, return_lse=False, out=None, workspace=None,
+                 stream=None):
+    """Attention with score modifiers: o (and lse) of q bf16 [B, Lq, H, 128] and
+    k, v bf16 [B, Lk, Hkv, 128], Hkv a divisor of H.  `workspace`: a contiguous
+    float32 device tensor (by default one of vidax_attn_mod_fwd_workspace_floats
+    values is allocated where the call needs one)."""
+    import torch
+
+    _check_mod_qkv(q, k, v)
+    B, Lq, H, d = q.shape
+    Lk, Hkv = k.shape[1], k.shape[2]
+    desc = _score_desc(score, q, Lk)
+    o = torch.empty_like(q) if out is None else out
+    if out is not None:
+        _check_dense("out", o, q.dtype, q.shape, q.device)
+    lse = torch.empty((B, H, Lq), dtype=torch.float32, device=q.device) if return_lse else None
+    if workspace is None:
+        need = _on(q.device, lib().vidax_attn_mod_fwd_workspace_floats, B, H, Hkv, Lq, Lk, d, int(desc.k_doc is not None))
+        ws = _workspace(None, need, q.device)
+    else:
+        ws = _workspace(workspace, 0, q.device)
+    _call("vidax_attn_mod_fwd", q.device, stream, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), B, H, Hkv, Lq, Lk, d,
+          _SCALE_128 if scale is None else float(scale), ctypes.byref(desc), _ptr(ws), 0 if ws is None else ws.numel())
+    return (o, lse) if return_lse else o
+
+
+# -------------------------------------------------------- block norm ----
 
 _NORMS = {None: 0, "layer": 1, "rms": 2}
 
@@ -496,12 +604,7 @@ def block_norm_bwd(dh, dx, x, y=None, gate=None, scale=None, shift=None, gain=No
             got[n] = torch.empty(t.shape, dtype=torch.float32, device=x.device)
     g = BlockNormGrads(*(got[n].data_ptr() if n in got else None for n, _ in BlockNormGrads._fields_))
     sums = (not d.per_token and len(token) > 0) or gain is not None or post_gain is not None
-    if workspace is not None:
-        if (workspace.dtype != torch.float32 or workspace.device != x.device or not workspace.is_contiguous()):
-            raise ValueError(f"workspace must be a contiguous float32 tensor on {x.device}")
-    elif sums:
-        n = lib().vidax_block_norm_bwd_workspace_floats(B, L, C)
-        workspace = torch.empty((n,), dtype=torch.float32, device=x.device)
+    workspace = _workspace(workspace, lib().vidax_block_norm_bwd_workspace_floats(B, L, C) if sums else 0, x.device)
     _call("vidax_block_norm_bwd", x.device, stream, _ptr(dh), _ptr(dx), _ptr(x), _ptr(y), _ptr(got["dx"]),
           _ptr(got.get("dy")), ctypes.byref(g), _ptr(workspace), 0 if workspace is None else workspace.numel(), B, L, C,
           ctypes.byref(d))

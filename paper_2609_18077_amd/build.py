@@ -39,6 +39,7 @@ HIPCC_FLAGS = [
 # benchmark shape); the other kernels are slower with it, so it is not global.
 SOURCE_FLAGS = {
     "attn_fwd_split.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"],
+    "attn_mod_fwd.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"],
     "attn_fwd.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"],
 }
 

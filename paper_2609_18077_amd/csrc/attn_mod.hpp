@@ -1,0 +1,110 @@
+// Device definitions shared by the kernels of attention with score modifiers:
+// visibility, the cap, and the search for the next tile that a workgroup has to
+// visit.
+#pragma once
+
+#include "attn_tile.hpp"
+#include "launch_mod.hpp"
+
+namespace vidax {
+namespace mod {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.69314718055994531f;
+constexpr int kStartLimit = 1 << 30;  // positions stay within +- 2^30 + L
+
+// Scores in log2 units: y = mul * f(q.k) with f the identity (mul = |scale|
+// log2 e; the sign of scale goes into q) or, capped, t = tanh(ku q.k) (mul = cap
+// log2 e, ku = |scale| / cap).
+struct Scores {
+  float mul, ku;
+  uint32_t qxor, qand;  // applied to q's bf16 pairs: sign of scale, zero where it is 0
+};
+
+inline Scores make_scores(const ModCall& c) {
+  Scores s;
+  const float a = c.scale < 0.f ? -c.scale : c.scale;
+  s.qxor = c.scale < 0.f ? 0x80008000u : 0u;
+  s.qand = a == 0.f ? 0u : 0xffffffffu;
+  s.ku = c.s.cap > 0.f ? a / c.s.cap : 0.f;
+  s.mul = c.s.cap > 0.f ? c.s.cap * kLog2e : a == 0.f ? 1.f : a * kLog2e;
+  return s;
+}
+
+// tanh of 16 products times ku, in place.  An odd polynomial of degree 9 where
+// the whole wave's block stays within 1/2 (its error there is 1.2e-7 of the value;
+// coefficients by least squares on Chebyshev points), else by the exponential,
+// whose absolute error of 1e-7 is then small against the block's largest score.
+__device__ __forceinline__ float tanh_small(float u) {
+  const float w = u * u;
+  float p = fmaf(w, 1.799921878e-2f, -5.339105427e-2f);
+  p = fmaf(w, p, 1.333051324e-1f);
+  p = fmaf(w, p, -3.333331048e-1f);
+  p = fmaf(w, p, 1.0f);
+  return u * p;
+}
+__device__ __forceinline__ float tanh_any(float u) {
+  const float e = __builtin_amdgcn_exp2f(u * (2.f * kLog2e));
+  return fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f);
+}
+__device__ __forceinline__ void cap16(f32x16& s, float ku) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    s[i] *= ku;
+    m = fmaxf(m, fabsf(s[i]));
+  }
+  if (__builtin_amdgcn_ballot_w64(!(m <= 0.5f)) == 0) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = tanh_small(s[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = tanh_any(s[i]);
+  }
+}
+
+// Batch values (uniform).
+struct Batch {
+  int lv;      // keys j < lv exist
+  int start;   // position of query 0
+  int prefix;  // causal: keys j < prefix are seen by all
+};
+__device__ __forceinline__ Batch batch_of(const ModCall& c, int b) {
+  Batch r;
+  r.lv = c.Lk;
+  if (c.s.kv_valid_len) r.lv = min(max(c.s.kv_valid_len[b], 0), c.Lk);
+  r.start = c.Lk - c.Lq;
+  if (c.s.q_start) r.start = min(max(c.s.q_start[b], -kStartLimit), kStartLimit);
+  r.prefix = c.s.prefix_len ? max(c.s.prefix_len[b], 0) : 0;
+  r.lv = __builtin_amdgcn_readfirstlane(r.lv);
+  r.start = __builtin_amdgcn_readfirstlane(r.start);
+  r.prefix = __builtin_amdgcn_readfirstlane(r.prefix);
+  return r;
+}
+// Keys that a query at position p sees, documents apart: [0, key_limit).
+__device__ __forceinline__ int key_limit(const Batch& b, int causal, int p) {
+  return causal ? min(b.lv, max(max(p + 1, 0), b.prefix)) : b.lv;
+}
+
+// Document range of some tokens: least and largest id >= 0 (least > largest:
+// none), and whether an id < 0 is among them.
+struct Docs {
+  int lo, hi;
+  bool neg;
+};
+__device__ __forceinline__ Docs docs_of(int2 r) { return Docs{r.x, r.y & 0x7fffffff, r.y < 0}; }
+__device__ __forceinline__ Docs join(const Docs& a, const Docs& b) {
+  return Docs{min(a.lo, b.lo), max(a.hi, b.hi), a.neg || b.neg};
+}
+__device__ __forceinline__ Docs uniform(const Docs& d) {
+  return Docs{__builtin_amdgcn_readfirstlane(d.lo), __builtin_amdgcn_readfirstlane(d.hi),
+              (bool)__builtin_amdgcn_readfirstlane((int)d.neg)};
+}
+__device__ __forceinline__ bool meet(const Docs& a, const Docs& b) { return a.lo <= b.hi && b.lo <= a.hi; }
+// every token of both in one and the same document
+__device__ __forceinline__ bool same(const Docs& a, const Docs& b) {
+  return !a.neg && !b.neg && a.lo == a.hi && b.lo == b.hi && a.lo == b.lo;
+}
+
+}  // namespace mod
+}  // namespace vidax

@@ -1,0 +1,525 @@
+// Attention with score modifiers, forward, for gfx950: 256 query rows of one
+// (batch, head) a workgroup, bf16 MFMA (32x32x16) with fp32 accumulation and a
+// streaming softmax.  Head dim 128.
+//
+//   y_ij = log2 e * (cap tanh(scale q.k / cap) - slope |p_i - j|),  o = softmax2(y) v
+//
+// The dataflow is the dense forward's (attn_fwd.hip): a wave owns 32 query rows,
+// S^T = K Q^T puts a query in each lane, keys and values stream through LDS in
+// tiles of 64 in operand order, two buffers each, one barrier a tile, the scores
+// of the next tile formed beside the softmax of this one.  What differs:
+//   Tiles.  The workgroup visits the tiles that one of its rows may see, found 64
+//     at a time by a ballot over the tiles' document ranges and the causal limits;
+//     a wave whose own 32 rows see nothing of a tile leaves its products out, and
+//     only a wave for which a tile is not seen whole by all its rows masks it.
+//   Masks.  A score that is not seen becomes -inf after the cap.  A row's
+//     reference m is unset until it has seen a key: its sum starts at +inf, which
+//     sends every block through the reset until then.  A row that sees nothing
+//     ends with a sum of 0: o = 0, lse = -inf.  Keys that no row may see (past
+//     the valid length or the last row's position, or of a negative document) are
+//     read as zeros, so that nothing that lies there reaches the output.
+//   Sums add the fp32 probabilities, not their bf16 roundings: the log-sum-exp is
+//     then good to fp32, and costs eight additions a block more.
+//   Few tiles of rows: the keys are cut into runs, a workgroup each, whose
+//     normalised fp32 outputs and log-sum-exps a second launch joins.
+#include "attn_mod.hpp"
+#include "launch.hpp"
+
+namespace vidax {
+namespace {
+
+using namespace tile;
+using namespace mod;
+
+constexpr int D = kHeadDim;
+constexpr int BM = kModRows;
+constexpr int BN = kModKeys;
+constexpr int NW = 8;
+constexpr int NT = NW * 64;
+constexpr int TILE = BN * D;  // elements of a K or V tile
+constexpr int BLK = 512;      // elements of an operand block
+constexpr int kNoTile = -1;
+
+struct FwdArgs {
+  ModCall c;
+  Scores sc;
+  const uint16_t *q, *k, *v;
+  uint16_t* o;
+  float* lse;
+  float *po, *pl;  // partial outputs [runs][B][H][Lq][D] and log2-sum-exps [runs][B][H][Lq], or null
+  ModRanges r;
+  int nqt, nwg, runs;
+  int kr, qr;      // document ranges a batch
+};
+
+// CAP, BIAS: the scores' modifiers.
+template <bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
+  __shared__ __attribute__((aligned(16))) uint16_t K0[TILE], K1[TILE], V0[TILE], V1[TILE];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31;
+  const int hi = lane >> 5;
+  const ModCall& c = a.c;
+  const int qtok = c.H * D, ktok = c.Hkv * D;  // elements between tokens
+  const int qbytes = qtok * 2, kbytes = ktok * 2;
+
+  // Runs of one tile are neighbours (they share its queries), then the tiles of
+  // one head (they share its keys).  Causal tiles are taken from both ends in
+  // turn: any stretch of a head's tiles is then about the same work.
+  const int lid = balanced_tile(blockIdx.x, a.nwg, c.B);
+  const int run = lid % a.runs, t0 = lid / a.runs;
+  int qt = t0 % a.nqt;
+  if (c.s.causal) qt = qt & 1 ? qt >> 1 : a.nqt - 1 - (qt >> 1);
+  const int bh = t0 / a.nqt, h = bh % c.H, b = bh / c.H, hk = h / (c.H / c.Hkv);
+  const Batch bt = batch_of(c, b);
+  const int row0 = qt * BM;                     // of the workgroup
+  const int wrow = row0 + wave * 32;            // of the wave
+  const int qrow = wrow + l32;
+  const bool qlive = qrow < c.Lq;
+  const int wlast = min(wrow + 32, c.Lq) - 1;   // last row of the wave (< wrow: none)
+  const int glast = min(row0 + BM, c.Lq) - 1;
+  const uint16_t* const kbh = a.k + (size_t)b * c.Lk * ktok + (size_t)hk * D;
+  const uint16_t* const vbh = a.v + (size_t)b * c.Lk * ktok + (size_t)hk * D;
+
+  // ---- what the lane's row, the wave's rows and the workgroup's rows may see
+  int lim = qlive ? key_limit(bt, c.s.causal, bt.start + qrow) : 0;
+  int qd = 0;
+  Docs wdoc{0, 0, false}, gdoc{0, 0, false};
+  const bool docs = a.r.k != nullptr;
+  if (docs) {
+    if (qlive) qd = c.s.q_doc[(size_t)b * c.Lq + qrow];
+    if (qd < 0) lim = 0;
+    const int2* const qr = a.r.q + (size_t)b * a.qr;
+    const int first = row0 >> 5;
+    gdoc = docs_of(qr[first]);
+    for (int i = 1; i < BM / 32; ++i)
+      if (first + i < a.qr) gdoc = join(gdoc, docs_of(qr[first + i]));
+    gdoc = uniform(gdoc);
+    wdoc = wrow < c.Lq ? uniform(docs_of(qr[wrow >> 5])) : Docs{0x7fffffff, 0, false};
+  }
+  const int wmax = wlast >= wrow ? key_limit(bt, c.s.causal, bt.start + wlast) : 0;
+  const int wmin = wlast >= wrow ? key_limit(bt, c.s.causal, bt.start + wrow) : 0;
+  const int gmax = key_limit(bt, c.s.causal, bt.start + glast);
+  const int ntiles = (gmax + BN - 1) / BN;
+  const int first_tile = (int)((int64_t)ntiles * run / a.runs), end_tile = (int)((int64_t)ntiles * (run + 1) / a.runs);
+
+  // ---- the next tile to visit: a group of 64 tiles is looked at together, lane
+  // l at tile 64 g + l.  (visit: some row of the workgroup may see a key of it;
+  // mine, whole: the same for the wave, all its rows see all of it; neg: it holds
+  // keys of negative documents.)
+  int grp = first_tile >> 6;
+  uint64_t visit = 0, mine = 0, whole = 0, neg = 0;
+  auto look = [&](int g) __attribute__((always_inline)) {
+    const int t = 64 * g + lane;
+    const bool in = t >= first_tile && t < end_tile;
+    bool v = in, m = in && t * BN < wmax, w = in && t * BN + BN <= wmin, n = false;
+    if (docs && in) {
+      const int4 r = *reinterpret_cast<const int4*>(a.r.k + (size_t)b * a.kr + 2 * t);
+      const Docs d = mod::join(docs_of(make_int2(r.x, r.y)), docs_of(make_int2(r.z, r.w)));
+      v = meet(d, gdoc);
+      m = m && meet(d, wdoc);
+      w = w && same(d, wdoc);
+      n = d.neg;
+    }
+    visit = __builtin_amdgcn_ballot_w64(v);
+    mine = __builtin_amdgcn_ballot_w64(m);
+    whole = __builtin_amdgcn_ballot_w64(w);
+    neg = __builtin_amdgcn_ballot_w64(n);
+  };
+  struct Tile {
+    int t;             // kNoTile: none left
+    bool mine, whole, neg;
+  };
+  auto next = [&]() __attribute__((always_inline)) {
+    while (visit == 0) {
+      if (64 * (grp + 1) >= end_tile) return Tile{kNoTile, false, false, false};
+      look(++grp);
+    }
+    const int i = __builtin_ctzll(visit);
+    visit &= visit - 1;
+    return Tile{64 * grp + i, (bool)(mine >> i & 1), (bool)(whole >> i & 1), (bool)(neg >> i & 1)};
+  };
+
+  uint16_t* const stage = (wave < 2 ? K0 : wave < 4 ? K1 : wave < 6 ? V0 : V1) + (wave & 1) * 32 * D;
+
+  // The wave's 32 query rows whole into its staging area, then out of it as B
+  // operands (chunk 2 s + hi of the lane's own row).
+  bf16x8 qreg[8];
+  auto dma_q = [&]() __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t rq = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(a.q + (size_t)b * c.Lq * qtok + (size_t)h * D), (short)0, c.Lq * qbytes, kBufferFlags);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 4 * i + (lane >> 4);
+      const int off = wrow + r < c.Lq ? (wrow + r) * qbytes + stage_slot(lane & 15, r) * 16 : 0x7ffffff0;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_ptr)(stage + 4 * i * D), 16, off, 0, 0, 0);
+    }
+  };
+  auto take_q = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const uint4 x = *reinterpret_cast<const uint4*>(stage + l32 * D + stage_slot(2 * s + hi, l32) * 8);
+      qreg[s] = __builtin_bit_cast(bf16x8, make_uint4((x.x ^ a.sc.qxor) & a.sc.qand, (x.y ^ a.sc.qxor) & a.sc.qand,
+                                                      (x.z ^ a.sc.qxor) & a.sc.qand, (x.w ^ a.sc.qxor) & a.sc.qand));
+    }
+  };
+
+  // ---- copies (as in the dense forward): wave w fills blocks 2 w, 2 w + 1 of a
+  // K and of a V tile; records end at the last key that a row may see
+  const int kg0 = l32 * kbytes + (2 * wave + hi) * 16, kg1 = kg0 + 32 * kbytes;
+  const int vrow = 8 * hi + 4 * ((lane >> 4) & 1) + ((lane & 7) >> 1);
+  const int vd = 16 * ((lane >> 3) & 1) + 8 * (lane & 1);
+  const int vr = vrow + 16 * (wave >> 1);  // blocks 2 wave and 2 wave + 1 are of one key step
+  const int vg0 = vr * kbytes + 2 * (vd + 32 * (2 * wave & 3)), vg1 = vg0 + 64;
+  auto tile_rsrc = [&](const uint16_t* base, int t) __attribute__((always_inline)) {
+    const int nbytes = __builtin_amdgcn_readfirstlane(min(max(gmax - t * BN, 0), BN) * kbytes);
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (size_t)t * BN * ktok), (short)0, nbytes, kBufferFlags);
+  };
+  auto dma_k = [&](int t, uint16_t* buf) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t rs = tile_rsrc(kbh, t);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(buf + (2 * wave) * BLK), 16, kg0, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(buf + (2 * wave + 1) * BLK), 16, kg1, 0, 0, 0);
+  };
+  auto dma_v = [&](const Tile& t, uint16_t* buf) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t rs = tile_rsrc(vbh, t.t);
+    int g0 = vg0, g1 = vg1;
+    if (t.neg) {  // uniform: values of keys of negative documents arrive as zeros
+      const int key = t.t * BN + vr;
+      if (key >= c.Lk || c.s.k_doc[(size_t)b * c.Lk + min(key, c.Lk - 1)] < 0) g0 = g1 = 0x7ffffff0;
+    }
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(buf + (2 * wave) * BLK), 16, g0, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(buf + (2 * wave + 1) * BLK), 16, g1, 0, 0, 0);
+  };
+
+  const int koff = lane * 8, voff = lane * 4;
+  auto qk = [&](const uint16_t* kb, f32x16 s[2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int st = 0; st < 8; ++st)
+#pragma unroll
+      for (int blk = 0; blk < 2; ++blk) {
+        const bf16x8 kop = *reinterpret_cast<const bf16x8*>(kb + (2 * st + blk) * BLK + koff);
+        s[blk] = mfma32(kop, qreg[st], st == 0 ? f32x16{} : s[blk]);
+      }
+  };
+
+  f32x16 oacc[4];
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb) oacc[mb] = f32x16{};
+  float mref = -INFINITY;  // the row's reference, log2 units
+  float nm = 0.f;          // -mref, 0 while unset
+  float sum0 = INFINITY;   // +inf until the row has a reference: forces the reset
+  float lsum = 0.f;        // this lane half's sum
+  const float mul = a.sc.mul;
+  const float slope = BIAS ? -c.s.slopes[h] * kLog2e : 0.f;
+
+  // y + n of element i of a block; dist: position minus the block's first key of this lane half
+  auto logit = [&](float s, float n, float dist, int i) __attribute__((always_inline)) {
+    float y = fmaf(s, mul, n);
+    if (BIAS) y = fmaf(slope, fabsf(dist - (float)(8 * (i >> 2) + (i & 3))), y);
+    return y;
+  };
+  auto softmax_p = [&](const f32x16& s, bf16x8 pop[2], float tsum, float dist) __attribute__((always_inline)) {
+    float odd = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      uint32_t pw[4];
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(logit(s[8 * ks + e], nm, dist, 8 * ks + e));
+        const float p1 = __builtin_amdgcn_exp2f(logit(s[8 * ks + e + 1], nm, dist, 8 * ks + e + 1));
+        pw[e >> 1] = pack_bf16x2(p0, p1);  // one rounding of the weights: 2^-9 of each, independent
+        tsum += p0;
+        odd += p1;
+      }
+      pop[ks] = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+    }
+    return tsum + odd;
+  };
+  auto softmax_blk = [&](f32x16& s, bf16x8 pop[2], float dist) __attribute__((always_inline)) {
+    float tsum = softmax_p(s, pop, sum0, dist);
+    if (__builtin_amdgcn_ballot_w64(!(tsum < kSumLimit)) != 0) {
+      float m = logit(s[0], 0.f, dist, 0);
+#pragma unroll
+      for (int i = 1; i < 16; ++i) m = fmaxf(m, logit(s[i], 0.f, dist, i));
+      const float mnew = fmaxf(mref, wave_half_max(m));
+      const bool set = mnew > -INFINITY;
+      const float alpha = set ? __builtin_amdgcn_exp2f(mref - mnew) : 1.f;
+      lsum *= alpha;
+#pragma unroll
+      for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
+      mref = mnew;
+      nm = set ? -mnew : 0.f;
+      sum0 = set ? 0.f : INFINITY;
+      tsum = softmax_p(s, pop, 0.f, dist);
+    }
+    lsum += tsum;
+  };
+  auto pv_blk = [&](const uint16_t* vb, const bf16x8 pop[2], int blk) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2) {
+      const int ks = 2 * blk + k2;
+#pragma unroll
+      for (int mb = 0; mb < 4; ++mb) {
+        const i16x4 lo = lds_read_tr16(vb + (4 * ks + mb) * BLK + voff);
+        const i16x4 hi4 = lds_read_tr16(vb + (4 * ks + mb) * BLK + BLK / 2 + voff);
+        const bf16x8 vop = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
+        oacc[mb] = mfma32(vop, pop[k2], oacc[mb]);
+      }
+    }
+  };
+  // -inf for what the lane's row does not see of the tile
+  auto mask = [&](f32x16 s[2], int t) __attribute__((always_inline)) {
+    const int left = lim - t * BN - 4 * hi;
+#pragma unroll
+    for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (32 * blk + 8 * (i >> 2) + (i & 3) >= left) s[blk][i] = -INFINITY;
+    if (docs) {
+      // ids past Lk: past the buffer's records (the limit has masked them)
+      const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc(
+          (void*)(c.s.k_doc + (size_t)b * c.Lk), (short)0, c.Lk * 4, kBufferFlags);
+#pragma unroll
+      for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const u32x4 d = __builtin_amdgcn_raw_buffer_load_b128(rd, (t * BN + 32 * blk + 8 * g + 4 * hi) * 4, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if ((int)d[e] != qd) s[blk][4 * g + e] = -INFINITY;
+        }
+    }
+  };
+  auto softmax_pv = [&](f32x16 s[2], const uint16_t* vb, const Tile& t) __attribute__((always_inline)) {
+    bf16x8 pop0[2], pop1[2];
+    if (CAP) {
+      cap16(s[0], a.sc.ku);
+      cap16(s[1], a.sc.ku);
+    }
+    if (!t.whole) mask(s, t.t);  // uniform
+    const float dist = BIAS ? (float)(bt.start + qrow - t.t * BN - 4 * hi) : 0.f;
+    softmax_blk(s[0], pop0, dist);
+    pv_blk(vb, pop0, 0);
+    softmax_blk(s[1], pop1, dist - 32.f);
+    pv_blk(vb, pop1, 1);
+  };
+
+  // ---- output, whole rows through the staging area; empty rows: o = 0, lse = -inf
+  const size_t nrow = (size_t)c.B * c.H * c.Lq, orow = ((size_t)b * c.H + h) * c.Lq;
+  auto store_o = [&]() __attribute__((always_inline)) {
+    const float l = wave_half_sum(lsum);
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const float lse2 = l == 0.f ? -INFINITY : mref + __log2f(l);
+    if (a.po) {  // fp32 rows of this run
+      if (qlive) {
+        float* const p = a.po + ((size_t)run * nrow + orow + qrow) * D;
+#pragma unroll
+        for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<float4*>(p + 32 * mb + 8 * g + 4 * hi) =
+                make_float4(oacc[mb][4 * g] * inv, oacc[mb][4 * g + 1] * inv, oacc[mb][4 * g + 2] * inv,
+                            oacc[mb][4 * g + 3] * inv);
+        if (hi == 0) a.pl[(size_t)run * nrow + orow + qrow] = lse2;
+      }
+      return;
+    }
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        u32x2 pk;
+        pk[0] = pack_bf16x2(oacc[mb][4 * g + 0] * inv, oacc[mb][4 * g + 1] * inv);
+        pk[1] = pack_bf16x2(oacc[mb][4 * g + 2] * inv, oacc[mb][4 * g + 3] * inv);
+        *reinterpret_cast<u32x2*>(stage + l32 * D + stage_slot(4 * mb + g, l32) * 8 + 4 * hi) = pk;
+      }
+    wave_lds_fence();
+    const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(a.o + (size_t)b * c.Lq * qtok + (size_t)h * D), (short)0, c.Lq * qbytes, kBufferFlags);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 4 * i + (lane >> 4);
+      const u32x4 v = *reinterpret_cast<const u32x4*>(stage + r * D + (lane & 15) * 8);
+      const int grow = wrow + r;
+      const int off = grow < c.Lq ? grow * qbytes + stage_slot(lane & 15, r) * 16 : 0x7ffffff0;
+      __builtin_amdgcn_raw_buffer_store_b128(v, ro, off, 0, 0);
+    }
+    if (a.lse && qlive && hi == 0) a.lse[orow + qrow] = lse2 * kLn2;
+  };
+
+  Tile cur{kNoTile, false, false, false}, nxt = cur;
+  if (first_tile < end_tile) {
+    look(grp);
+    cur = next();
+    nxt = next();
+  }
+  if (cur.t == kNoTile) {  // nothing to see
+    store_o();
+    return;
+  }
+  dma_q();
+  __builtin_amdgcn_s_waitcnt(0);  // this wave's query rows have landed
+  take_q();
+  __syncthreads();  // every wave has its queries out of the K/V buffers
+  dma_k(cur.t, K0);
+  dma_v(cur, V0);
+  if (nxt.t != kNoTile) dma_k(nxt.t, K1);
+  __builtin_amdgcn_s_waitcnt(0);  // this wave's copies have landed in LDS
+  __syncthreads();
+  f32x16 sa[2], sb[2];
+  qk(K0, sa);
+  __syncthreads();  // the first step refills K0
+  // Step on the tile `cur` (parity of its buffers at compile time); false after the last
+  auto step = [&](auto parity, f32x16 scur[2], f32x16 snext[2]) __attribute__((always_inline)) {
+    constexpr int P = decltype(parity)::value;
+    const Tile aft = next();
+    if (aft.t != kNoTile) dma_k(aft.t, P ? K1 : K0);
+    if (nxt.t != kNoTile) {
+      dma_v(nxt, P ? V0 : V1);
+      if (nxt.mine) qk(P ? K0 : K1, snext);
+    }
+    if (cur.mine) softmax_pv(scur, P ? V1 : V0, cur);
+    cur = nxt;
+    nxt = aft;
+    __builtin_amdgcn_s_waitcnt(0);  // this wave's copies have landed
+    __syncthreads();
+    return cur.t != kNoTile;
+  };
+  while (step(std::integral_constant<int, 0>(), sa, sb) && step(std::integral_constant<int, 1>(), sb, sa)) {
+  }
+  store_o();
+}
+
+// Ranges of document ids of every 32 tokens: a wave takes 64 tokens of a batch.
+struct RangeArgs {
+  const int32_t *k, *q;
+  int2 *kr, *qr;
+  int B, Lk, Lq, nk, nq;  // groups of 64 tokens a batch
+};
+__global__ __launch_bounds__(256) void mod_ranges_kernel(RangeArgs a) {
+  const int lane = threadIdx.x & 63;
+  int w = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const bool isk = w < a.B * a.nk;
+  if (!isk) w -= a.B * a.nk;
+  const int n = isk ? a.nk : a.nq, L = isk ? a.Lk : a.Lq;
+  if (w >= a.B * n) return;
+  const int b = w / n, g = w - b * n, t = 64 * g + lane;
+  const bool live = t < L;
+  const int id = live ? (isk ? a.k : a.q)[(size_t)b * L + t] : -1;
+  int lo = id >= 0 ? id : 0x7fffffff, hi = id >= 0 ? id : 0;
+#pragma unroll
+  for (int m = 1; m < 32; m <<= 1) {
+    lo = min(lo, __shfl_xor(lo, m));
+    hi = max(hi, __shfl_xor(hi, m));
+  }
+  const uint64_t bad = __builtin_amdgcn_ballot_w64(live && id < 0);
+  const bool neg = (uint32_t)(lane < 32 ? bad : bad >> 32) != 0;
+  if ((lane & 31) == 0) {
+    int2* const out = (isk ? a.kr : a.qr) + (size_t)w * 2 + (lane >> 5);
+    *out = make_int2(lo, hi | (neg ? (int)0x80000000 : 0));
+  }
+}
+
+// Joins the runs of every (batch, head, query): a wave a row, lane l its
+// channels 2 l, 2 l + 1.  o = sum_r 2^(lse_r - max) o_r / sum_r 2^(lse_r - max).
+struct JoinArgs {
+  const float *po, *pl;
+  uint16_t* o;
+  float* lse;
+  int B, H, Lq, runs;
+};
+__global__ __launch_bounds__(256) void mod_join_kernel(JoinArgs a) {
+  const size_t nrow = (size_t)a.B * a.H * a.Lq;
+  const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // (b, h, i)
+  if (row >= nrow) return;
+  const int lane = threadIdx.x & 63;
+  float m = -INFINITY;
+  for (int r = 0; r < a.runs; ++r) m = fmaxf(m, a.pl[r * nrow + row]);
+  float x = 0.f, y = 0.f, l = 0.f;
+  if (m > -INFINITY) {
+#pragma unroll 4
+    for (int r = 0; r < a.runs; ++r) {
+      const float w = __builtin_amdgcn_exp2f(a.pl[r * nrow + row] - m);
+      const float2 v = *reinterpret_cast<const float2*>(a.po + (r * nrow + row) * D + 2 * lane);
+      l += w;
+      x = fmaf(w, v.x, x);
+      y = fmaf(w, v.y, y);
+    }
+    const float inv = 1.0f / l;
+    x *= inv;
+    y *= inv;
+  }
+  const size_t i = row % a.Lq, bh = row / a.Lq, b = bh / a.H, h = bh % a.H;
+  *reinterpret_cast<uint32_t*>(a.o + ((b * a.Lq + i) * a.H + h) * D + 2 * lane) = pack_bf16x2(x, y);
+  if (a.lse && lane == 0) a.lse[row] = m > -INFINITY ? (m + __log2f(l)) * kLn2 : -INFINITY;
+}
+
+}  // namespace
+
+hipError_t launch_mod_ranges(const ModCall& c, float* ws, ModRanges* out, hipStream_t stream) {
+  *out = ModRanges{nullptr, nullptr};
+  if (!c.s.k_doc) return hipSuccess;
+  RangeArgs a;
+  a.k = c.s.k_doc;
+  a.q = c.s.q_doc;
+  a.B = c.B;
+  a.Lk = c.Lk;
+  a.Lq = c.Lq;
+  a.nk = (int)(mod_ranges(c.Lk) / 2);
+  a.nq = (int)(mod_ranges(c.Lq) / 2);
+  a.kr = reinterpret_cast<int2*>(ws);
+  a.qr = a.kr + (size_t)c.B * mod_ranges(c.Lk);
+  *out = ModRanges{a.kr, a.qr};
+  const unsigned waves = (unsigned)c.B * (unsigned)(a.nk + a.nq);
+  return launch_kernel(mod_ranges_kernel, (waves + 3) / 4, 256u, stream, a);
+}
+
+hipError_t launch_mod_join(const ModFwd& f, const ModSplit& s, hipStream_t stream) {
+  JoinArgs a;
+  const size_t nrow = (size_t)f.c.B * f.c.H * f.c.Lq;
+  a.po = f.ws + s.part;
+  a.pl = a.po + (size_t)s.runs * nrow * D;
+  a.o = f.o;
+  a.lse = f.lse;
+  a.B = f.c.B;
+  a.H = f.c.H;
+  a.Lq = f.c.Lq;
+  a.runs = s.runs;
+  return launch_kernel(mod_join_kernel, (unsigned)((nrow + 3) / 4), 256u, stream, a);
+}
+
+hipError_t launch_attn_mod_fwd(const ModFwd& f, hipStream_t stream) {
+  const ModCall& c = f.c;
+  const ModSplit s = mod_fwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr, device_cu_count(), f.ws_floats);
+  FwdArgs a;
+  a.c = c;
+  a.sc = make_scores(c);
+  a.q = f.q;
+  a.k = f.k;
+  a.v = f.v;
+  a.o = f.o;
+  a.lse = f.lse;
+  a.nqt = (c.Lq + BM - 1) / BM;
+  a.runs = s.runs;
+  a.nwg = a.nqt * c.B * c.H * s.runs;
+  a.kr = (int)mod_ranges(c.Lk);
+  a.qr = (int)mod_ranges(c.Lq);
+  a.po = s.runs > 1 ? f.ws + s.part : nullptr;
+  a.pl = s.runs > 1 ? a.po + (size_t)s.runs * c.B * c.H * c.Lq * D : nullptr;
+  hipError_t e = launch_mod_ranges(c, f.ws, &a.r, stream);
+  if (e != hipSuccess) return e;
+  const bool cap = c.s.cap > 0.f, bias = c.s.slopes != nullptr;
+  e = cap ? (bias ? launch_kernel(attn_mod_fwd_kernel<true, true>, (unsigned)a.nwg, (unsigned)NT, stream, a)
+                  : launch_kernel(attn_mod_fwd_kernel<true, false>, (unsigned)a.nwg, (unsigned)NT, stream, a))
+          : (bias ? launch_kernel(attn_mod_fwd_kernel<false, true>, (unsigned)a.nwg, (unsigned)NT, stream, a)
+                  : launch_kernel(attn_mod_fwd_kernel<false, false>, (unsigned)a.nwg, (unsigned)NT, stream, a));
+  if (e != hipSuccess || s.runs == 1) return e;
+  return launch_mod_join(f, s, stream);
+}
+
+}  // namespace vidax

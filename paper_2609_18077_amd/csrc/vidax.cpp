@@ -8,6 +8,7 @@
 #include "../../include/vidax.h"
 #include "launch.hpp"
 #include "launch_block.hpp"
+#include "launch_mod.hpp"
 
 static_assert(VIDAX_NOALLOC_MAX_ROWS == vidax::kNoAllocRows, "allocation-free scratch size");
 
@@ -222,6 +223,44 @@ bool any_overlap(const Buf (&outs)[NO], const Buf (&ins)[NI], int io_out = -1, i
   return false;
 }
 
+// The checks that attention with score modifiers shares between forward and
+// backward; bufs: the descriptor's arrays.
+vidax_status mod_common(int32_t B, int32_t H, int32_t Hkv, int32_t Lq, int32_t Lk, int32_t d, float scale,
+                        const vidax_score_desc* s, vidax::ModCall* c, Buf (&bufs)[6]) {
+  if (B < 0 || H < 0 || Hkv < 0 || Lq < 0 || Lk < 0 || d < 0) return VIDAX_ERR_INVALID_ARG;
+  if ((Hkv == 0) != (H == 0) || (Hkv > 0 && H % Hkv != 0)) return VIDAX_ERR_INVALID_ARG;
+  if (numel4(B, Lq, H, d) < 0 || numel4(B, Lk, Hkv, d) < 0) return VIDAX_ERR_INVALID_ARG;
+  if (!isfinite(scale)) return VIDAX_ERR_INVALID_ARG;
+  static const vidax_score_desc plain{};
+  if (!s) s = &plain;
+  if (s->causal != 0 && s->causal != 1) return VIDAX_ERR_INVALID_ARG;
+  // (scale / cap has to be a number, too)
+  if (!(s->cap >= 0.0f) || !isfinite(s->cap) || (s->cap > 0.0f && !isfinite(scale / s->cap))) return VIDAX_ERR_INVALID_ARG;
+  const uint64_t nq = (uint64_t)B * Lq, nk = (uint64_t)B * Lk;
+  if ((nq > 0 && nk > 0 && (s->q_doc != nullptr) != (s->k_doc != nullptr)) || (s->prefix_len && !s->causal))
+    return VIDAX_ERR_INVALID_ARG;
+  const Buf all[6] = {{s->slopes, (uint64_t)H * 4}, {s->q_doc, nq * 4}, {s->k_doc, nk * 4},
+                      {s->kv_valid_len, (uint64_t)B * 4}, {s->prefix_len, (uint64_t)B * 4}, {s->q_start, (uint64_t)B * 4}};
+  for (int i = 0; i < 6; ++i) {
+    if (!aligned(all[i].p, 4)) return VIDAX_ERR_INVALID_ARG;
+    bufs[i] = all[i];
+  }
+  if (d != vidax::kHeadDim) return VIDAX_ERR_UNSUPPORTED;
+  // buffer offsets are 32-bit: within a batch of q, within 64 tokens of k, and within a row of ids
+  if ((int64_t)Lq * H * d * 2 > INT32_MAX - 4096 || (int64_t)64 * Hkv * d * 2 > INT32_MAX - 4096 ||
+      (int64_t)64 * H * d * 2 > INT32_MAX - 4096 || Lk > (1 << 28) || Lq > (1 << 28))
+    return VIDAX_ERR_UNSUPPORTED;
+  // launch sizes: the forward's tiles in up to 64 runs, the joining launch, the ranges
+  const int64_t tiles = ((int64_t)Lq + 127) / 128 + ((int64_t)Lk + 127) / 128;
+  if ((__int128)tiles * B * H * 64 > INT32_MAX || (__int128)B * H * Lq > INT32_MAX) return VIDAX_ERR_UNSUPPORTED;
+  const bool docs = s->q_doc && s->k_doc;
+  *c = vidax::ModCall{B, H, Hkv, Lq, Lk, scale,
+                      vidax::ModScore{s->causal, s->cap > 1e30f ? 0.0f : s->cap,  // (tanh is then the identity in fp32)
+                                      s->slopes, docs ? s->q_doc : nullptr, docs ? s->k_doc : nullptr, s->kv_valid_len,
+                                      s->prefix_len, s->q_start}};
+  return VIDAX_OK;
+}
+
 // Bytes from a modulation's first element to behind its last, or -1 if its
 // strides are not allowed.
 int64_t mod_bytes(const vidax_block_mod& m, int64_t B, int64_t L, int64_t C) {
@@ -406,6 +445,44 @@ vidax_status vidax_qkv_proj(const void* x, const void* w, const float* bias, con
   const hipError_t e = vidax::launch_qkv_proj((const uint16_t*)x, (const uint16_t*)w, bias, gain_q, gain_k, eps,
                                               (uint16_t*)q, (uint16_t*)k, (uint16_t*)v, B, L, H, C, rp, stream);
   return e == hipSuccess ? VIDAX_OK : VIDAX_ERR_LAUNCH;
+}
+
+vidax_status vidax_attn_mod_fwd(const void* q, const void* k, const void* v, void* o, float* lse, int32_t B, int32_t H,
+                                int32_t Hkv, int32_t Lq, int32_t Lk, int32_t d, float scale,
+                                const vidax_score_desc* score, float* workspace, size_t workspace_floats,
+                                hipStream_t stream) {
+  vidax::ModFwd a;
+  Buf s[6];
+  const vidax_status st = mod_common(B, H, Hkv, Lq, Lk, d, scale, score, &a.c, s);
+  if (st == VIDAX_ERR_INVALID_ARG) return st;
+  const uint64_t nq = (uint64_t)B * Lq * H * d, nk = (uint64_t)B * Lk * Hkv * d;
+  if ((nq > 0 && (!q || !o)) || (nq > 0 && nk > 0 && (!k || !v))) return VIDAX_ERR_INVALID_ARG;
+  for (const void* p : {q, k, v, (const void*)o, (const void*)workspace})
+    if (!aligned(p, 16)) return VIDAX_ERR_INVALID_ARG;
+  if (!aligned(lse, 4) || workspace_floats > ((uint64_t)1 << 60)) return VIDAX_ERR_INVALID_ARG;
+  if (!workspace) workspace_floats = 0;
+  const Buf outs[3] = {{o, nq * 2}, {lse, (uint64_t)B * H * Lq * 4}, {workspace, (uint64_t)workspace_floats * 4}};
+  const Buf ins[9] = {{q, nq * 2}, {k, nk * 2}, {v, nk * 2}, s[0], s[1], s[2], s[3], s[4], s[5]};
+  if (any_overlap(outs, ins)) return VIDAX_ERR_INVALID_ARG;
+  if (st != VIDAX_OK || nq == 0) return st;
+  if (workspace_floats < vidax::mod_doc_floats(B, Lq, Lk, a.c.s.k_doc != nullptr)) return VIDAX_ERR_INVALID_ARG;
+  if (!vidax::launch_attn_mod_fwd) return VIDAX_ERR_LAUNCH;
+  a.q = (const uint16_t*)q;
+  a.k = (const uint16_t*)k;
+  a.v = (const uint16_t*)v;
+  a.o = (uint16_t*)o;
+  a.lse = lse;
+  a.ws = workspace;
+  a.ws_floats = workspace_floats;
+  return vidax::launch_attn_mod_fwd(a, stream) == hipSuccess ? VIDAX_OK : VIDAX_ERR_LAUNCH;
+}
+
+size_t vidax_attn_mod_fwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, int32_t Lq, int32_t Lk, int32_t d,
+                                           int32_t docs) {
+  vidax::ModCall c;
+  Buf s[6];
+  if (mod_common(B, H, Hkv, Lq, Lk, d, 1.0f, nullptr, &c, s) != VIDAX_OK || B == 0 || H == 0 || Lq == 0) return 0;
+  return vidax::mod_fwd_split(B, H, Hkv, Lq, Lk, docs != 0 && Lk > 0, vidax::device_cu_count(), SIZE_MAX).floats;
 }
 
 vidax_status vidax_block_norm_fwd(const void* x, const void* y, void* xo, void* h, int32_t B, int32_t L, int32_t C,

@@ -69,13 +69,17 @@ struct Batch {
   int start;   // position of query 0
   int prefix;  // causal: keys j < prefix are seen by all
 };
-__device__ __forceinline__ Batch batch_of(const ModCall& c, int b) {
+__device__ __forceinline__ Batch batch_of_lane(const ModCall& c, int b) {  // (b may differ from lane to lane)
   Batch r;
   r.lv = c.Lk;
   if (c.s.kv_valid_len) r.lv = min(max(c.s.kv_valid_len[b], 0), c.Lk);
   r.start = c.Lk - c.Lq;
   if (c.s.q_start) r.start = min(max(c.s.q_start[b], -kStartLimit), kStartLimit);
   r.prefix = c.s.prefix_len ? max(c.s.prefix_len[b], 0) : 0;
+  return r;
+}
+__device__ __forceinline__ Batch batch_of(const ModCall& c, int b) {
+  Batch r = batch_of_lane(c, b);
   r.lv = __builtin_amdgcn_readfirstlane(r.lv);
   r.start = __builtin_amdgcn_readfirstlane(r.start);
   r.prefix = __builtin_amdgcn_readfirstlane(r.prefix);
@@ -104,6 +108,31 @@ __device__ __forceinline__ bool meet(const Docs& a, const Docs& b) { return a.lo
 // every token of both in one and the same document
 __device__ __forceinline__ bool same(const Docs& a, const Docs& b) {
   return !a.neg && !b.neg && a.lo == a.hi && b.lo == b.hi && a.lo == b.lo;
+}
+
+// ---- tiles as rows: 256-byte rows whose 16-byte chunks are permuted, chunk c of
+// row r at position c ^ swz(r), free of bank conflicts for row reads and for the
+// transposing reads (the layout of the dense backward, attn_bwd.hip).  A copy
+// instruction fills rows 4 j .. 4 j + 3.
+constexpr int kRow = kHeadDim;  // elements of a row
+__device__ __forceinline__ int swz(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
+struct RowOffsets {
+  int row, tr;  // elements: row operand of row l32, d 8 hi; transposed operand
+};
+__device__ __forceinline__ RowOffsets row_offsets(int lane) {
+  const int l32 = lane & 31, hi = lane >> 5, g = lane >> 4, w = lane & 15, r = 4 * hi + (w >> 2);
+  return RowOffsets{l32 * kRow + 8 * (hi ^ swz(l32)),
+                    r * kRow + 8 * ((2 * (g & 1) + ((w >> 1) & 1)) ^ swz(r)) + 4 * (w & 1)};
+}
+// rows l32 of a 32-row block, d = 16 st + 8 hi ..
+__device__ __forceinline__ bf16x8 read_row(const uint16_t* block, int row, int st) {
+  return *reinterpret_cast<const bf16x8*>(block + (row ^ (16 * st)));
+}
+// 16 rows transposed, d block mb, in the accumulators' row order
+__device__ __forceinline__ bf16x8 read_tr(const uint16_t* rows16, int tr, int mb) {
+  const tile::i16x4 lo = tile::lds_read_tr16(rows16 + (tr ^ (32 * mb)));
+  const tile::i16x4 up = tile::lds_read_tr16(rows16 + (tr ^ (32 * mb) ^ 16) + 8 * kRow);
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 }  // namespace mod

@@ -446,7 +446,7 @@ __global__ __launch_bounds__(256) void mod_join_kernel(JoinArgs a) {
     for (int r = 0; r < a.runs; ++r) {
       const float w = __builtin_amdgcn_exp2f(a.pl[r * nrow + row] - m);
       const float2 v = *reinterpret_cast<const float2*>(a.po + (r * nrow + row) * D + 2 * lane);
-      l += w;
+      l += w;  // (a run that saw nothing wrote zeros: weight 0)
       x = fmaf(w, v.x, x);
       y = fmaf(w, v.y, y);
     }
@@ -479,6 +479,7 @@ hipError_t launch_mod_ranges(const ModCall& c, float* ws, ModRanges* out, hipStr
   return launch_kernel(mod_ranges_kernel, (waves + 3) / 4, 256u, stream, a);
 }
 
+namespace {
 hipError_t launch_mod_join(const ModFwd& f, const ModSplit& s, hipStream_t stream) {
   JoinArgs a;
   const size_t nrow = (size_t)f.c.B * f.c.H * f.c.Lq;
@@ -492,10 +493,12 @@ hipError_t launch_mod_join(const ModFwd& f, const ModSplit& s, hipStream_t strea
   a.runs = s.runs;
   return launch_kernel(mod_join_kernel, (unsigned)((nrow + 3) / 4), 256u, stream, a);
 }
+}  // namespace
 
 hipError_t launch_attn_mod_fwd(const ModFwd& f, hipStream_t stream) {
   const ModCall& c = f.c;
-  const ModSplit s = mod_fwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr, device_cu_count(), f.ws_floats);
+  const ModSplit s = mod_fwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr,
+                                   c.s.kv_valid_len || c.s.q_start, device_cu_count(), f.ws_floats);
   FwdArgs a;
   a.c = c;
   a.sc = make_scores(c);
@@ -513,6 +516,7 @@ hipError_t launch_attn_mod_fwd(const ModFwd& f, hipStream_t stream) {
   a.pl = s.runs > 1 ? a.po + (size_t)s.runs * c.B * c.H * c.Lq * D : nullptr;
   hipError_t e = launch_mod_ranges(c, f.ws, &a.r, stream);
   if (e != hipSuccess) return e;
+  if (s.few) return launch_mod_few(f, s, a.r, stream);
   const bool cap = c.s.cap > 0.f, bias = c.s.slopes != nullptr;
   e = cap ? (bias ? launch_kernel(attn_mod_fwd_kernel<true, true>, (unsigned)a.nwg, (unsigned)NT, stream, a)
                   : launch_kernel(attn_mod_fwd_kernel<true, false>, (unsigned)a.nwg, (unsigned)NT, stream, a))

@@ -55,49 +55,66 @@ inline size_t mod_doc_floats(int B, int Lq, int Lk, bool docs) {
 // ---- forward ----
 //
 // Few rows (a group's query heads times the queries, at most kFewRows): the form
-// for single tokens, whose workgroups stream a run of keys and hold all rows.
-// Otherwise tiles of 256 query rows.  Either may cut the keys into runs, one
-// workgroup each, and join them in a second launch.
+// for single tokens (attn_mod_few.hip).  Otherwise tiles of 256 query rows, whose
+// keys may be cut into runs, one workgroup each, that a second launch joins.
 constexpr int kModRows = 256;
 constexpr int kModKeys = 64;
 constexpr int kFewRows = 32;
 
 struct ModSplit {
   bool few;
-  int runs;
+  int runs;       // of the 256-row form
+  int units;      // of the form for few rows; 0: a workgroup takes a whole batch
   size_t part;    // first value of the partial results in the workspace
   size_t floats;  // values of the workspace
 };
 
-inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, int cus, size_t max_floats) {
+inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, bool lengths, int cus, size_t max_floats) {
   ModSplit r;
   r.runs = 1;
-  r.part = (mod_doc_floats(B, Lq, Lk, docs) + 63) / 64 * 64;
-  const int rep = Hkv > 0 ? H / Hkv : 1;
-  r.few = false;
-  (void)rep;
-  const int64_t tiles = ((int64_t)Lk + kModKeys - 1) / kModKeys;
-  const int64_t wgs = r.few ? (int64_t)B * Hkv : (int64_t)((Lq + kModRows - 1) / kModRows) * B * H;
+  r.units = 0;
+  r.floats = mod_doc_floats(B, Lq, Lk, docs);
+  r.part = (r.floats + 63) / 64 * 64;
+  r.few = Hkv > 0 && (int64_t)(H / Hkv) * Lq <= kFewRows;
   const int64_t rows = (int64_t)B * H * Lq;
-  if (wgs > 0 && tiles > 0) {
-    // least time, in tiles of a workgroup: rounds x (tiles a run + start and
-    // end) + the joining launch and its bytes
-    const int slots = cus;
-    const double start = 3.0;
-    double best = 1e30;
-    for (int s = 1; s <= 64 && s <= tiles; ++s) {
-      if (s > 1 && r.part + (size_t)s * rows * 129 > max_floats) break;
-      const int64_t rounds = (wgs * s + slots - 1) / slots;
-      const int64_t per = (tiles + s - 1) / s;
-      const double cost = rounds * (per + start) + (s > 1 ? 3.0 + (double)s * rows * 1056 / 8e6 : 0.0);
-      if (cost < best) {
-        best = cost;
-        r.runs = s;
-      }
+  if (rows == 0 || Lk == 0) return r;
+  if (r.few) {
+    // one workgroup a compute unit in either form.  A unit takes at least a tile
+    // a wave; the joining launch and its partial results cost 5 us.  A whole
+    // batch a workgroup: 1.5 us for its four waves' next 32-key tiles (128 KB in
+    // flight), 3.4 when every unit is busy (64 KB at its share of 5 TB/s).  Where
+    // the batches have lengths of their own, a unit's part is taken as two thirds:
+    // units share what is there, whole batches wait for the longest.
+    const int64_t tiles = ((int64_t)Lk + 31) / 32, wgs = (int64_t)B * Hkv;
+    int64_t u = cus / Hkv < B * tiles / 4 ? cus / Hkv : B * tiles / 4;
+    auto us = [&](int64_t n, int64_t per) {  // n workgroups with `per` tiles each
+      const int64_t rounds = (n + cus - 1) / cus, busy = n < cus ? n : cus;
+      const double step = busy * 65536 / 5e6 > 1.5 ? busy * 65536 / 5e6 : 1.5;
+      return rounds * (3.0 + (per + 3) / 4 * step);
+    };
+    const size_t need = r.part + (size_t)(u + B) * H * Lq * 129;
+    if (u > 0 && need <= max_floats && us(u * Hkv, (B * tiles * (lengths && B > 1 ? 2 : 3) / 3 + u - 1) / u) + 5.0 < us(wgs, tiles)) {
+      r.units = (int)u;
+      r.floats = need;
+    }
+    return r;
+  }
+  // 256-row workgroups, one a compute unit: 1.4 us a tile of 64 keys, 4 to start
+  // and end; the joining launch 4 us and its bytes.
+  const int64_t tiles = ((int64_t)Lk + kModKeys - 1) / kModKeys;
+  const int64_t wgs = (int64_t)((Lq + kModRows - 1) / kModRows) * B * H;
+  double best = 1e30;
+  for (int s = 1; s <= 64 && s <= tiles; ++s) {
+    const size_t need = r.part + (size_t)s * rows * 129;  // a run's rows: 128 outputs and a log-sum-exp each
+    if (s > 1 && need > max_floats) break;
+    const int64_t rounds = (wgs * s + cus - 1) / cus, per = (tiles + s - 1) / s;
+    const double cost = rounds * (per * 1.4 + 4.0) + (s > 1 ? 4.0 + (double)s * rows * 1056 / 5e6 : 0.0);
+    if (cost < best) {
+      best = cost;
+      r.runs = s;
+      if (s > 1) r.floats = need;
     }
   }
-  // a run's rows: 128 outputs and a log-sum-exp each
-  r.floats = r.runs > 1 ? r.part + (size_t)r.runs * rows * 129 : mod_doc_floats(B, Lq, Lk, docs);
   return r;
 }
 
@@ -109,7 +126,6 @@ struct ModRanges {
   const int2 *k, *q;  // [B][mod_ranges(Lk)], [B][mod_ranges(Lq)], or null
 };
 hipError_t launch_mod_ranges(const ModCall& c, float* ws, ModRanges* out, hipStream_t stream);
-hipError_t launch_mod_few(const ModFwd& a, const ModSplit& s, hipStream_t stream);
-hipError_t launch_mod_join(const ModFwd& a, const ModSplit& s, hipStream_t stream);
+hipError_t launch_mod_few(const ModFwd& a, const ModSplit& s, const ModRanges& r, hipStream_t stream);
 
 }  // namespace vidax

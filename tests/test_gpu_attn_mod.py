@@ -346,3 +346,19 @@ def test_offsets_past_32_bits(Lq):
     # two runs of the same rounding in other groupings
     assert (o.float() - ro.float()).abs().max() <= 4 * HALF * ro.float().abs().max()
     assert (lse - rl).abs().max() <= 2.0 ** -16
+
+
+@pytest.mark.parametrize("B,H,Hkv,Lq,Lk", [(70, 2, 1, 1, 260), (130, 1, 1, 2, 129), (3, 4, 2, 3, 2100), (5, 32, 1, 1, 1000),
+                                           (2, 12, 12, 1, 3000), (9, 8, 2, 7, 640), (1, 8, 4, 16, 4097)])
+@pytest.mark.parametrize("fill", ["ragged", "mostly_empty", "full"])
+def test_single_tokens_against_caches_of_any_fill(B, H, Hkv, Lq, Lk, fill):
+    """Batches cut into units that end one cache and begin the next; empty caches among them."""
+    q, k, v = make(B, H, Hkv, Lq, Lk, B + Lk)
+    rng = np.random.default_rng([B, Lk])
+    n = rng.integers(0, Lk + 1, size=B)
+    if fill == "mostly_empty":
+        n[rng.random(B) < 0.8] = 0
+        n[-1] = Lk // 2
+    if fill == "full":
+        n[:] = Lk
+    check(q, k, v, causal=True, cap=30.0, kv_valid_len=n, q_start=n - Lq, what=f"{B}x{H}/{Hkv} {Lq}x{Lk} {fill}")

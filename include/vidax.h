@@ -350,6 +350,40 @@ size_t vidax_attn_mod_fwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, in
                                            int32_t docs);
 
 /*
+ * Gradient of vidax_attn_mod_fwd.  With P the softmax weights and t_ij =
+ * tanh(scale <q_i, k_j> / cap):
+ *
+ *   dv = P^T dout,  ds = P * (dout v^T - D) [* (1 - t^2)],  D_i = <dout_i, o_i>,
+ *   dq = scale ds k,  dk = scale ds^T q,
+ *
+ * dk and dv summed over the query heads that share a K/V head.  Queries that see
+ * no key get dq = 0 and count for nothing (whatever q and dout hold there), keys
+ * that nothing sees get dk = dv = 0; slopes get no gradient.
+ *   q, o, dout, dq: bf16 [B, Lq, H, d];  k, v, dk, dv: bf16 [B, Lk, Hkv, d]
+ *   lse      : fp32 [B, H, Lq], as the forward returned it with the same arguments
+ *              (o is its output).
+ *   workspace: fp32 device memory, required.  With
+ *              vidax_attn_mod_bwd_workspace_floats(...) values the key side may cut
+ *              the query stream into runs that work side by side, their fp32 sums
+ *              added in a further launch (at most 384 MiB); with fewer it takes the
+ *              runs that fit; VIDAX_ERR_INVALID_ARG below what one run needs,
+ *              B H Lq + 2 ceil(Lq / 64) B + 192 values and, with documents, twice
+ *              2 B (ceil(Lk / 64) + ceil(Lq / 64)) more.
+ * Same call, same bits: no atomics.  Products on bf16 inputs (P and ds rounded to
+ * bf16) with fp32 accumulation.  Pointers, sizes and overlap as for the forward
+ * (lse 4-byte aligned).
+ */
+vidax_status vidax_attn_mod_bwd(const void* q, const void* k, const void* v, const void* o, const void* dout,
+                                const float* lse, void* dq, void* dk, void* dv, int32_t B, int32_t H, int32_t Hkv,
+                                int32_t Lq, int32_t Lk, int32_t d, float scale, const vidax_score_desc* score,
+                                float* workspace, size_t workspace_floats, hipStream_t stream);
+
+/* fp32 values of that workspace on the current device (docs: 1 with documents);
+ * 0 for invalid arguments. */
+size_t vidax_attn_mod_bwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, int32_t Lq, int32_t Lk, int32_t d,
+                                           int32_t docs);
+
+/*
  * The step between two sublayers of a block (Section 3, "Supported Models":
  * adaptive layer norm per sample or per token; the paper gives no formula):
  * the sublayer's output y joins the residual stream x, and the sum is

@@ -31,6 +31,8 @@ EXPORTED_SYMBOLS = (
     "vidax_qk_norm_rope",
     "vidax_attn_mod_fwd",
     "vidax_attn_mod_fwd_workspace_floats",
+    "vidax_attn_mod_bwd",
+    "vidax_attn_mod_bwd_workspace_floats",
     "vidax_block_norm_fwd",
     "vidax_block_norm_bwd",
     "vidax_block_norm_bwd_workspace_floats",
@@ -169,6 +171,10 @@ def lib() -> ctypes.CDLL:
         L.vidax_attn_mod_fwd.restype = i32
         L.vidax_attn_mod_fwd_workspace_floats.argtypes = [i32] * 7
         L.vidax_attn_mod_fwd_workspace_floats.restype = ctypes.c_size_t
+        L.vidax_attn_mod_bwd.argtypes = ([vp] * 9 + [i32] * 6 + [f32, ctypes.POINTER(ScoreDesc), vp, ctypes.c_size_t, vp])
+        L.vidax_attn_mod_bwd.restype = i32
+        L.vidax_attn_mod_bwd_workspace_floats.argtypes = [i32] * 7
+        L.vidax_attn_mod_bwd_workspace_floats.restype = ctypes.c_size_t
         L.vidax_block_norm_fwd.argtypes = [vp] * 4 + [i32] * 3 + [ctypes.POINTER(BlockNormDesc), vp]
         L.vidax_block_norm_fwd.restype = i32
         L.vidax_block_norm_bwd.argtypes = ([vp] * 6 + [ctypes.POINTER(BlockNormGrads), vp, ctypes.c_size_t]
@@ -491,14 +497,43 @@ def attn_mod_fwd(q, k, v, score: Score | None = None, scale=None, return_lse=Fal
     if out is not None:
         _check_dense("out", o, q.dtype, q.shape, q.device)
     lse = torch.empty((B, H, Lq), dtype=torch.float32, device=q.device) if return_lse else None
+    need = 0
     if workspace is None:
         need = _on(q.device, lib().vidax_attn_mod_fwd_workspace_floats, B, H, Hkv, Lq, Lk, d, int(desc.k_doc is not None))
-        ws = _workspace(None, need, q.device)
-    else:
-        ws = _workspace(workspace, 0, q.device)
+    ws = _workspace(workspace, need, q.device)
     _call("vidax_attn_mod_fwd", q.device, stream, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), B, H, Hkv, Lq, Lk, d,
           _SCALE_128 if scale is None else float(scale), ctypes.byref(desc), _ptr(ws), 0 if ws is None else ws.numel())
     return (o, lse) if return_lse else o
+
+
+def attn_mod_bwd(q, k, v, o, dout, lse, score: Score | None = None, scale=None, out=None, workspace=None, stream=None):
+    """(dq, dk, dv) of attn_mod_fwd from its o and lse; dk and dv are summed over
+    the query heads of a K/V head.  `out` = tensors to write into; `workspace`: a
+    contiguous float32 device tensor (by default one of
+    vidax_attn_mod_bwd_workspace_floats values is allocated)."""
+    import torch
+
+    _check_mod_qkv(q, k, v)
+    B, Lq, H, d = q.shape
+    Lk, Hkv = k.shape[1], k.shape[2]
+    for n, t in (("o", o), ("dout", dout)):
+        _check_dense(n, t, q.dtype, q.shape, q.device)
+    _check_dense("lse", lse, torch.float32, (B, H, Lq), q.device)
+    desc = _score_desc(score, q, Lk)
+    if out is None:
+        dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    else:
+        dq, dk, dv = out
+        for n, t, ref in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
+            _check_dense(n, t, ref.dtype, ref.shape, q.device)
+    need = 0
+    if workspace is None:
+        need = _on(q.device, lib().vidax_attn_mod_bwd_workspace_floats, B, H, Hkv, Lq, Lk, d, int(desc.k_doc is not None))
+    ws = _workspace(workspace, need, q.device)
+    _call("vidax_attn_mod_bwd", q.device, stream, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(dout), _ptr(lse), _ptr(dq),
+          _ptr(dk), _ptr(dv), B, H, Hkv, Lq, Lk, d, _SCALE_128 if scale is None else float(scale), ctypes.byref(desc),
+          _ptr(ws), 0 if ws is None else ws.numel())
+    return dq, dk, dv
 
 
 # -------------------------------------------------------- block norm ----

@@ -1,0 +1,802 @@
+// Attention with score modifiers, backward, for gfx950: with x = scale q.k, t =
+// tanh(x / cap) and P = exp(s - lse) on the keys that a query sees (else 0),
+//
+//   D_i = <dO_i, O_i>,  dS = P (dO V^T - D) (1 - t^2)      (1 - t^2 with a cap)
+//   dQ = scale dS K                 dq kernel: 256 queries of a head a workgroup
+//   dV = P^T dO, dK = scale dS^T Q  dkdv kernel: 256 keys of a K/V head a
+//                                   workgroup, the queries of all its query heads
+//                                   streamed past (their sum needs no atomics)
+//
+// The dataflow is the dense backward's (attn_bwd.hip): 32 own rows a wave, the
+// streamed tiles of 64 rows in LDS as permuted 256-byte rows, read by rows and
+// transposed, double-buffered, one barrier a tile.  The tiles to visit and to mask
+// are found as in the forward (attn_mod_fwd.hip), for the key side with the roles
+// of queries and keys exchanged.  Rows that see nothing (lse = -inf) get P = 0 and
+// count as zeros wherever they are read, as do keys that nothing sees.
+#include "attn_mod.hpp"
+#include "launch.hpp"
+
+namespace vidax {
+namespace {
+
+using namespace tile;
+using namespace mod;
+
+constexpr int D = kHeadDim;
+constexpr int BN = 64;         // rows of a streamed tile
+constexpr int NW = 8;
+constexpr int NT = NW * 64;
+constexpr int TILE = BN * D;   // elements
+constexpr int BM = 256;        // own rows of a workgroup
+constexpr int kOff = 0x7ffffff0;  // past any buffer's records
+
+struct BwdArgs {
+  ModCall c;
+  Scores sc;
+  const uint16_t *q, *k, *v, *o, *dout;
+  const float* lse;
+  uint16_t *dq, *dk, *dv;
+  float* delta;       // [B, H, Lq]
+  int32_t* empty;     // [B][qr]: whether a row of these 32 sees nothing
+  ModRanges r;
+  int kr, qr;         // ranges a batch
+  int ntile, nwg;     // tiles of own rows a head, workgroups of the launched kernel
+  int runs;           // key side: the stream is cut into runs, a workgroup each
+  float* part;        // runs > 1: fp32 dK, dV of every run ([runs][B][Lk][Hkv][D], dV after dK)
+};
+
+// Rows 16 k2 .. + 15 of an accumulator as a bf16 B operand, in the accumulator's row order.
+__device__ __forceinline__ bf16x8 pack8(const f32x16& x, int k2) {
+  uint32_t w[4];
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) w[e >> 1] = pack_bf16x2(x[8 * k2 + e], x[8 * k2 + e + 1]);
+  return __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+}
+// Row of register i of accumulator block blk, of lane half 0.
+constexpr int acc_row(int blk, int i) { return 32 * blk + 8 * (i >> 2) + (i & 3); }
+// x, as a value of iteration t (what is computed from it stays in the loop).
+__device__ __forceinline__ int in_loop(int x, int t) {
+  asm("" : "+v"(x) : "s"(t));
+  return x;
+}
+__device__ __forceinline__ bf16x8 apply_sign(uint4 x, const Scores& s) {
+  return __builtin_bit_cast(bf16x8, make_uint4((x.x ^ s.qxor) & s.qand, (x.y ^ s.qxor) & s.qand, (x.z ^ s.qxor) & s.qand,
+                                               (x.w ^ s.qxor) & s.qand));
+}
+// 64-row tile `t` of rows [0, limit) of a buffer: later rows read as zero.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const uint16_t* base, int t, int limit, int tok) {
+  const int nbytes = __builtin_amdgcn_readfirstlane(min(max(limit - t * BN, 0), BN) * tok * 2);
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (size_t)t * BN * tok), (short)0, nbytes, kBufferFlags);
+}
+
+// ------------------------------------------------------------------- dQ ----
+
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ void dq_body(const BwdArgs& a) {
+  __shared__ __attribute__((aligned(1024))) uint16_t K0[TILE], K1[TILE], V0[TILE], V1[TILE];
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const ModCall& c = a.c;
+  const int lid = balanced_tile(blockIdx.x, a.nwg, c.B);
+  int qt = lid % a.ntile;
+  if (c.s.causal) qt = qt & 1 ? qt >> 1 : a.ntile - 1 - (qt >> 1);  // (as in the forward)
+  const int bh = lid / a.ntile, h = bh % c.H, b = bh / c.H, hk = h / (c.H / c.Hkv);
+  const int qtok = c.H * D, qbytes = qtok * 2, ktok = c.Hkv * D, kbytes = ktok * 2;
+  const Batch bt = batch_of(c, b);
+  const int row0 = qt * BM, wrow = row0 + wave * 32, qrow = wrow + l32;
+  const bool qlive = qrow < c.Lq;
+  const int wlast = min(wrow + 32, c.Lq) - 1, glast = min(row0 + BM, c.Lq) - 1;
+  const size_t lrow = ((size_t)b * c.H + h) * c.Lq + (qlive ? qrow : 0);
+  float lse = qlive ? a.lse[lrow] : -INFINITY;
+  const bool none = lse == -INFINITY;  // the row sees nothing
+  const float lse2 = none ? INFINITY : lse * kLog2e;
+
+  int lim = qlive ? key_limit(bt, c.s.causal, bt.start + qrow) : 0;
+  int qd = 0;
+  Docs wdoc{0, 0, false}, gdoc{0, 0, false};
+  const bool docs = a.r.k != nullptr;
+  if (docs) {
+    if (qlive) qd = c.s.q_doc[(size_t)b * c.Lq + qrow];
+    if (qd < 0) lim = 0;
+    const int2* const qr = a.r.q + (size_t)b * a.qr;
+    const int first = row0 >> 5;
+    gdoc = docs_of(qr[first]);
+    for (int i = 1; i < BM / 32; ++i)
+      if (first + i < a.qr) gdoc = mod::join(gdoc, docs_of(qr[first + i]));
+    gdoc = uniform(gdoc);
+    wdoc = wrow < c.Lq ? uniform(docs_of(qr[wrow >> 5])) : Docs{0x7fffffff, 0, false};
+  }
+  const int wmax = wlast >= wrow ? key_limit(bt, c.s.causal, bt.start + wlast) : 0;
+  const int wmin = wlast >= wrow ? key_limit(bt, c.s.causal, bt.start + wrow) : 0;
+  const int gmax = key_limit(bt, c.s.causal, bt.start + glast);
+  const int end_tile = (gmax + BN - 1) / BN;
+
+  int grp = 0;
+  uint64_t visit = 0, mine = 0, whole = 0, neg = 0;
+  auto look = [&](int g) __attribute__((always_inline)) {
+    const int t = 64 * g + lane;
+    const bool in = t < end_tile;
+    bool v = in, m = in && t * BN < wmax, w = in && t * BN + BN <= wmin, n = false;
+    if (docs && in) {
+      const int4 r = *reinterpret_cast<const int4*>(a.r.k + (size_t)b * a.kr + 2 * t);
+      const Docs d = mod::join(docs_of(make_int2(r.x, r.y)), docs_of(make_int2(r.z, r.w)));
+      v = meet(d, gdoc);
+      m = m && meet(d, wdoc);
+      w = w && same(d, wdoc);
+      n = d.neg;
+    }
+    visit = __builtin_amdgcn_ballot_w64(v);
+    mine = __builtin_amdgcn_ballot_w64(m);
+    whole = __builtin_amdgcn_ballot_w64(w);
+    neg = __builtin_amdgcn_ballot_w64(n);
+  };
+  struct Tile {
+    int t;  // -1: none left
+    bool mine, whole, neg;
+  };
+  auto next = [&]() __attribute__((always_inline)) {
+    while (visit == 0) {
+      if (64 * (grp + 1) >= end_tile) return Tile{-1, false, false, false};
+      look(++grp);
+    }
+    const int i = __builtin_ctzll(visit);
+    visit &= visit - 1;
+    return Tile{64 * grp + i, (bool)(mine >> i & 1), (bool)(whole >> i & 1), (bool)(neg >> i & 1)};
+  };
+
+  // own rows in and out whole, through the tile buffers
+  uint16_t* const area = (wave < 2 ? K0 : wave < 4 ? K1 : wave < 6 ? V0 : V1) + (wave & 1) * 32 * D;
+  const size_t off0 = ((size_t)b * c.Lq + wrow) * qtok + (size_t)h * D;
+  auto rows_rsrc = [&](const uint16_t* base) __attribute__((always_inline)) {
+    return __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(base + off0), (short)0, __builtin_amdgcn_readfirstlane(min(max(c.Lq - wrow, 0), 32) * qbytes), kBufferFlags);
+  };
+  auto row_off = [&](int i) __attribute__((always_inline)) {
+    const int r = 4 * i + (lane >> 4);
+    return r * qbytes + ((lane & 15) ^ swz(r)) * 16;
+  };
+  auto rows_in = [&](const uint16_t* base) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t rs = rows_rsrc(base);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(area + 4 * i * D), 16, row_off(i), 0, 0, 0);
+  };
+  const RowOffsets off = row_offsets(lane);
+  auto own_rows = [&](bf16x8 op[8]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < 8; ++s) op[s] = read_row(area, off.row, s);
+  };
+  f32x16 acc[4];
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb) acc[mb] = f32x16{};
+  auto rows_out = [&](float mul) __attribute__((always_inline)) {
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        uint2 pk;
+        pk.x = pack_bf16x2(acc[mb][4 * g + 0] * mul, acc[mb][4 * g + 1] * mul);
+        pk.y = pack_bf16x2(acc[mb][4 * g + 2] * mul, acc[mb][4 * g + 3] * mul);
+        if (none) pk = make_uint2(0u, 0u);
+        *reinterpret_cast<uint2*>(area + l32 * D + ((4 * mb + g) ^ swz(l32)) * 8 + 4 * hi) = pk;
+      }
+    wave_lds_fence();
+    const __amdgpu_buffer_rsrc_t rs = rows_rsrc(a.dq);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(area + (4 * i + (lane >> 4)) * D + (lane & 15) * 8);
+      __builtin_amdgcn_raw_buffer_store_b128(v, rs, row_off(i), 0, 0);
+    }
+  };
+  bf16x8 dop[8], qop[8], oop[8];
+  rows_in(a.dout);
+  {
+    const uint16_t* const p = a.o + ((size_t)b * c.Lq + (qlive ? qrow : 0)) * qtok + (size_t)h * D;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) oop[s] = *reinterpret_cast<const bf16x8*>(p + (2 * s + hi) * 8);
+  }
+  __builtin_amdgcn_s_waitcnt(0);  // this wave's rows have landed
+  own_rows(dop);
+  const bf16x8 zero8 = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0));
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+    if (none) dop[s] = oop[s] = zero8;
+  __builtin_amdgcn_s_waitcnt(0);  // dO is out of the area
+  rows_in(a.q);
+  float dl;
+  {
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const uint4 x = __builtin_bit_cast(uint4, dop[s]), y = __builtin_bit_cast(uint4, oop[s]);
+      const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int p = 0; p < 4; ++p) sum[p & 1] = dot2(xw[p], yw[p], sum[p & 1]);
+    }
+    dl = wave_half_sum(sum[0] + sum[1]);
+    if (qlive && hi == 0) a.delta[lrow] = dl;
+    const uint64_t bad = __builtin_amdgcn_ballot_w64(qlive && none);
+    if (h == 0 && lane == 0 && wrow < c.Lq) a.empty[(size_t)b * a.qr + (wrow >> 5)] = bad != 0;
+  }
+  __builtin_amdgcn_s_waitcnt(0);
+  own_rows(qop);
+#pragma unroll
+  for (int s = 0; s < 8; ++s) qop[s] = none ? zero8 : apply_sign(__builtin_bit_cast(uint4, qop[s]), a.sc);
+  __builtin_amdgcn_s_waitcnt(0);  // the rows are out of the staging areas
+  __syncthreads();
+
+  Tile cur{-1, false, false, false}, nxt = cur;
+  if (end_tile > 0) {
+    look(0);
+    cur = next();
+  }
+  if (cur.t < 0) {  // nothing to see: dQ = 0
+    rows_out(0.f);
+    return;
+  }
+  const uint16_t* const kbh = a.k + (size_t)b * c.Lk * ktok + (size_t)hk * D;
+  const uint16_t* const vbh = a.v + (size_t)b * c.Lk * ktok + (size_t)hk * D;
+  // the wave's copies 2 wave, 2 wave + 1 of a tile (4 rows each)
+  auto copies = [&](const Tile& t, uint16_t* kb, uint16_t* vb) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t rk = tile_rsrc(kbh, t.t, gmax, ktok), rv = tile_rsrc(vbh, t.t, gmax, ktok);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int r = 4 * (2 * wave + u) + (lane >> 4);
+      int g = r * kbytes + ((lane & 15) ^ swz(r)) * 16;
+      if (t.neg) {  // uniform: keys of negative documents arrive as zeros
+        const int key = t.t * BN + r;
+        if (key >= c.Lk || c.s.k_doc[(size_t)b * c.Lk + min(key, c.Lk - 1)] < 0) g = kOff;
+      }
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_ptr)(kb + (2 * wave + u) * 512), 16, g, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_ptr)(vb + (2 * wave + u) * 512), 16, g, 0, 0, 0);
+    }
+  };
+  copies(cur, K0, V0);
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+
+  const float mul = a.sc.mul, ku = a.sc.ku;
+  const float slope = BIAS ? -c.s.slopes[h] * kLog2e : 0.f;
+  // One tile, one slot a product, as in the dense backward: each slot issues the
+  // operand reads of the product three slots on and its share of the vector work.
+  // With a cap both blocks' scores come first (their tanh branches), and the
+  // exponentials run beside dP.  MASK: elements that are not seen get P = 0.
+  auto products = [&](auto msk, const Tile& t, const uint16_t* kt, const uint16_t* vt, uint32_t seen) __attribute__((always_inline)) {
+    constexpr bool MASK = decltype(msk)::value;
+    const int orow = in_loop(off.row, t.t), otr = in_loop(off.tr, t.t);
+    f32x16 sc[2], dp[2];
+    bf16x8 ds[2][2];
+    const float dist = BIAS ? (float)(bt.start + qrow - t.t * BN - 4 * hi) : 0.f;
+    auto exps = [&](int blk, int i0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = i0; i < i0 + 2; ++i) {
+        const float s = sc[blk][i];
+        float x = fmaf(s, mul, -lse2);
+        if (BIAS) x = fmaf(slope, fabsf(dist - (float)acc_row(blk, i)), x);
+        if (MASK) x = (seen >> (16 * blk + i)) & 1 ? x : -INFINITY;
+        float p = __builtin_amdgcn_exp2f(x);
+        if (CAP) p *= fmaf(-s, s, 1.f);
+        sc[blk][i] = p;
+      }
+    };
+    auto mul4 = [&](int blk, int i0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = i0; i < i0 + 4; ++i) dp[blk][i] *= sc[blk][i];
+    };
+    // products in order: S0 dP0 S1 dP1 dQ0 dQ1, with a cap S0 S1 dP0 dP1 dQ0 dQ1
+    bf16x8 op[48];
+    auto read_op = [&](auto N) __attribute__((always_inline)) {
+      constexpr int n = decltype(N)::value;
+      if constexpr (n < 48) {
+        constexpr bool isv = CAP ? (n >> 4) & 1 : (n >> 3) & 1;
+        constexpr int blk = n >= 32 ? (n - 32) >> 3 : CAP ? (n >> 3) & 1 : n >> 4;
+        if constexpr (n >= 32) op[n] = read_tr(kt + (32 * blk + 16 * ((n >> 2) & 1)) * D, otr, n & 3);
+        else op[n] = read_row((isv ? vt : kt) + 32 * blk * D, orow, n & 7);
+      }
+    };
+    auto product = [&](auto N) __attribute__((always_inline)) {
+      constexpr int n = decltype(N)::value, u = n & 7;
+      constexpr bool isv = CAP ? (n >> 4) & 1 : (n >> 3) & 1;
+      constexpr int blk = n >= 32 ? (n - 32) >> 3 : CAP ? (n >> 3) & 1 : n >> 4;
+      if constexpr (n >= 32) acc[u & 3] = mfma32(op[n], ds[blk][u >> 2], acc[u & 3]);
+      else if constexpr (isv) {
+        if constexpr (u == 0)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) dp[blk][i] = -dl;
+        dp[blk] = mfma32(op[n], dop[u], dp[blk]);
+      } else sc[blk] = mfma32(op[n], qop[u], u == 0 ? f32x16{} : sc[blk]);
+    };
+    // vector work of block vb from slot `from` on: eight slots of exponentials, four of products, the packs
+    auto vector = [&](auto N, auto V, auto F) __attribute__((always_inline)) {
+      constexpr int vb = decltype(V)::value, r = decltype(N)::value - decltype(F)::value;
+      if constexpr (r >= 0 && r < 8) exps(vb, 2 * r);
+      if constexpr (r >= 8 && r < 12) mul4(vb, 4 * (r - 8));
+      if constexpr (r == 10) ds[vb][0] = pack8(dp[vb], 0);
+      if constexpr (r == 12) ds[vb][1] = pack8(dp[vb], 1);
+    };
+    using zero = std::integral_constant<int, 0>;
+    using one = std::integral_constant<int, 1>;
+    for_slots<3>(read_op);
+    SLOT();
+    if constexpr (CAP) {
+      for_slots<16>([&](auto N) __attribute__((always_inline)) {
+        product(N);
+        read_op(std::integral_constant<int, decltype(N)::value + 3>());
+        SLOT();
+      });
+      cap16(sc[0], ku);
+      cap16(sc[1], ku);
+      for_slots<32>([&](auto M) __attribute__((always_inline)) {
+        using N = std::integral_constant<int, decltype(M)::value + 16>;
+        product(N());
+        read_op(std::integral_constant<int, N::value + 3>());
+        vector(N(), zero(), std::integral_constant<int, 16>());
+        vector(N(), one(), std::integral_constant<int, 24>());
+        SLOT();
+      });
+    } else {
+      for_slots<48>([&](auto N) __attribute__((always_inline)) {
+        product(N);
+        read_op(std::integral_constant<int, decltype(N)::value + 3>());
+        vector(N, zero(), std::integral_constant<int, 10>());
+        vector(N, one(), std::integral_constant<int, 26>());
+        SLOT();
+      });
+    }
+  };
+  auto step = [&](auto par) __attribute__((always_inline)) {
+    constexpr int P = decltype(par)::value;
+    const uint16_t* const kt = P ? K1 : K0;
+    const uint16_t* const vt = P ? V1 : V0;
+    uint32_t seen = 0xffffffffu;  // bit 16 blk + i: element i of block blk
+    if (cur.mine && !cur.whole) {
+      const int left = lim - cur.t * BN - 4 * hi;
+      seen = 0;
+      u32x4 d[8];
+      if (docs) {
+        const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(c.s.k_doc + (size_t)b * c.Lk), (short)0, c.Lk * 4, kBufferFlags);
+#pragma unroll
+        for (int g = 0; g < 8; ++g)
+          d[g] = __builtin_amdgcn_raw_buffer_load_b128(rd, (cur.t * BN + 8 * g + 4 * hi) * 4, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const bool s = acc_row(i >> 4, i & 15) < left && (!docs || (int)d[i >> 2][i & 3] == qd);
+        seen |= s ? 1u << i : 0u;
+      }
+    }
+    nxt = next();
+    if (nxt.t >= 0) copies(nxt, P ? K0 : K1, P ? V0 : V1);
+    if (cur.mine) {
+      if (cur.whole) products(std::false_type(), cur, kt, vt, seen);
+      else products(std::true_type(), cur, kt, vt, seen);
+    }
+    cur = nxt;
+    __builtin_amdgcn_s_waitcnt(0);  // this wave's copies have landed
+    __syncthreads();
+    return cur.t >= 0;
+  };
+  while (step(std::integral_constant<int, 0>()) && step(std::integral_constant<int, 1>())) {
+  }
+  rows_out(c.scale);
+}
+
+template <bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT) void mod_dq_kernel(BwdArgs a) {
+  dq_body<CAP, BIAS>(a);
+}
+
+// ------------------------------------------------------------- dK and dV ----
+
+template <bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint16_t Q0[TILE], Q1[TILE], O0[TILE], O1[TILE];
+  __shared__ __attribute__((aligned(16))) uint16_t KB[NW * 32 * D];
+  __shared__ __attribute__((aligned(16))) float Lt[2][BN], Dt[2][BN];
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const ModCall& c = a.c;
+  const int lid = balanced_tile(blockIdx.x, a.nwg, c.B);
+  int kt = lid % a.ntile;
+  if (c.s.causal) kt = kt & 1 ? kt >> 1 : a.ntile - 1 - (kt >> 1);
+  const int sbh = lid / a.ntile, run = sbh % a.runs, bh = sbh / a.runs, hk = bh % c.Hkv, b = bh / c.Hkv;
+  const int rep = c.H / c.Hkv;
+  const int qtok = c.H * D, qbytes = qtok * 2, ktok = c.Hkv * D, kbytes = ktok * 2;
+  const Batch bt = batch_of(c, b);
+  const int used = key_limit(bt, c.s.causal, bt.start + c.Lq - 1);  // keys that some query may see
+  const int key0 = kt * BM, wkey = key0 + wave * 32, krow = wkey + l32;
+  int kd = 0;
+  Docs wdoc{0, 0, false}, gdoc{0, 0, false};
+  const bool docs = a.r.k != nullptr;
+  if (docs) {
+    if (krow < c.Lk) kd = c.s.k_doc[(size_t)b * c.Lk + krow];
+    const int2* const kr = a.r.k + (size_t)b * a.kr;
+    const int first = key0 >> 5;
+    gdoc = docs_of(kr[first]);
+    for (int i = 1; i < BM / 32; ++i)
+      if (first + i < a.kr) gdoc = mod::join(gdoc, docs_of(kr[first + i]));
+    gdoc = uniform(gdoc);
+    wdoc = wkey < c.Lk ? uniform(docs_of(kr[wkey >> 5])) : Docs{0x7fffffff, 0, false};
+  }
+  const bool klive = krow < used && kd >= 0;
+  const bool wlive = wkey < used;  // uniform
+  const int wend = min(wkey + 32, used);  // behind the wave's last key
+
+  // query tiles of a head that may see a key of the workgroup: [qa, qb); the
+  // stream: heads of the group in turn, this run's part of rep (qb - qa) tiles
+  const int qb = (c.Lq + BN - 1) / BN;
+  int qa = 0;
+  if (c.s.causal && key0 >= bt.prefix) qa = min(max(key0 - bt.start, 0) / BN, qb);
+  const int64_t items = key0 < used ? (int64_t)rep * (qb - qa) : 0;
+  const int64_t i0 = items * run / a.runs, i1 = items * (run + 1) / a.runs;
+  int g = qb > qa ? (int)(i0 / (qb - qa)) : 0;  // head of the group
+  int ta = qb > qa ? qa + (int)(i0 % (qb - qa)) : 0, tb = 0;  // its tiles
+  int64_t left_items = i1 - i0;
+  // first row that sees the lane's key, by position (-2^31: all, prefix)
+  const int rmin = !c.s.causal || krow < bt.prefix ? INT32_MIN : krow - bt.start;
+  const int wrmax = !c.s.causal || wend - 1 < bt.prefix ? INT32_MIN : wend - 1 - bt.start;  // first row that sees all of the wave's
+  const int wrmin = !c.s.causal || wkey < bt.prefix ? INT32_MIN : wkey - bt.start;          // ... that sees one of them
+
+  int grp = 0;
+  uint64_t visit = 0, mine = 0, whole = 0, none = 0;
+  auto look = [&](int s) __attribute__((always_inline)) {
+    const int t = 64 * s + lane;
+    const bool in = t >= ta && t < tb;
+    bool v = in, m = in && wlive && t * BN + BN - 1 >= wrmin, w = in && t * BN >= wrmax, n = false;
+    if (in) {
+      const int2 e = *reinterpret_cast<const int2*>(a.empty + (size_t)b * a.qr + 2 * t);
+      n = (e.x != 0) || (t * BN + 32 < c.Lq && e.y != 0);
+      if (docs) {
+        const int4 r = *reinterpret_cast<const int4*>(a.r.q + (size_t)b * a.qr + 2 * t);
+        const Docs d = mod::join(docs_of(make_int2(r.x, r.y)), docs_of(make_int2(r.z, r.w)));
+        v = meet(d, gdoc);
+        m = m && meet(d, wdoc);
+        w = w && same(d, wdoc);
+      }
+    }
+    visit = __builtin_amdgcn_ballot_w64(v);
+    mine = __builtin_amdgcn_ballot_w64(m);
+    whole = __builtin_amdgcn_ballot_w64(w);
+    none = __builtin_amdgcn_ballot_w64(n);
+  };
+  // the tiles of head g from ta on, as far as the run goes
+  auto begin_head = [&]() __attribute__((always_inline)) {
+    const int64_t n = qb - ta < left_items ? qb - ta : left_items;
+    tb = ta + (int)n;
+    left_items -= n;
+    grp = ta >> 6;
+    look(grp);
+  };
+  struct Tile {
+    int t, g;  // t < 0: none left
+    bool mine, whole, none;
+  };
+  auto next = [&]() __attribute__((always_inline)) {
+    while (visit == 0) {
+      if (64 * (grp + 1) < tb) {
+        look(++grp);
+      } else {
+        if (left_items <= 0) return Tile{-1, 0, false, false, false};
+        ++g;
+        ta = qa;
+        begin_head();
+      }
+    }
+    const int i = __builtin_ctzll(visit);
+    visit &= visit - 1;
+    return Tile{64 * grp + i, g, (bool)(mine >> i & 1), (bool)(whole >> i & 1), (bool)(none >> i & 1)};
+  };
+
+  f32x16 dk[4], dv[4];
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb) dk[mb] = dv[mb] = f32x16{};
+  auto partials_out = [&]() __attribute__((always_inline)) {
+    if (krow >= c.Lk) return;
+    const size_t rowoff = ((size_t)b * c.Lk + krow) * ktok + (size_t)hk * D, n = (size_t)c.B * c.Lk * ktok;
+    float* const pk = a.part + (size_t)run * n + rowoff;
+    float* const pv = a.part + (size_t)(a.runs + run) * n + rowoff;
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
+        if (klive) {
+          x = make_float4(dk[mb][4 * i], dk[mb][4 * i + 1], dk[mb][4 * i + 2], dk[mb][4 * i + 3]);
+          y = make_float4(dv[mb][4 * i], dv[mb][4 * i + 1], dv[mb][4 * i + 2], dv[mb][4 * i + 3]);
+        }
+        *reinterpret_cast<float4*>(pk + 32 * mb + 8 * i + 4 * hi) = x;
+        *reinterpret_cast<float4*>(pv + 32 * mb + 8 * i + 4 * hi) = y;
+      }
+  };
+  // acc * mul (zero for keys that nothing sees) to the wave's key rows, whole, through an area of its own
+  auto rows_out = [&](uint16_t* dst, const f32x16 acc[4], float m, uint16_t* area) __attribute__((always_inline)) {
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint2 pk = make_uint2(0u, 0u);
+        if (klive) {
+          pk.x = pack_bf16x2(acc[mb][4 * i + 0] * m, acc[mb][4 * i + 1] * m);
+          pk.y = pack_bf16x2(acc[mb][4 * i + 2] * m, acc[mb][4 * i + 3] * m);
+        }
+        *reinterpret_cast<uint2*>(area + l32 * D + ((4 * mb + i) ^ swz(l32)) * 8 + 4 * hi) = pk;
+      }
+    wave_lds_fence();
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(dst + ((size_t)b * c.Lk + wkey) * ktok + (size_t)hk * D), (short)0,
+        __builtin_amdgcn_readfirstlane(min(max(c.Lk - wkey, 0), 32) * kbytes), kBufferFlags);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 4 * i + (lane >> 4);
+      const u32x4 x = *reinterpret_cast<const u32x4*>(area + r * D + (lane & 15) * 8);
+      __builtin_amdgcn_raw_buffer_store_b128(x, rs, r * kbytes + ((lane & 15) ^ swz(r)) * 16, 0, 0);
+    }
+    wave_lds_fence();
+  };
+
+  // own k and v as B operands: lane holds key krow; k goes to LDS
+  uint16_t* const kb = KB + wave * 32 * D + lane * 8;
+  bf16x8 vop[8];
+  {
+    const size_t rowoff = ((size_t)b * c.Lk + (klive ? krow : 0)) * ktok + (size_t)hk * D;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      uint4 x = make_uint4(0, 0, 0, 0), y = x;
+      if (klive) {
+        x = *reinterpret_cast<const uint4*>(a.k + rowoff + (2 * s + hi) * 8);
+        y = *reinterpret_cast<const uint4*>(a.v + rowoff + (2 * s + hi) * 8);
+      }
+      *reinterpret_cast<bf16x8*>(kb + s * 512) = apply_sign(x, a.sc);  // (the sign of scale; dQ and dK take it outside)
+      vop[s] = __builtin_bit_cast(bf16x8, y);
+    }
+  }
+  const size_t qbase = (size_t)b * c.Lq * qtok;
+  float lrow = INFINITY, drow = 0.f;
+  auto copies = [&](const Tile& t, uint16_t* qs, uint16_t* os) __attribute__((always_inline)) {
+    const size_t hoff = qbase + (size_t)(hk * rep + t.g) * D;
+    const size_t lbase = ((size_t)b * c.H + hk * rep + t.g) * c.Lq;
+    const __amdgpu_buffer_rsrc_t rq = tile_rsrc(a.q + hoff, t.t, c.Lq, qtok), ro = tile_rsrc(a.dout + hoff, t.t, c.Lq, qtok);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int r = 4 * (2 * wave + u) + (lane >> 4);
+      int off = r * qbytes + ((lane & 15) ^ swz(r)) * 16;
+      if (t.none) {  // uniform: rows that see nothing arrive as zeros
+        const int row = t.t * BN + r;
+        if (row >= c.Lq || a.lse[lbase + min(row, c.Lq - 1)] == -INFINITY) off = kOff;
+      }
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_ptr)(qs + (2 * wave + u) * 512), 16, off, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ro, (lds_ptr)(os + (2 * wave + u) * 512), 16, off, 0, 0, 0);
+    }
+    if (tid < BN) {
+      const int r = t.t * BN + tid;
+      lrow = r < c.Lq ? a.lse[lbase + r] : INFINITY;
+      drow = r < c.Lq ? a.delta[lbase + r] : 0.f;
+      if (lrow == -INFINITY) lrow = INFINITY;  // P = 0
+    }
+  };
+  auto put_rows = [&](int buf) __attribute__((always_inline)) {
+    if (tid < BN) {
+      Lt[buf][tid] = -lrow * kLog2e;
+      Dt[buf][tid] = -drow;
+    }
+  };
+  const RowOffsets off = row_offsets(lane);
+  const float mul = a.sc.mul, ku = a.sc.ku;
+  // One 32-query block of a tile, one slot a product (as in the dense backward).
+  // Without a cap P is formed beside dP; with one the scores' tanh comes first.
+  auto block = [&](auto msk, auto B_, auto par, const Tile& t, const uint16_t* qt, const uint16_t* ot, uint32_t seen, float slope)
+                   __attribute__((always_inline)) {
+    constexpr bool MASK = decltype(msk)::value;
+    constexpr int blk = decltype(B_)::value, P = decltype(par)::value;
+    const int orow = in_loop(off.row, t.t), otr = in_loop(off.tr, t.t);
+    const uint16_t* const qb_ = qt + 32 * blk * D;
+    const uint16_t* const ob = ot + 32 * blk * D;
+    const float dist = BIAS ? (float)(bt.start + t.t * BN + 32 * blk + 4 * hi - krow) : 0.f;
+    f32x16 s = f32x16{}, dp;
+    bf16x8 qa_[8], ka[8], oa[8], tr_o[8], tr_q[8], db[2];
+    uint32_t pw[8];
+    float4 nl[4];
+    auto exps = [&](int i) __attribute__((always_inline)) {  // P of elements i, i + 1; s becomes P (1 - t^2)
+      const float4 l4 = nl[i >> 2];
+      float p[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float z = s[i + e];
+        float x = fmaf(z, mul, (i & 2) ? (e ? l4.w : l4.z) : (e ? l4.y : l4.x));
+        if (BIAS) x = fmaf(slope, fabsf(dist + (float)acc_row(0, i + e)), x);
+        if (MASK) x = (seen >> (16 * blk + i + e)) & 1 ? x : -INFINITY;
+        p[e] = __builtin_amdgcn_exp2f(x);
+        s[i + e] = CAP ? p[e] * fmaf(-z, z, 1.f) : p[e];
+      }
+      pw[i >> 1] = pack_bf16x2(p[0], p[1]);
+    };
+    auto read_qk = [&](int st) __attribute__((always_inline)) {
+      qa_[st] = read_row(qb_, orow, st);
+      ka[st] = *reinterpret_cast<const bf16x8*>(kb + st * 512);
+    };
+    auto p_op = [&](int k2) __attribute__((always_inline)) {
+      return __builtin_bit_cast(bf16x8, make_uint4(pw[4 * k2], pw[4 * k2 + 1], pw[4 * k2 + 2], pw[4 * k2 + 3]));
+    };
+#pragma unroll
+    for (int st = 0; st < 3; ++st) read_qk(st);
+    SLOT();
+#pragma unroll
+    for (int st = 0; st < 8; ++st) {  // S
+      s = mfma32(qa_[st], ka[st], s);
+      if (st + 3 < 8) read_qk(st + 3);
+      else oa[st - 5] = read_row(ob, orow, st - 5);
+      if (st >= 1 && st < 5) {
+        const float4 d4 = *reinterpret_cast<const float4*>(&Dt[P][32 * blk + 8 * (st - 1) + 4 * hi]);
+        dp[4 * st - 4] = d4.x; dp[4 * st - 3] = d4.y; dp[4 * st - 2] = d4.z; dp[4 * st - 1] = d4.w;
+      }
+      SLOT();
+    }
+    if (CAP) cap16(s, ku);
+#pragma unroll
+    for (int st = 0; st < 8; ++st) {  // dP - D; P of elements 0 .. 11
+      dp = mfma32(oa[st], vop[st], dp);
+      if (st + 3 < 8) oa[st + 3] = read_row(ob, orow, st + 3);
+      else tr_o[st - 5] = read_tr(ob, otr, st - 5);
+      if (st < 4) nl[st] = *reinterpret_cast<const float4*>(&Lt[P][32 * blk + 8 * st + 4 * hi]);
+      if (st >= 2) exps(2 * (st - 2));
+      SLOT();
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {  // dV; the rest of P, then dS
+      const int mb = u & 3;
+      dv[mb] = mfma32(tr_o[u], p_op(u >> 2), dv[mb]);
+      if (u + 3 < 8) tr_o[u + 3] = read_tr(ob + 16 * ((u + 3) >> 2) * D, otr, (u + 3) & 3);
+      else tr_q[u - 5] = read_tr(qb_, otr, u - 5);
+      if (u < 2) exps(12 + 2 * u);
+      if (u >= 3 && u < 7) {
+#pragma unroll
+        for (int i = 4 * (u - 3); i < 4 * (u - 3) + 4; ++i) dp[i] *= s[i];
+      }
+      if (u == 5) db[0] = pack8(dp, 0);
+      if (u == 7) db[1] = pack8(dp, 1);
+      SLOT();
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {  // dK
+      const int mb = u & 3;
+      dk[mb] = mfma32(tr_q[u], db[u >> 2], dk[mb]);
+      if (u + 3 < 8) tr_q[u + 3] = read_tr(qb_ + 16 * ((u + 3) >> 2) * D, otr, (u + 3) & 3);
+      SLOT();
+    }
+  };
+  Tile cur{-1, 0, false, false, false}, nxt = cur;
+  if (left_items > 0) {
+    begin_head();
+    cur = next();
+  }
+  if (cur.t >= 0) {
+    copies(cur, Q0, O0);
+    put_rows(0);
+  }
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  auto step = [&](auto par) __attribute__((always_inline)) {
+    constexpr int P = decltype(par)::value;
+    const uint16_t* const qt = P ? Q1 : Q0;
+    const uint16_t* const ot = P ? O1 : O0;
+    uint32_t seen = 0xffffffffu;
+    if (cur.mine && !cur.whole) {
+      const int from = rmin == INT32_MIN ? INT32_MIN : rmin - cur.t * BN - 4 * hi;  // first element row seen
+      seen = 0;
+      u32x4 d[8];
+      if (docs) {
+        const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(c.s.q_doc + (size_t)b * c.Lq), (short)0, c.Lq * 4, kBufferFlags);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          d[i] = __builtin_amdgcn_raw_buffer_load_b128(rd, (cur.t * BN + 8 * i + 4 * hi) * 4, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const bool s = acc_row(i >> 4, i & 15) >= from && (!docs || (int)d[i >> 2][i & 3] == kd);
+        seen |= s ? 1u << i : 0u;
+      }
+    }
+    nxt = next();
+    if (nxt.t >= 0) copies(nxt, P ? Q0 : Q1, P ? O0 : O1);
+    if (cur.mine) {
+      const float slope = BIAS ? -c.s.slopes[hk * rep + cur.g] * kLog2e : 0.f;
+      using zero = std::integral_constant<int, 0>;
+      using one = std::integral_constant<int, 1>;
+      if (cur.whole) {
+        block(std::false_type(), zero(), par, cur, qt, ot, seen, slope);
+        block(std::false_type(), one(), par, cur, qt, ot, seen, slope);
+      } else {
+        block(std::true_type(), zero(), par, cur, qt, ot, seen, slope);
+        block(std::true_type(), one(), par, cur, qt, ot, seen, slope);
+      }
+    }
+    cur = nxt;
+    if (nxt.t >= 0) put_rows(1 - P);
+    __builtin_amdgcn_s_waitcnt(0);  // this wave's copies have landed
+    __syncthreads();
+    return cur.t >= 0;
+  };
+  if (cur.t >= 0)
+    while (step(std::integral_constant<int, 0>()) && step(std::integral_constant<int, 1>())) {
+    }
+  if (a.runs > 1) return partials_out();
+  uint16_t* const area = KB + wave * 32 * D;  // read by this wave alone
+  rows_out(a.dk, dk, c.scale, area);
+  rows_out(a.dv, dv, 1.f, area);
+}
+
+// dK = scale * sum of the runs' partials, dV = their sum: 8 values a thread.
+__global__ __launch_bounds__(256) void mod_reduce_kernel(BwdArgs a) {
+  const size_t n = (size_t)a.c.B * a.c.Lk * a.c.Hkv * D, groups = n / 8;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < 2 * groups; i += (size_t)gridDim.x * 256) {
+    const bool isk = i < groups;
+    const size_t e = (isk ? i : i - groups) * 8;
+    const float* src = a.part + (isk ? 0 : (size_t)a.runs * n) + e;
+    float4 x0 = make_float4(0.f, 0.f, 0.f, 0.f), x1 = x0;
+    for (int r = 0; r < a.runs; ++r) {
+      const float4 u = *reinterpret_cast<const float4*>(src + (size_t)r * n);
+      const float4 v = *reinterpret_cast<const float4*>(src + (size_t)r * n + 4);
+      x0.x += u.x; x0.y += u.y; x0.z += u.z; x0.w += u.w;
+      x1.x += v.x; x1.y += v.y; x1.z += v.z; x1.w += v.w;
+    }
+    const float m = isk ? a.c.scale : 1.f;
+    uint4 o;
+    o.x = pack_bf16x2(x0.x * m, x0.y * m);
+    o.y = pack_bf16x2(x0.z * m, x0.w * m);
+    o.z = pack_bf16x2(x1.x * m, x1.y * m);
+    o.w = pack_bf16x2(x1.z * m, x1.w * m);
+    *reinterpret_cast<uint4*>((isk ? a.dk : a.dv) + e) = o;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
+  const ModCall& c = f.c;
+  const bool docs = c.s.k_doc != nullptr;
+  const ModBwdSplit s = mod_bwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, docs, device_cu_count(), f.ws_floats);
+  BwdArgs a;
+  a.c = c;
+  a.sc = make_scores(c);
+  a.q = f.q; a.k = f.k; a.v = f.v; a.o = f.o; a.dout = f.dout; a.lse = f.lse;
+  a.dq = f.dq; a.dk = f.dk; a.dv = f.dv;
+  a.delta = f.ws + s.delta;
+  a.empty = reinterpret_cast<int32_t*>(f.ws + s.empty);
+  a.part = f.ws + s.part;
+  a.kr = (int)mod_ranges(c.Lk);
+  a.qr = (int)mod_ranges(c.Lq);
+  a.runs = s.runs;
+  hipError_t e = launch_mod_ranges(c, f.ws, &a.r, stream);
+  if (e != hipSuccess) return e;
+  const bool cap = c.s.cap > 0.f, bias = c.s.slopes != nullptr;
+  if (c.Lq > 0) {
+    a.ntile = (c.Lq + BM - 1) / BM;
+    a.nwg = a.ntile * c.B * c.H;
+    const unsigned grid = (unsigned)a.nwg;
+    e = cap ? (bias ? launch_kernel(mod_dq_kernel<true, true>, grid, (unsigned)NT, stream, a)
+                    : launch_kernel(mod_dq_kernel<true, false>, grid, (unsigned)NT, stream, a))
+            : (bias ? launch_kernel(mod_dq_kernel<false, true>, grid, (unsigned)NT, stream, a)
+                    : launch_kernel(mod_dq_kernel<false, false>, grid, (unsigned)NT, stream, a));
+    if (e != hipSuccess) return e;
+  }
+  if (c.Lk > 0) {
+    a.ntile = (c.Lk + BM - 1) / BM;
+    a.nwg = a.ntile * c.B * c.Hkv * s.runs;
+    const unsigned grid = (unsigned)a.nwg;
+    e = cap ? (bias ? launch_kernel(mod_dkdv_kernel<true, true>, grid, (unsigned)NT, stream, a)
+                    : launch_kernel(mod_dkdv_kernel<true, false>, grid, (unsigned)NT, stream, a))
+            : (bias ? launch_kernel(mod_dkdv_kernel<false, true>, grid, (unsigned)NT, stream, a)
+                    : launch_kernel(mod_dkdv_kernel<false, false>, grid, (unsigned)NT, stream, a));
+    if (e != hipSuccess) return e;
+    if (s.runs > 1) {
+      size_t g = ((size_t)2 * c.B * c.Lk * c.Hkv * D / 8 + 255) / 256;
+      if (g > 16384) g = 16384;
+      e = launch_kernel(mod_reduce_kernel, (unsigned)g, 256u, stream, a);
+    }
+  }
+  return e;
+}
+
+}  // namespace vidax

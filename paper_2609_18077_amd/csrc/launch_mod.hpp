@@ -118,6 +118,43 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
   return r;
 }
 
+// ---- backward ----
+//
+// D, the flags of rows that see nothing, and where the key side has few
+// workgroups the fp32 partial dK and dV of its runs.
+struct ModBwdSplit {
+  int runs;
+  size_t delta, empty, part;  // first values of these in the workspace (document ranges at 0)
+  size_t least, floats;       // values of the workspace: for one run, for `runs`
+};
+
+inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, int cus, size_t max_floats) {
+  auto up = [](size_t x) { return (x + 63) / 64 * 64; };
+  ModBwdSplit r;
+  r.runs = 1;
+  r.delta = up(mod_doc_floats(B, Lq, Lk, docs));
+  r.empty = up(r.delta + (size_t)B * H * Lq);
+  r.least = r.floats = r.empty + (size_t)B * mod_ranges(Lq);
+  r.part = up(r.least);
+  if (B == 0 || H == 0 || Lq == 0 || Lk == 0) return r;
+  const size_t run = 2 * (size_t)B * Lk * Hkv * 128;  // partial values of a run
+  const int64_t items = (int64_t)(H / Hkv) * ((Lq + 63) / 64), wgs = (int64_t)((Lk + 255) / 256) * B * Hkv;
+  double best = 1e30;
+  for (int s = 1; s <= 32 && s <= items; ++s) {
+    const size_t need = r.part + s * run;
+    if (s > 1 && (need > max_floats || s * run > ((size_t)96 << 20))) break;
+    // in tiles' times (2 us): rounds x (tiles a run + start and end) + the launch and bytes of the sum
+    const int64_t rounds = (wgs * s + cus - 1) / cus;
+    const double cost = rounds * ((items + s - 1) / s + 2.0) + (s > 1 ? 3.0 + s * (run * 8 / 14e6) : 0.0);
+    if (cost < best) {
+      best = cost;
+      r.runs = s;
+      if (s > 1) r.floats = need;
+    }
+  }
+  return r;
+}
+
 __attribute__((weak)) hipError_t launch_attn_mod_fwd(const ModFwd& a, hipStream_t stream);
 __attribute__((weak)) hipError_t launch_attn_mod_bwd(const ModBwd& a, hipStream_t stream);
 

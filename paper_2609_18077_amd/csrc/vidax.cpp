@@ -477,6 +477,51 @@ vidax_status vidax_attn_mod_fwd(const void* q, const void* k, const void* v, voi
   return vidax::launch_attn_mod_fwd(a, stream) == hipSuccess ? VIDAX_OK : VIDAX_ERR_LAUNCH;
 }
 
+vidax_status vidax_attn_mod_bwd(const void* q, const void* k, const void* v, const void* o, const void* dout,
+                                const float* lse, void* dq, void* dk, void* dv, int32_t B, int32_t H, int32_t Hkv,
+                                int32_t Lq, int32_t Lk, int32_t d, float scale, const vidax_score_desc* score,
+                                float* workspace, size_t workspace_floats, hipStream_t stream) {
+  vidax::ModBwd a;
+  Buf s[6];
+  const vidax_status st = mod_common(B, H, Hkv, Lq, Lk, d, scale, score, &a.c, s);
+  if (st == VIDAX_ERR_INVALID_ARG) return st;
+  const uint64_t nq = (uint64_t)B * Lq * H * d, nk = (uint64_t)B * Lk * Hkv * d, nr = (uint64_t)B * H * Lq;
+  if ((nq > 0 && (!q || !o || !dout || !dq || !lse)) || (nk > 0 && (!dk || !dv)) || (nq > 0 && nk > 0 && (!k || !v)))
+    return VIDAX_ERR_INVALID_ARG;
+  for (const void* p : {q, k, v, o, dout, (const void*)dq, (const void*)dk, (const void*)dv, (const void*)workspace})
+    if (!aligned(p, 16)) return VIDAX_ERR_INVALID_ARG;
+  if (!aligned(lse, 4) || workspace_floats > ((uint64_t)1 << 60)) return VIDAX_ERR_INVALID_ARG;
+  if (!workspace) workspace_floats = 0;
+  const Buf outs[4] = {{dq, nq * 2}, {dk, nk * 2}, {dv, nk * 2}, {workspace, (uint64_t)workspace_floats * 4}};
+  const Buf ins[12] = {{q, nq * 2}, {k, nk * 2}, {v, nk * 2}, {o, nq * 2}, {dout, nq * 2}, {lse, nr * 4},
+                       s[0], s[1], s[2], s[3], s[4], s[5]};
+  if (any_overlap(outs, ins)) return VIDAX_ERR_INVALID_ARG;
+  if (st != VIDAX_OK || (nq == 0 && nk == 0)) return st;
+  const size_t least = vidax::mod_bwd_split(B, H, Hkv, Lq, Lk, a.c.s.k_doc != nullptr, 1, 0).least;
+  if (workspace_floats < least) return VIDAX_ERR_INVALID_ARG;
+  if (!vidax::launch_attn_mod_bwd) return VIDAX_ERR_LAUNCH;
+  a.q = (const uint16_t*)q;
+  a.k = (const uint16_t*)k;
+  a.v = (const uint16_t*)v;
+  a.o = (const uint16_t*)o;
+  a.dout = (const uint16_t*)dout;
+  a.lse = lse;
+  a.dq = (uint16_t*)dq;
+  a.dk = (uint16_t*)dk;
+  a.dv = (uint16_t*)dv;
+  a.ws = workspace;
+  a.ws_floats = workspace_floats;
+  return vidax::launch_attn_mod_bwd(a, stream) == hipSuccess ? VIDAX_OK : VIDAX_ERR_LAUNCH;
+}
+
+size_t vidax_attn_mod_bwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, int32_t Lq, int32_t Lk, int32_t d,
+                                           int32_t docs) {
+  vidax::ModCall c;
+  Buf s[6];
+  if (mod_common(B, H, Hkv, Lq, Lk, d, 1.0f, nullptr, &c, s) != VIDAX_OK) return 0;
+  return vidax::mod_bwd_split(B, H, Hkv, Lq, Lk, docs != 0, vidax::device_cu_count(), SIZE_MAX).floats;
+}
+
 size_t vidax_attn_mod_fwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, int32_t Lq, int32_t Lk, int32_t d,
                                            int32_t docs) {
   vidax::ModCall c;

@@ -63,6 +63,28 @@ __device__ __forceinline__ bf16x8 apply_sign(uint4 x, const Scores& s) {
   return __builtin_bit_cast(bf16x8, make_uint4((x.x ^ s.qxor) & s.qand, (x.y ^ s.qxor) & s.qand, (x.z ^ s.qxor) & s.qand,
                                                (x.w ^ s.qxor) & s.qand));
 }
+// 1 - t^2; 0 for the -inf of what is not seen.
+__device__ __forceinline__ float cap_slope(float t) { return __builtin_amdgcn_fmed3f(fmaf(-t, t, 1.f), 0.f, 1.f); }
+// 0 for the 16 elements of a block that are seen, -inf for the others: the value
+// that their products start from (or that replaces them, after a cap).
+//   causal part: element rows [from, to) of the lane half's block are seen;
+//   documents (ids != null): those of id `own` (four 16-byte LDS reads).
+template <typename F>
+__device__ __forceinline__ void each_hidden(int from, int to, const int* ids, int own, F&& hide) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (acc_row(0, i) < from || acc_row(0, i) >= to) hide(i);
+  if (ids) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int4 d = *reinterpret_cast<const int4*>(ids + 8 * g);
+      if (d.x != own) hide(4 * g);
+      if (d.y != own) hide(4 * g + 1);
+      if (d.z != own) hide(4 * g + 2);
+      if (d.w != own) hide(4 * g + 3);
+    }
+  }
+}
 // 64-row tile `t` of rows [0, limit) of a buffer: later rows read as zero.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const uint16_t* base, int t, int limit, int tok) {
   const int nbytes = __builtin_amdgcn_readfirstlane(min(max(limit - t * BN, 0), BN) * tok * 2);
@@ -74,6 +96,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const uint16_t* base
 template <bool CAP, bool BIAS>
 __device__ __forceinline__ void dq_body(const BwdArgs& a) {
   __shared__ __attribute__((aligned(1024))) uint16_t K0[TILE], K1[TILE], V0[TILE], V1[TILE];
+  __shared__ __attribute__((aligned(16))) int Kd[2][BN];  // ids of the tiles' keys
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const ModCall& c = a.c;
@@ -251,7 +274,14 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_ptr)(vb + (2 * wave + u) * 512), 16, g, 0, 0, 0);
     }
   };
+  // ids of a tile's keys, with the copies; into LDS at the end of the step
+  int kid = 0;
+  auto load_ids = [&](int t) __attribute__((always_inline)) {
+    if (docs && tid < BN) kid = c.s.k_doc[(size_t)b * c.Lk + min(t * BN + tid, c.Lk - 1)];
+  };
+  load_ids(cur.t);
   copies(cur, K0, V0);
+  if (docs && tid < BN) Kd[0][tid] = kid;
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
 
@@ -259,23 +289,26 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
   const float slope = BIAS ? -c.s.slopes[h] * kLog2e : 0.f;
   // One tile, one slot a product, as in the dense backward: each slot issues the
   // operand reads of the product three slots on and its share of the vector work.
-  // With a cap both blocks' scores come first (their tanh branches), and the
-  // exponentials run beside dP.  MASK: elements that are not seen get P = 0.
-  auto products = [&](auto msk, const Tile& t, const uint16_t* kt, const uint16_t* vt, uint32_t seen) __attribute__((always_inline)) {
-    constexpr bool MASK = decltype(msk)::value;
+  // What the row does not see starts at -inf, which the products keep.  With a cap
+  // both blocks' scores come first (their tanh branches), the exponentials run
+  // beside dP, and what is not seen becomes -inf after the tanh.
+  auto products = [&](const Tile& t, const uint16_t* kt, const uint16_t* vt, const int* ids) __attribute__((always_inline)) {
     const int orow = in_loop(off.row, t.t), otr = in_loop(off.tr, t.t);
     f32x16 sc[2], dp[2];
     bf16x8 ds[2][2];
     const float dist = BIAS ? (float)(bt.start + qrow - t.t * BN - 4 * hi) : 0.f;
+    auto hidden = [&](int blk, f32x16& x) __attribute__((always_inline)) {
+      each_hidden(INT32_MIN, lim - t.t * BN - 4 * hi - 32 * blk, docs ? ids + 32 * blk + 4 * hi : nullptr, qd,
+                  [&](int i) __attribute__((always_inline)) { x[i] = -INFINITY; });
+    };
     auto exps = [&](int blk, int i0) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = i0; i < i0 + 2; ++i) {
         const float s = sc[blk][i];
         float x = fmaf(s, mul, -lse2);
         if (BIAS) x = fmaf(slope, fabsf(dist - (float)acc_row(blk, i)), x);
-        if (MASK) x = (seen >> (16 * blk + i)) & 1 ? x : -INFINITY;
         float p = __builtin_amdgcn_exp2f(x);
-        if (CAP) p *= fmaf(-s, s, 1.f);
+        if (CAP) p *= cap_slope(s);
         sc[blk][i] = p;
       }
     };
@@ -304,7 +337,15 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) dp[blk][i] = -dl;
         dp[blk] = mfma32(op[n], dop[u], dp[blk]);
-      } else sc[blk] = mfma32(op[n], qop[u], u == 0 ? f32x16{} : sc[blk]);
+      } else if constexpr (u > 0 || CAP) {
+        sc[blk] = mfma32(op[n], qop[u], u == 0 ? f32x16{} : sc[blk]);
+      } else if (t.whole) {  // uniform
+        sc[blk] = mfma32(op[n], qop[u], f32x16{});
+      } else {
+        f32x16 x = f32x16{};
+        hidden(blk, x);
+        sc[blk] = mfma32(op[n], qop[u], x);
+      }
     };
     // vector work of block vb from slot `from` on: eight slots of exponentials, four of products, the packs
     auto vector = [&](auto N, auto V, auto F) __attribute__((always_inline)) {
@@ -326,6 +367,10 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
       });
       cap16(sc[0], ku);
       cap16(sc[1], ku);
+      if (!t.whole) {
+        hidden(0, sc[0]);
+        hidden(1, sc[1]);
+      }
       for_slots<32>([&](auto M) __attribute__((always_inline)) {
         using N = std::integral_constant<int, decltype(M)::value + 16>;
         product(N());
@@ -348,30 +393,13 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
     constexpr int P = decltype(par)::value;
     const uint16_t* const kt = P ? K1 : K0;
     const uint16_t* const vt = P ? V1 : V0;
-    uint32_t seen = 0xffffffffu;  // bit 16 blk + i: element i of block blk
-    if (cur.mine && !cur.whole) {
-      const int left = lim - cur.t * BN - 4 * hi;
-      seen = 0;
-      u32x4 d[8];
-      if (docs) {
-        const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc(
-            (void*)(c.s.k_doc + (size_t)b * c.Lk), (short)0, c.Lk * 4, kBufferFlags);
-#pragma unroll
-        for (int g = 0; g < 8; ++g)
-          d[g] = __builtin_amdgcn_raw_buffer_load_b128(rd, (cur.t * BN + 8 * g + 4 * hi) * 4, 0, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const bool s = acc_row(i >> 4, i & 15) < left && (!docs || (int)d[i >> 2][i & 3] == qd);
-        seen |= s ? 1u << i : 0u;
-      }
-    }
     nxt = next();
-    if (nxt.t >= 0) copies(nxt, P ? K0 : K1, P ? V0 : V1);
-    if (cur.mine) {
-      if (cur.whole) products(std::false_type(), cur, kt, vt, seen);
-      else products(std::true_type(), cur, kt, vt, seen);
+    if (nxt.t >= 0) {
+      load_ids(nxt.t);
+      copies(nxt, P ? K0 : K1, P ? V0 : V1);
     }
+    if (cur.mine) products(cur, kt, vt, Kd[P]);
+    if (docs && tid < BN) Kd[1 - P][tid] = kid;
     cur = nxt;
     __builtin_amdgcn_s_waitcnt(0);  // this wave's copies have landed
     __syncthreads();
@@ -394,6 +422,7 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
   __shared__ __attribute__((aligned(1024))) uint16_t Q0[TILE], Q1[TILE], O0[TILE], O1[TILE];
   __shared__ __attribute__((aligned(16))) uint16_t KB[NW * 32 * D];
   __shared__ __attribute__((aligned(16))) float Lt[2][BN], Dt[2][BN];
+  __shared__ __attribute__((aligned(16))) int Qd[2][BN];  // ids of the tiles' queries
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const ModCall& c = a.c;
@@ -553,6 +582,7 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
   }
   const size_t qbase = (size_t)b * c.Lq * qtok;
   float lrow = INFINITY, drow = 0.f;
+  int qid = 0;
   auto copies = [&](const Tile& t, uint16_t* qs, uint16_t* os) __attribute__((always_inline)) {
     const size_t hoff = qbase + (size_t)(hk * rep + t.g) * D;
     const size_t lbase = ((size_t)b * c.H + hk * rep + t.g) * c.Lq;
@@ -573,22 +603,28 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
       lrow = r < c.Lq ? a.lse[lbase + r] : INFINITY;
       drow = r < c.Lq ? a.delta[lbase + r] : 0.f;
       if (lrow == -INFINITY) lrow = INFINITY;  // P = 0
+      if (docs) qid = c.s.q_doc[(size_t)b * c.Lq + min(r, c.Lq - 1)];
     }
   };
   auto put_rows = [&](int buf) __attribute__((always_inline)) {
     if (tid < BN) {
       Lt[buf][tid] = -lrow * kLog2e;
       Dt[buf][tid] = -drow;
+      if (docs) Qd[buf][tid] = qid;
     }
   };
   const RowOffsets off = row_offsets(lane);
   const float mul = a.sc.mul, ku = a.sc.ku;
   // One 32-query block of a tile, one slot a product (as in the dense backward).
   // Without a cap P is formed beside dP; with one the scores' tanh comes first.
-  auto block = [&](auto msk, auto B_, auto par, const Tile& t, const uint16_t* qt, const uint16_t* ot, uint32_t seen, float slope)
+  auto block = [&](int blk, auto par, const Tile& t, const uint16_t* qt, const uint16_t* ot, float slope)
                    __attribute__((always_inline)) {
-    constexpr bool MASK = decltype(msk)::value;
-    constexpr int blk = decltype(B_)::value, P = decltype(par)::value;
+    constexpr int P = decltype(par)::value;
+    auto hidden = [&](f32x16& x) __attribute__((always_inline)) {
+      each_hidden(rmin == INT32_MIN ? INT32_MIN : rmin - t.t * BN - 4 * hi - 32 * blk, INT32_MAX,
+                  docs ? &Qd[P][32 * blk + 4 * hi] : nullptr, kd,
+                  [&](int i) __attribute__((always_inline)) { x[i] = -INFINITY; });
+    };
     const int orow = in_loop(off.row, t.t), otr = in_loop(off.tr, t.t);
     const uint16_t* const qb_ = qt + 32 * blk * D;
     const uint16_t* const ob = ot + 32 * blk * D;
@@ -605,9 +641,8 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
         const float z = s[i + e];
         float x = fmaf(z, mul, (i & 2) ? (e ? l4.w : l4.z) : (e ? l4.y : l4.x));
         if (BIAS) x = fmaf(slope, fabsf(dist + (float)acc_row(0, i + e)), x);
-        if (MASK) x = (seen >> (16 * blk + i + e)) & 1 ? x : -INFINITY;
         p[e] = __builtin_amdgcn_exp2f(x);
-        s[i + e] = CAP ? p[e] * fmaf(-z, z, 1.f) : p[e];
+        s[i + e] = CAP ? p[e] * cap_slope(z) : p[e];
       }
       pw[i >> 1] = pack_bf16x2(p[0], p[1]);
     };
@@ -623,7 +658,12 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
     SLOT();
 #pragma unroll
     for (int st = 0; st < 8; ++st) {  // S
-      s = mfma32(qa_[st], ka[st], s);
+      if (st == 0 && !CAP && !t.whole) {  // uniform
+        hidden(s);
+        s = mfma32(qa_[st], ka[st], s);
+      } else {
+        s = mfma32(qa_[st], ka[st], st == 0 ? f32x16{} : s);
+      }
       if (st + 3 < 8) read_qk(st + 3);
       else oa[st - 5] = read_row(ob, orow, st - 5);
       if (st >= 1 && st < 5) {
@@ -632,7 +672,10 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
       }
       SLOT();
     }
-    if (CAP) cap16(s, ku);
+    if (CAP) {
+      cap16(s, ku);
+      if (!t.whole) hidden(s);
+    }
 #pragma unroll
     for (int st = 0; st < 8; ++st) {  // dP - D; P of elements 0 .. 11
       dp = mfma32(oa[st], vop[st], dp);
@@ -680,37 +723,12 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
     constexpr int P = decltype(par)::value;
     const uint16_t* const qt = P ? Q1 : Q0;
     const uint16_t* const ot = P ? O1 : O0;
-    uint32_t seen = 0xffffffffu;
-    if (cur.mine && !cur.whole) {
-      const int from = rmin == INT32_MIN ? INT32_MIN : rmin - cur.t * BN - 4 * hi;  // first element row seen
-      seen = 0;
-      u32x4 d[8];
-      if (docs) {
-        const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc(
-            (void*)(c.s.q_doc + (size_t)b * c.Lq), (short)0, c.Lq * 4, kBufferFlags);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          d[i] = __builtin_amdgcn_raw_buffer_load_b128(rd, (cur.t * BN + 8 * i + 4 * hi) * 4, 0, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const bool s = acc_row(i >> 4, i & 15) >= from && (!docs || (int)d[i >> 2][i & 3] == kd);
-        seen |= s ? 1u << i : 0u;
-      }
-    }
     nxt = next();
     if (nxt.t >= 0) copies(nxt, P ? Q0 : Q1, P ? O0 : O1);
     if (cur.mine) {
       const float slope = BIAS ? -c.s.slopes[hk * rep + cur.g] * kLog2e : 0.f;
-      using zero = std::integral_constant<int, 0>;
-      using one = std::integral_constant<int, 1>;
-      if (cur.whole) {
-        block(std::false_type(), zero(), par, cur, qt, ot, seen, slope);
-        block(std::false_type(), one(), par, cur, qt, ot, seen, slope);
-      } else {
-        block(std::true_type(), zero(), par, cur, qt, ot, seen, slope);
-        block(std::true_type(), one(), par, cur, qt, ot, seen, slope);
-      }
+#pragma unroll
+      for (int blk = 0; blk < 2; ++blk) block(blk, par, cur, qt, ot, slope);
     }
     cur = nxt;
     if (nxt.t >= 0) put_rows(1 - P);

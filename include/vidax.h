@@ -324,8 +324,8 @@ typedef struct vidax_score_desc {
  *   lse  : fp32 [B, H, Lq], natural-log sum-exp of the seen scores, or NULL.
  *   score: host pointer, or NULL (no modifier, all keys seen).
  *   workspace: fp32 device memory, 16-byte aligned.  With documents at least
- *          2 B (2 ceil(Lk / 64) + 2 ceil(Lq / 64)) values (VIDAX_ERR_INVALID_ARG
- *          below); otherwise NULL is allowed.  With at least
+ *          B (4 ceil(Lk / 64) + 4 ceil(Lq / 64) + ceil(Lk / 256) + ceil(Lq / 256))
+ *          values (VIDAX_ERR_INVALID_ARG below); otherwise NULL is allowed.  With at least
  *          vidax_attn_mod_fwd_workspace_floats(...) values, calls of few query
  *          rows cut the keys into runs that work side by side; with fewer they
  *          take the runs that fit.  The result differs by fp32 rounding only.
@@ -367,8 +367,8 @@ size_t vidax_attn_mod_fwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, in
  *              the query stream into runs that work side by side, their fp32 sums
  *              added in a further launch (at most 384 MiB); with fewer it takes the
  *              runs that fit; VIDAX_ERR_INVALID_ARG below what one run needs,
- *              B H Lq + 2 ceil(Lq / 64) B + 192 values and, with documents, twice
- *              2 B (ceil(Lk / 64) + ceil(Lq / 64)) more.
+ *              B H Lq + 2 ceil(Lq / 64) B + 192 values and, with documents, those
+ *              of the forward more.
  * Same call, same bits: no atomics.  Products on bf16 inputs (P and ds rounded to
  * bf16) with fp32 accumulation.  Pointers, sizes and overlap as for the forward
  * (lse 4-byte aligned).

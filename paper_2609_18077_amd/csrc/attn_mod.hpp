@@ -105,10 +105,64 @@ __device__ __forceinline__ Docs uniform(const Docs& d) {
               (bool)__builtin_amdgcn_readfirstlane((int)d.neg)};
 }
 __device__ __forceinline__ bool meet(const Docs& a, const Docs& b) { return a.lo <= b.hi && b.lo <= a.hi; }
+// all of one document
+__device__ __forceinline__ bool one_doc(const Docs& a) { return !a.neg && a.lo == a.hi; }
 // every token of both in one and the same document
 __device__ __forceinline__ bool same(const Docs& a, const Docs& b) {
-  return !a.neg && !b.neg && a.lo == a.hi && b.lo == b.hi && a.lo == b.lo;
+  return one_doc(a) && one_doc(b) && a.lo == b.lo;
 }
+
+// Which 256-row tile t of (batch b, head h of `heads`) and which of its runs the
+// workgroup takes.  Neighbours in number go to different XCDs.
+//   Tiles of equal work: an XCD takes a stretch of a head's tiles, whose other
+// side then stays in its L2.
+//   Otherwise the most work first, all heads of a tile side by side: a late
+// start of a long tile would hold the launch up (16384 causal, 12 heads: 1172 us
+// with long and short tiles in turn, XCD by XCD; 845 so).
+template <typename A>
+__device__ __forceinline__ void place(const A& a, int heads, const int32_t* order, int& run, int& t, int& b, int& h) {
+  const ModCall& c = a.c;
+  if (order || c.s.causal || c.s.kv_valid_len) {
+    int i = blockIdx.x;
+    run = i % a.runs;
+    i /= a.runs;
+    if (order) {
+      h = i % heads;
+      const int x = __builtin_amdgcn_readfirstlane(order[i / heads]);
+      b = x / a.ntile;
+      t = x - b * a.ntile;
+    } else {
+      const int n = c.B * heads, bh = i % n;
+      b = bh / heads;
+      h = bh - b * heads;
+      t = a.first_most ? i / n : a.ntile - 1 - i / n;
+    }
+    return;
+  }
+  const int i = balanced_tile(blockIdx.x, a.nwg, c.B);
+  run = i % a.runs;
+  const int x = i / a.runs, bh = x / a.ntile;
+  t = x - bh * a.ntile;
+  b = bh / heads;
+  h = bh - b * heads;
+}
+
+// A tile of the streamed side, as a workgroup or wave meets it (uniform).
+struct Tile {
+  int t;   // < 0: none left
+  int f;   // bits:
+  int id;  // kOne: the document
+  enum {
+    kMine = 1,   // some row of the wave may see (or be seen by) some of it
+    kWhole = 2,  // all of the wave's rows see (are seen by) all of it
+    kZero = 4,   // it holds tokens that have to be read as zeros
+    kOne = 8     // its tokens are of one document
+  };
+  __device__ __forceinline__ bool mine() const { return f & kMine; }
+  __device__ __forceinline__ bool whole() const { return f & kWhole; }
+  __device__ __forceinline__ bool zero() const { return f & kZero; }
+  __device__ __forceinline__ bool one() const { return f & kOne; }
+};
 
 // ---- tiles as rows: 256-byte rows whose 16-byte chunks are permuted, chunk c of
 // row r at position c ^ swz(r), free of bank conflicts for row reads and for the

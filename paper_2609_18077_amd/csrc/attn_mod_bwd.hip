@@ -42,6 +42,7 @@ struct BwdArgs {
   int kr, qr;         // ranges a batch
   int ntile, nwg;     // tiles of own rows a head, workgroups of the launched kernel
   int runs;           // key side: the stream is cut into runs, a workgroup each
+  int first_most;     // causal: the first tile of a head has the most work (else the last)
   float* part;        // runs > 1: fp32 dK, dV of every run ([runs][B][Lk][Hkv][D], dV after dK)
 };
 
@@ -68,7 +69,7 @@ __device__ __forceinline__ float cap_slope(float t) { return __builtin_amdgcn_fm
 // 0 for the 16 elements of a block that are seen, -inf for the others: the value
 // that their products start from (or that replaces them, after a cap).
 //   causal part: element rows [from, to) of the lane half's block are seen;
-//   documents (ids != null): those of id `own` (four 16-byte LDS reads).
+//   documents (ids != null, uniform): those of id `own` (four 16-byte LDS reads).
 template <typename F>
 __device__ __forceinline__ void each_hidden(int from, int to, const int* ids, int own, F&& hide) {
 #pragma unroll
@@ -100,10 +101,9 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const ModCall& c = a.c;
-  const int lid = balanced_tile(blockIdx.x, a.nwg, c.B);
-  int qt = lid % a.ntile;
-  if (c.s.causal) qt = qt & 1 ? qt >> 1 : a.ntile - 1 - (qt >> 1);  // (as in the forward)
-  const int bh = lid / a.ntile, h = bh % c.H, b = bh / c.H, hk = h / (c.H / c.Hkv);
+  int b, h, qt, run;
+  place(a, c.H, a.r.q_order, run, qt, b, h);
+  const int hk = h / (c.H / c.Hkv);
   const int qtok = c.H * D, qbytes = qtok * 2, ktok = c.Hkv * D, kbytes = ktok * 2;
   const Batch bt = batch_of(c, b);
   const int row0 = qt * BM, wrow = row0 + wave * 32, qrow = wrow + l32;
@@ -134,37 +134,30 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
   const int gmax = key_limit(bt, c.s.causal, bt.start + glast);
   const int end_tile = (gmax + BN - 1) / BN;
 
-  int grp = 0;
-  uint64_t visit = 0, mine = 0, whole = 0, neg = 0;
+  int grp = 0, fl = 0, id = 0;
+  uint64_t visit = 0;
   auto look = [&](int g) __attribute__((always_inline)) {
     const int t = 64 * g + lane;
-    const bool in = t < end_tile;
-    bool v = in, m = in && t * BN < wmax, w = in && t * BN + BN <= wmin, n = false;
-    if (docs && in) {
+    bool v = t < end_tile;
+    fl = (t * BN < wmax ? Tile::kMine : 0) | (t * BN + BN <= wmin ? Tile::kWhole : 0) | Tile::kOne;
+    if (docs && v) {
       const int4 r = *reinterpret_cast<const int4*>(a.r.k + (size_t)b * a.kr + 2 * t);
       const Docs d = mod::join(docs_of(make_int2(r.x, r.y)), docs_of(make_int2(r.z, r.w)));
       v = meet(d, gdoc);
-      m = m && meet(d, wdoc);
-      w = w && same(d, wdoc);
-      n = d.neg;
+      fl &= (meet(d, wdoc) ? Tile::kMine : 0) | (same(d, wdoc) ? Tile::kWhole : 0) | (one_doc(d) ? Tile::kOne : 0);
+      if (d.neg) fl |= Tile::kZero;
+      id = d.lo;
     }
     visit = __builtin_amdgcn_ballot_w64(v);
-    mine = __builtin_amdgcn_ballot_w64(m);
-    whole = __builtin_amdgcn_ballot_w64(w);
-    neg = __builtin_amdgcn_ballot_w64(n);
-  };
-  struct Tile {
-    int t;  // -1: none left
-    bool mine, whole, neg;
   };
   auto next = [&]() __attribute__((always_inline)) {
     while (visit == 0) {
-      if (64 * (grp + 1) >= end_tile) return Tile{-1, false, false, false};
+      if (64 * (grp + 1) >= end_tile) return Tile{-1, 0, 0};
       look(++grp);
     }
     const int i = __builtin_ctzll(visit);
     visit &= visit - 1;
-    return Tile{64 * grp + i, (bool)(mine >> i & 1), (bool)(whole >> i & 1), (bool)(neg >> i & 1)};
+    return Tile{64 * grp + i, __builtin_amdgcn_readlane(fl, i), __builtin_amdgcn_readlane(id, i)};
   };
 
   // own rows in and out whole, through the tile buffers
@@ -248,7 +241,7 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
   __builtin_amdgcn_s_waitcnt(0);  // the rows are out of the staging areas
   __syncthreads();
 
-  Tile cur{-1, false, false, false}, nxt = cur;
+  Tile cur{-1, 0, 0}, nxt = cur;
   if (end_tile > 0) {
     look(0);
     cur = next();
@@ -266,7 +259,7 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
     for (int u = 0; u < 2; ++u) {
       const int r = 4 * (2 * wave + u) + (lane >> 4);
       int g = r * kbytes + ((lane & 15) ^ swz(r)) * 16;
-      if (t.neg) {  // uniform: keys of negative documents arrive as zeros
+      if (t.zero()) {  // uniform: keys of negative documents arrive as zeros
         const int key = t.t * BN + r;
         if (key >= c.Lk || c.s.k_doc[(size_t)b * c.Lk + min(key, c.Lk - 1)] < 0) g = kOff;
       }
@@ -276,10 +269,10 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
   };
   // ids of a tile's keys, with the copies; into LDS at the end of the step
   int kid = 0;
-  auto load_ids = [&](int t) __attribute__((always_inline)) {
-    if (docs && tid < BN) kid = c.s.k_doc[(size_t)b * c.Lk + min(t * BN + tid, c.Lk - 1)];
+  auto load_ids = [&](const Tile& t) __attribute__((always_inline)) {
+    if (docs && !t.one() && tid < BN) kid = c.s.k_doc[(size_t)b * c.Lk + min(t.t * BN + tid, c.Lk - 1)];
   };
-  load_ids(cur.t);
+  load_ids(cur);
   copies(cur, K0, V0);
   if (docs && tid < BN) Kd[0][tid] = kid;
   __builtin_amdgcn_s_waitcnt(0);
@@ -298,7 +291,8 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
     bf16x8 ds[2][2];
     const float dist = BIAS ? (float)(bt.start + qrow - t.t * BN - 4 * hi) : 0.f;
     auto hidden = [&](int blk, f32x16& x) __attribute__((always_inline)) {
-      each_hidden(INT32_MIN, lim - t.t * BN - 4 * hi - 32 * blk, docs ? ids + 32 * blk + 4 * hi : nullptr, qd,
+      each_hidden(INT32_MIN, docs && t.one() && qd != t.id ? 0 : lim - t.t * BN - 4 * hi - 32 * blk,
+                  docs && !t.one() ? ids + 32 * blk + 4 * hi : nullptr, qd,
                   [&](int i) __attribute__((always_inline)) { x[i] = -INFINITY; });
     };
     auto exps = [&](int blk, int i0) __attribute__((always_inline)) {
@@ -339,7 +333,7 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
         dp[blk] = mfma32(op[n], dop[u], dp[blk]);
       } else if constexpr (u > 0 || CAP) {
         sc[blk] = mfma32(op[n], qop[u], u == 0 ? f32x16{} : sc[blk]);
-      } else if (t.whole) {  // uniform
+      } else if (t.whole()) {  // uniform
         sc[blk] = mfma32(op[n], qop[u], f32x16{});
       } else {
         f32x16 x = f32x16{};
@@ -367,7 +361,7 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
       });
       cap16(sc[0], ku);
       cap16(sc[1], ku);
-      if (!t.whole) {
+      if (!t.whole()) {
         hidden(0, sc[0]);
         hidden(1, sc[1]);
       }
@@ -395,11 +389,11 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
     const uint16_t* const vt = P ? V1 : V0;
     nxt = next();
     if (nxt.t >= 0) {
-      load_ids(nxt.t);
+      load_ids(nxt);
       copies(nxt, P ? K0 : K1, P ? V0 : V1);
     }
-    if (cur.mine) products(cur, kt, vt, Kd[P]);
-    if (docs && tid < BN) Kd[1 - P][tid] = kid;
+    if (cur.mine()) products(cur, kt, vt, Kd[P]);
+    if (docs && !nxt.one() && tid < BN) Kd[1 - P][tid] = kid;
     cur = nxt;
     __builtin_amdgcn_s_waitcnt(0);  // this wave's copies have landed
     __syncthreads();
@@ -426,10 +420,8 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const ModCall& c = a.c;
-  const int lid = balanced_tile(blockIdx.x, a.nwg, c.B);
-  int kt = lid % a.ntile;
-  if (c.s.causal) kt = kt & 1 ? kt >> 1 : a.ntile - 1 - (kt >> 1);
-  const int sbh = lid / a.ntile, run = sbh % a.runs, bh = sbh / a.runs, hk = bh % c.Hkv, b = bh / c.Hkv;
+  int b, hk, kt, run;
+  place(a, c.Hkv, a.r.k_order, run, kt, b, hk);
   const int rep = c.H / c.Hkv;
   const int qtok = c.H * D, qbytes = qtok * 2, ktok = c.Hkv * D, kbytes = ktok * 2;
   const Batch bt = batch_of(c, b);
@@ -452,69 +444,54 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
   const bool wlive = wkey < used;  // uniform
   const int wend = min(wkey + 32, used);  // behind the wave's last key
 
-  // query tiles of a head that may see a key of the workgroup: [qa, qb); the
-  // stream: heads of the group in turn, this run's part of rep (qb - qa) tiles
+  // query tiles of a head that may see a key of the workgroup lie in [qa, qb); the
+  // stream: those of the group's heads in turn, this run's part of it
   const int qb = (c.Lq + BN - 1) / BN;
   int qa = 0;
   if (c.s.causal && key0 >= bt.prefix) qa = min(max(key0 - bt.start, 0) / BN, qb);
-  const int64_t items = key0 < used ? (int64_t)rep * (qb - qa) : 0;
-  const int64_t i0 = items * run / a.runs, i1 = items * (run + 1) / a.runs;
-  int g = qb > qa ? (int)(i0 / (qb - qa)) : 0;  // head of the group
-  int ta = qb > qa ? qa + (int)(i0 % (qb - qa)) : 0, tb = 0;  // its tiles
-  int64_t left_items = i1 - i0;
+  if (key0 >= used) qa = qb;
   // first row that sees the lane's key, by position (-2^31: all, prefix)
   const int rmin = !c.s.causal || krow < bt.prefix ? INT32_MIN : krow - bt.start;
   const int wrmax = !c.s.causal || wend - 1 < bt.prefix ? INT32_MIN : wend - 1 - bt.start;  // first row that sees all of the wave's
   const int wrmin = !c.s.causal || wkey < bt.prefix ? INT32_MIN : wkey - bt.start;          // ... that sees one of them
 
-  int grp = 0;
-  uint64_t visit = 0, mine = 0, whole = 0, none = 0;
+  int grp = qa >> 6, g = 0;  // group of 64 tiles, head of the group
+  int left = 0;              // tiles to visit in this run
+  int fl = 0, id = 0;
+  uint64_t visit = 0;
   auto look = [&](int s) __attribute__((always_inline)) {
     const int t = 64 * s + lane;
-    const bool in = t >= ta && t < tb;
-    bool v = in, m = in && wlive && t * BN + BN - 1 >= wrmin, w = in && t * BN >= wrmax, n = false;
-    if (in) {
+    bool v = t >= qa && t < qb;
+    fl = (wlive && t * BN + BN - 1 >= wrmin ? Tile::kMine : 0) | (t * BN >= wrmax ? Tile::kWhole : 0) | Tile::kOne;
+    if (v) {
       const int2 e = *reinterpret_cast<const int2*>(a.empty + (size_t)b * a.qr + 2 * t);
-      n = (e.x != 0) || (t * BN + 32 < c.Lq && e.y != 0);
+      if (e.x != 0 || (t * BN + 32 < c.Lq && e.y != 0)) fl |= Tile::kZero;
       if (docs) {
         const int4 r = *reinterpret_cast<const int4*>(a.r.q + (size_t)b * a.qr + 2 * t);
         const Docs d = mod::join(docs_of(make_int2(r.x, r.y)), docs_of(make_int2(r.z, r.w)));
         v = meet(d, gdoc);
-        m = m && meet(d, wdoc);
-        w = w && same(d, wdoc);
+        fl &= Tile::kZero | (meet(d, wdoc) ? Tile::kMine : 0) | (same(d, wdoc) ? Tile::kWhole : 0) |
+              (one_doc(d) ? Tile::kOne : 0);
+        id = d.lo;
       }
     }
     visit = __builtin_amdgcn_ballot_w64(v);
-    mine = __builtin_amdgcn_ballot_w64(m);
-    whole = __builtin_amdgcn_ballot_w64(w);
-    none = __builtin_amdgcn_ballot_w64(n);
   };
-  // the tiles of head g from ta on, as far as the run goes
-  auto begin_head = [&]() __attribute__((always_inline)) {
-    const int64_t n = qb - ta < left_items ? qb - ta : left_items;
-    tb = ta + (int)n;
-    left_items -= n;
-    grp = ta >> 6;
-    look(grp);
-  };
-  struct Tile {
-    int t, g;  // t < 0: none left
-    bool mine, whole, none;
-  };
+  int head = 0;  // of the tile that next() gave last
   auto next = [&]() __attribute__((always_inline)) {
+    if (left-- <= 0) return Tile{-1, 0, 0};
     while (visit == 0) {
-      if (64 * (grp + 1) < tb) {
+      if (64 * (grp + 1) < qb) {
         look(++grp);
       } else {
-        if (left_items <= 0) return Tile{-1, 0, false, false, false};
         ++g;
-        ta = qa;
-        begin_head();
+        look(grp = qa >> 6);
       }
     }
+    head = g;
     const int i = __builtin_ctzll(visit);
     visit &= visit - 1;
-    return Tile{64 * grp + i, g, (bool)(mine >> i & 1), (bool)(whole >> i & 1), (bool)(none >> i & 1)};
+    return Tile{64 * grp + i, __builtin_amdgcn_readlane(fl, i), __builtin_amdgcn_readlane(id, i)};
   };
 
   f32x16 dk[4], dv[4];
@@ -584,14 +561,14 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
   float lrow = INFINITY, drow = 0.f;
   int qid = 0;
   auto copies = [&](const Tile& t, uint16_t* qs, uint16_t* os) __attribute__((always_inline)) {
-    const size_t hoff = qbase + (size_t)(hk * rep + t.g) * D;
-    const size_t lbase = ((size_t)b * c.H + hk * rep + t.g) * c.Lq;
+    const size_t hoff = qbase + (size_t)(hk * rep + head) * D;
+    const size_t lbase = ((size_t)b * c.H + hk * rep + head) * c.Lq;
     const __amdgpu_buffer_rsrc_t rq = tile_rsrc(a.q + hoff, t.t, c.Lq, qtok), ro = tile_rsrc(a.dout + hoff, t.t, c.Lq, qtok);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int r = 4 * (2 * wave + u) + (lane >> 4);
       int off = r * qbytes + ((lane & 15) ^ swz(r)) * 16;
-      if (t.none) {  // uniform: rows that see nothing arrive as zeros
+      if (t.zero()) {  // uniform: rows that see nothing arrive as zeros
         const int row = t.t * BN + r;
         if (row >= c.Lq || a.lse[lbase + min(row, c.Lq - 1)] == -INFINITY) off = kOff;
       }
@@ -603,7 +580,7 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
       lrow = r < c.Lq ? a.lse[lbase + r] : INFINITY;
       drow = r < c.Lq ? a.delta[lbase + r] : 0.f;
       if (lrow == -INFINITY) lrow = INFINITY;  // P = 0
-      if (docs) qid = c.s.q_doc[(size_t)b * c.Lq + min(r, c.Lq - 1)];
+      if (docs && !t.one()) qid = c.s.q_doc[(size_t)b * c.Lq + min(r, c.Lq - 1)];
     }
   };
   auto put_rows = [&](int buf) __attribute__((always_inline)) {
@@ -621,8 +598,9 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
                    __attribute__((always_inline)) {
     constexpr int P = decltype(par)::value;
     auto hidden = [&](f32x16& x) __attribute__((always_inline)) {
-      each_hidden(rmin == INT32_MIN ? INT32_MIN : rmin - t.t * BN - 4 * hi - 32 * blk, INT32_MAX,
-                  docs ? &Qd[P][32 * blk + 4 * hi] : nullptr, kd,
+      each_hidden(rmin == INT32_MIN ? INT32_MIN : rmin - t.t * BN - 4 * hi - 32 * blk,
+                  docs && t.one() && kd != t.id ? INT32_MIN : INT32_MAX,
+                  docs && !t.one() ? &Qd[P][32 * blk + 4 * hi] : nullptr, kd,
                   [&](int i) __attribute__((always_inline)) { x[i] = -INFINITY; });
     };
     const int orow = in_loop(off.row, t.t), otr = in_loop(off.tr, t.t);
@@ -658,7 +636,7 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
     SLOT();
 #pragma unroll
     for (int st = 0; st < 8; ++st) {  // S
-      if (st == 0 && !CAP && !t.whole) {  // uniform
+      if (st == 0 && !CAP && !t.whole()) {  // uniform
         hidden(s);
         s = mfma32(qa_[st], ka[st], s);
       } else {
@@ -674,7 +652,7 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
     }
     if (CAP) {
       cap16(s, ku);
-      if (!t.whole) hidden(s);
+      if (!t.whole()) hidden(s);
     }
 #pragma unroll
     for (int st = 0; st < 8; ++st) {  // dP - D; P of elements 0 .. 11
@@ -708,10 +686,30 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
       SLOT();
     }
   };
-  Tile cur{-1, 0, false, false, false}, nxt = cur;
-  if (left_items > 0) {
-    begin_head();
-    cur = next();
+  Tile cur{-1, 0, 0}, nxt = cur;
+  int cur_head = 0;
+  if (qa < qb) {
+    int n = qb - qa;  // tiles to visit of a head
+    if (docs) {
+      n = 0;
+      for (int s = grp; 64 * s < qb; ++s) {
+        look(s);
+        n += __builtin_popcountll(visit);
+      }
+    }
+    if (n > 0) {
+      const int64_t i0 = (int64_t)n * rep * run / a.runs, i1 = (int64_t)n * rep * (run + 1) / a.runs;
+      g = (int)(i0 / n);
+      left = (int)(i1 - i0);
+      int skip = (int)(i0 - (int64_t)g * n);
+      look(grp);
+      while (left > 0 && skip >= __builtin_popcountll(visit)) {
+        skip -= __builtin_popcountll(visit);
+        look(++grp);
+      }
+      for (; left > 0 && skip > 0; --skip) visit &= visit - 1;
+      cur = next();
+    }
   }
   if (cur.t >= 0) {
     copies(cur, Q0, O0);
@@ -723,10 +721,11 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
     constexpr int P = decltype(par)::value;
     const uint16_t* const qt = P ? Q1 : Q0;
     const uint16_t* const ot = P ? O1 : O0;
+    cur_head = head;
     nxt = next();
     if (nxt.t >= 0) copies(nxt, P ? Q0 : Q1, P ? O0 : O1);
-    if (cur.mine) {
-      const float slope = BIAS ? -c.s.slopes[hk * rep + cur.g] * kLog2e : 0.f;
+    if (cur.mine()) {
+      const float slope = BIAS ? -c.s.slopes[hk * rep + cur_head] * kLog2e : 0.f;
 #pragma unroll
       for (int blk = 0; blk < 2; ++blk) block(blk, par, cur, qt, ot, slope);
     }
@@ -773,8 +772,8 @@ __global__ __launch_bounds__(256) void mod_reduce_kernel(BwdArgs a) {
 
 hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
   const ModCall& c = f.c;
-  const bool docs = c.s.k_doc != nullptr;
-  const ModBwdSplit s = mod_bwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, docs, device_cu_count(), f.ws_floats);
+  const int cus = device_cu_count();
+  const ModBwdSplit s = mod_bwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr, cus, f.ws_floats);
   BwdArgs a;
   a.c = c;
   a.sc = make_scores(c);
@@ -785,13 +784,15 @@ hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
   a.part = f.ws + s.part;
   a.kr = (int)mod_ranges(c.Lk);
   a.qr = (int)mod_ranges(c.Lq);
-  a.runs = s.runs;
-  hipError_t e = launch_mod_ranges(c, f.ws, &a.r, stream);
+  const size_t qwg = mod_tiles(c.Lq) * c.B * c.H, kwg = mod_tiles(c.Lk) * c.B * c.Hkv * s.runs;
+  hipError_t e = launch_mod_ranges(c, f.ws, qwg > (size_t)cus, kwg > (size_t)cus, &a.r, stream);
   if (e != hipSuccess) return e;
   const bool cap = c.s.cap > 0.f, bias = c.s.slopes != nullptr;
   if (c.Lq > 0) {
     a.ntile = (c.Lq + BM - 1) / BM;
     a.nwg = a.ntile * c.B * c.H;
+    a.runs = 1;
+    a.first_most = 0;
     const unsigned grid = (unsigned)a.nwg;
     e = cap ? (bias ? launch_kernel(mod_dq_kernel<true, true>, grid, (unsigned)NT, stream, a)
                     : launch_kernel(mod_dq_kernel<true, false>, grid, (unsigned)NT, stream, a))
@@ -802,6 +803,8 @@ hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
   if (c.Lk > 0) {
     a.ntile = (c.Lk + BM - 1) / BM;
     a.nwg = a.ntile * c.B * c.Hkv * s.runs;
+    a.runs = s.runs;
+    a.first_most = 1;
     const unsigned grid = (unsigned)a.nwg;
     e = cap ? (bias ? launch_kernel(mod_dkdv_kernel<true, true>, grid, (unsigned)NT, stream, a)
                     : launch_kernel(mod_dkdv_kernel<true, false>, grid, (unsigned)NT, stream, a))

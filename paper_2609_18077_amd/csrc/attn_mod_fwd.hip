@@ -13,9 +13,11 @@
 //     a wave whose own 32 rows see nothing of a tile leaves its products out, and
 //     only a wave for which a tile is not seen whole by all its rows masks it.
 //   Masks.  A score that is not seen becomes -inf after the cap.  A row's
-//     reference m is unset until it has seen a key: its sum starts at +inf, which
-//     sends every block through the reset until then.  A row that sees nothing
-//     ends with a sum of 0: o = 0, lse = -inf.  Keys that no row may see (past
+//     reference m is unset until it has seen a key: a block's exponents are then
+//     1e30 too large, so that the first key seen overflows the block's sum and sets
+//     the reference, while a block without one passes (the rows of a later document
+//     wait through an earlier one's tiles).  A row that sees nothing ends with a
+//     sum of 0: o = 0, lse = -inf.  Keys that no row may see (past
 //     the valid length or the last row's position, or of a negative document) are
 //     read as zeros, so that nothing that lies there reaches the output.
 //   Sums add the fp32 probabilities, not their bf16 roundings: the log-sum-exp is
@@ -38,7 +40,7 @@ constexpr int NW = 8;
 constexpr int NT = NW * 64;
 constexpr int TILE = BN * D;  // elements of a K or V tile
 constexpr int BLK = 512;      // elements of an operand block
-constexpr int kNoTile = -1;
+constexpr float kUnset = 1e30f;
 
 struct FwdArgs {
   ModCall c;
@@ -48,7 +50,8 @@ struct FwdArgs {
   float* lse;
   float *po, *pl;  // partial outputs [runs][B][H][Lq][D] and log2-sum-exps [runs][B][H][Lq], or null
   ModRanges r;
-  int nqt, nwg, runs;
+  int ntile, nwg, runs;
+  int first_most;  // causal: the first tile of a head has the most work (else the last)
   int kr, qr;      // document ranges a batch
 };
 
@@ -56,6 +59,7 @@ struct FwdArgs {
 template <bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
   __shared__ __attribute__((aligned(16))) uint16_t K0[TILE], K1[TILE], V0[TILE], V1[TILE];
+  __shared__ __attribute__((aligned(16))) int Kd[2][BN];  // ids of the tiles' keys, where they differ
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -66,14 +70,9 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
   const int qtok = c.H * D, ktok = c.Hkv * D;  // elements between tokens
   const int qbytes = qtok * 2, kbytes = ktok * 2;
 
-  // Runs of one tile are neighbours (they share its queries), then the tiles of
-  // one head (they share its keys).  Causal tiles are taken from both ends in
-  // turn: any stretch of a head's tiles is then about the same work.
-  const int lid = balanced_tile(blockIdx.x, a.nwg, c.B);
-  const int run = lid % a.runs, t0 = lid / a.runs;
-  int qt = t0 % a.nqt;
-  if (c.s.causal) qt = qt & 1 ? qt >> 1 : a.nqt - 1 - (qt >> 1);
-  const int bh = t0 / a.nqt, h = bh % c.H, b = bh / c.H, hk = h / (c.H / c.Hkv);
+  int b, h, qt, run;
+  place(a, c.H, a.r.q_order, run, qt, b, h);
+  const int hk = h / (c.H / c.Hkv);
   const Batch bt = batch_of(c, b);
   const int row0 = qt * BM;                     // of the workgroup
   const int wrow = row0 + wave * 32;            // of the wave
@@ -104,43 +103,35 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
   const int wmin = wlast >= wrow ? key_limit(bt, c.s.causal, bt.start + wrow) : 0;
   const int gmax = key_limit(bt, c.s.causal, bt.start + glast);
   const int ntiles = (gmax + BN - 1) / BN;
-  const int first_tile = (int)((int64_t)ntiles * run / a.runs), end_tile = (int)((int64_t)ntiles * (run + 1) / a.runs);
 
   // ---- the next tile to visit: a group of 64 tiles is looked at together, lane
-  // l at tile 64 g + l.  (visit: some row of the workgroup may see a key of it;
-  // mine, whole: the same for the wave, all its rows see all of it; neg: it holds
-  // keys of negative documents.)
-  int grp = first_tile >> 6;
-  uint64_t visit = 0, mine = 0, whole = 0, neg = 0;
+  // l at tile 64 g + l.
+  int grp = 0, left = INT32_MAX;  // group; tiles left of this run
+  uint64_t visit = 0;             // tiles that some row of the workgroup may see
+  int fl = 0, id = 0;             // of the lane's tile
   auto look = [&](int g) __attribute__((always_inline)) {
     const int t = 64 * g + lane;
-    const bool in = t >= first_tile && t < end_tile;
-    bool v = in, m = in && t * BN < wmax, w = in && t * BN + BN <= wmin, n = false;
-    if (docs && in) {
+    bool v = t < ntiles;
+    fl = (t * BN < wmax ? Tile::kMine : 0) | (t * BN + BN <= wmin ? Tile::kWhole : 0) | Tile::kOne;
+    if (docs && v) {
       const int4 r = *reinterpret_cast<const int4*>(a.r.k + (size_t)b * a.kr + 2 * t);
       const Docs d = mod::join(docs_of(make_int2(r.x, r.y)), docs_of(make_int2(r.z, r.w)));
       v = meet(d, gdoc);
-      m = m && meet(d, wdoc);
-      w = w && same(d, wdoc);
-      n = d.neg;
+      fl &= (meet(d, wdoc) ? Tile::kMine : 0) | (same(d, wdoc) ? Tile::kWhole : 0) | (one_doc(d) ? Tile::kOne : 0);
+      if (d.neg) fl |= Tile::kZero;
+      id = d.lo;
     }
     visit = __builtin_amdgcn_ballot_w64(v);
-    mine = __builtin_amdgcn_ballot_w64(m);
-    whole = __builtin_amdgcn_ballot_w64(w);
-    neg = __builtin_amdgcn_ballot_w64(n);
-  };
-  struct Tile {
-    int t;             // kNoTile: none left
-    bool mine, whole, neg;
   };
   auto next = [&]() __attribute__((always_inline)) {
     while (visit == 0) {
-      if (64 * (grp + 1) >= end_tile) return Tile{kNoTile, false, false, false};
+      if (64 * (grp + 1) >= ntiles) return Tile{-1, 0, 0};
       look(++grp);
     }
+    if (left-- <= 0) return Tile{-1, 0, 0};
     const int i = __builtin_ctzll(visit);
     visit &= visit - 1;
-    return Tile{64 * grp + i, (bool)(mine >> i & 1), (bool)(whole >> i & 1), (bool)(neg >> i & 1)};
+    return Tile{64 * grp + i, __builtin_amdgcn_readlane(fl, i), __builtin_amdgcn_readlane(id, i)};
   };
 
   uint16_t* const stage = (wave < 2 ? K0 : wave < 4 ? K1 : wave < 6 ? V0 : V1) + (wave & 1) * 32 * D;
@@ -186,7 +177,7 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
   auto dma_v = [&](const Tile& t, uint16_t* buf) __attribute__((always_inline)) {
     const __amdgpu_buffer_rsrc_t rs = tile_rsrc(vbh, t.t);
     int g0 = vg0, g1 = vg1;
-    if (t.neg) {  // uniform: values of keys of negative documents arrive as zeros
+    if (t.zero()) {  // uniform: values of keys of negative documents arrive as zeros
       const int key = t.t * BN + vr;
       if (key >= c.Lk || c.s.k_doc[(size_t)b * c.Lk + min(key, c.Lk - 1)] < 0) g0 = g1 = 0x7ffffff0;
     }
@@ -209,8 +200,7 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
 #pragma unroll
   for (int mb = 0; mb < 4; ++mb) oacc[mb] = f32x16{};
   float mref = -INFINITY;  // the row's reference, log2 units
-  float nm = 0.f;          // -mref, 0 while unset
-  float sum0 = INFINITY;   // +inf until the row has a reference: forces the reset
+  float nm = kUnset;       // -mref
   float lsum = 0.f;        // this lane half's sum
   const float mul = a.sc.mul;
   const float slope = BIAS ? -c.s.slopes[h] * kLog2e : 0.f;
@@ -239,7 +229,7 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
     return tsum + odd;
   };
   auto softmax_blk = [&](f32x16& s, bf16x8 pop[2], float dist) __attribute__((always_inline)) {
-    float tsum = softmax_p(s, pop, sum0, dist);
+    float tsum = softmax_p(s, pop, 0.f, dist);
     if (__builtin_amdgcn_ballot_w64(!(tsum < kSumLimit)) != 0) {
       float m = logit(s[0], 0.f, dist, 0);
 #pragma unroll
@@ -253,8 +243,7 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
       mref = mnew;
-      nm = set ? -mnew : 0.f;
-      sum0 = set ? 0.f : INFINITY;
+      nm = set ? -mnew : kUnset;
       tsum = softmax_p(s, pop, 0.f, dist);
     }
     lsum += tsum;
@@ -273,36 +262,30 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
     }
   };
   // -inf for what the lane's row does not see of the tile
-  auto mask = [&](f32x16 s[2], int t) __attribute__((always_inline)) {
-    const int left = lim - t * BN - 4 * hi;
+  auto mask = [&](f32x16 s[2], const Tile& t, const int* ids) __attribute__((always_inline)) {
+    int to = t.mine() ? lim - t.t * BN - 4 * hi : 0;
+    if (docs && t.one() && qd != t.id) to = 0;
 #pragma unroll
     for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (32 * blk + 8 * (i >> 2) + (i & 3) >= left) s[blk][i] = -INFINITY;
-    if (docs) {
-      // ids past Lk: past the buffer's records (the limit has masked them)
-      const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc(
-          (void*)(c.s.k_doc + (size_t)b * c.Lk), (short)0, c.Lk * 4, kBufferFlags);
+        if (32 * blk + 8 * (i >> 2) + (i & 3) >= to) s[blk][i] = -INFINITY;
+    if (docs && !t.one()) {  // uniform
 #pragma unroll
       for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const u32x4 d = __builtin_amdgcn_raw_buffer_load_b128(rd, (t * BN + 32 * blk + 8 * g + 4 * hi) * 4, 0, 0);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if ((int)d[e] != qd) s[blk][4 * g + e] = -INFINITY;
+          const int4 d = *reinterpret_cast<const int4*>(ids + 32 * blk + 8 * g + 4 * hi);
+          if (d.x != qd) s[blk][4 * g] = -INFINITY;
+          if (d.y != qd) s[blk][4 * g + 1] = -INFINITY;
+          if (d.z != qd) s[blk][4 * g + 2] = -INFINITY;
+          if (d.w != qd) s[blk][4 * g + 3] = -INFINITY;
         }
     }
   };
-  auto softmax_pv = [&](f32x16 s[2], const uint16_t* vb, const Tile& t) __attribute__((always_inline)) {
+  auto softmax_pv = [&](f32x16 s[2], const uint16_t* vb, int t) __attribute__((always_inline)) {
     bf16x8 pop0[2], pop1[2];
-    if (CAP) {
-      cap16(s[0], a.sc.ku);
-      cap16(s[1], a.sc.ku);
-    }
-    if (!t.whole) mask(s, t.t);  // uniform
-    const float dist = BIAS ? (float)(bt.start + qrow - t.t * BN - 4 * hi) : 0.f;
+    const float dist = BIAS ? (float)(bt.start + qrow - t * BN - 4 * hi) : 0.f;
     softmax_blk(s[0], pop0, dist);
     pv_blk(vb, pop0, 0);
     softmax_blk(s[1], pop1, dist - 32.f);
@@ -352,13 +335,32 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
     if (a.lse && qlive && hi == 0) a.lse[orow + qrow] = lse2 * kLn2;
   };
 
-  Tile cur{kNoTile, false, false, false}, nxt = cur;
-  if (first_tile < end_tile) {
-    look(grp);
+  Tile cur{-1, 0, 0}, nxt = cur;
+  if (ntiles > 0) {
+    if (a.runs > 1) {  // this run's part of the tiles to visit
+      int n = ntiles;
+      if (docs) {
+        n = 0;
+        for (int g = 0; 64 * g < ntiles; ++g) {
+          look(g);
+          n += __builtin_popcountll(visit);
+        }
+      }
+      int skip = (int)((int64_t)n * run / a.runs);
+      left = (int)((int64_t)n * (run + 1) / a.runs) - skip;
+      look(0);
+      while (left > 0 && skip >= __builtin_popcountll(visit)) {
+        skip -= __builtin_popcountll(visit);
+        look(++grp);
+      }
+      for (; left > 0 && skip > 0; --skip) visit &= visit - 1;
+    } else {
+      look(0);
+    }
     cur = next();
     nxt = next();
   }
-  if (cur.t == kNoTile) {  // nothing to see
+  if (cur.t < 0) {  // nothing to see
     store_o();
     return;
   }
@@ -366,9 +368,16 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
   __builtin_amdgcn_s_waitcnt(0);  // this wave's query rows have landed
   take_q();
   __syncthreads();  // every wave has its queries out of the K/V buffers
+  // ids of a tile's keys, in LDS for the step that masks it
+  int kid = 0;
+  auto load_ids = [&](const Tile& t) __attribute__((always_inline)) {
+    if (docs && !t.one() && tid < BN) kid = c.s.k_doc[(size_t)b * c.Lk + min(t.t * BN + tid, c.Lk - 1)];
+  };
+  load_ids(cur);
   dma_k(cur.t, K0);
   dma_v(cur, V0);
-  if (nxt.t != kNoTile) dma_k(nxt.t, K1);
+  if (nxt.t >= 0) dma_k(nxt.t, K1);
+  if (docs && tid < BN) Kd[0][tid] = kid;
   __builtin_amdgcn_s_waitcnt(0);  // this wave's copies have landed in LDS
   __syncthreads();
   f32x16 sa[2], sb[2];
@@ -378,17 +387,31 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
   auto step = [&](auto parity, f32x16 scur[2], f32x16 snext[2]) __attribute__((always_inline)) {
     constexpr int P = decltype(parity)::value;
     const Tile aft = next();
-    if (aft.t != kNoTile) dma_k(aft.t, P ? K1 : K0);
-    if (nxt.t != kNoTile) {
+    if (aft.t >= 0) dma_k(aft.t, P ? K1 : K0);
+    if (nxt.t >= 0) {
+      load_ids(nxt);
       dma_v(nxt, P ? V0 : V1);
-      if (nxt.mine) qk(P ? K0 : K1, snext);
     }
-    if (cur.mine) softmax_pv(scur, P ? V1 : V0, cur);
+    const uint16_t* const kn = P ? K0 : K1;
+    const uint16_t* const vc = P ? V1 : V0;
+    // One stretch of code for the products of the next tile and the softmax of this
+    // one, so that they overlap: a wave that needs only one of the two (at the ends
+    // of what it sees) does the other on whatever is there, unseen.
+    if (cur.mine() || nxt.mine()) {
+      if (CAP) {
+        cap16(scur[0], a.sc.ku);
+        cap16(scur[1], a.sc.ku);
+      }
+      if (!(cur.mine() && cur.whole())) mask(scur, cur, Kd[P]);
+      qk(kn, snext);
+      softmax_pv(scur, vc, cur.t);
+    }
+    if (docs && !nxt.one() && tid < BN) Kd[1 - P][tid] = kid;
     cur = nxt;
     nxt = aft;
     __builtin_amdgcn_s_waitcnt(0);  // this wave's copies have landed
     __syncthreads();
-    return cur.t != kNoTile;
+    return cur.t >= 0;
   };
   while (step(std::integral_constant<int, 0>(), sa, sb) && step(std::integral_constant<int, 1>(), sb, sa)) {
   }
@@ -422,6 +445,59 @@ __global__ __launch_bounds__(256) void mod_ranges_kernel(RangeArgs a) {
   if ((lane & 31) == 0) {
     int2* const out = (isk ? a.kr : a.qr) + (size_t)w * 2 + (lane >> 5);
     *out = make_int2(lo, hi | (neg ? (int)0x80000000 : 0));
+  }
+}
+
+// The order in which the 256-row tiles of the queries (block 0 + first) or keys (1)
+// are handed out: most tiles of the other side to visit first.  Documents make
+// tiles of very different work; in their own order the last ones to start held
+// the launch up (five clips in 16380 tokens, 12 heads, forward: 683 us; sorted 371).  A wave
+// counts a tile's work, 64 tiles of the other side at a time; ranks by counting.
+constexpr size_t kOrderMost = 4096;
+struct OrderArgs {
+  ModCall c;
+  ModRanges r;
+  int nq, nk, first;
+  int32_t *oq, *ok;
+};
+__global__ __launch_bounds__(1024) void mod_order_kernel(OrderArgs a) {
+  __shared__ int work[kOrderMost];
+  const ModCall& c = a.c;
+  const bool isq = blockIdx.x + a.first == 0;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int tiles = isq ? a.nq : a.nk, n = c.B * tiles;
+  const int own_len = isq ? c.Lq : c.Lk, other_len = isq ? c.Lk : c.Lq;
+  const int own_r = (int)mod_ranges(own_len), other_r = (int)mod_ranges(other_len);
+  const int2* const own = isq ? a.r.q : a.r.k;
+  const int2* const other = isq ? a.r.k : a.r.q;
+  for (int i = wave; i < n; i += 16) {
+    const int b = i / tiles, t = i - b * tiles;
+    const Batch bt = batch_of(c, b);
+    Docs d{0x7fffffff, 0, false};
+    for (int j = 0; j < 8; ++j)
+      if (8 * t + j < own_r) d = mod::join(d, docs_of(own[(size_t)b * own_r + 8 * t + j]));
+    // the part of the other side that the limits leave: keys [0, to), queries [from, ..)
+    const int last = min((t + 1) * BM, own_len) - 1;
+    const int to = isq ? key_limit(bt, c.s.causal, bt.start + last) : other_len;
+    const int from = !isq && c.s.causal && t * BM >= bt.prefix ? max(t * BM - bt.start, 0) : 0;
+    int w = 0;
+    for (int o = 0; o < to; o += 4096) {
+      const int g = o / 64 + lane;
+      bool v = g * 64 < to && g * 64 + 63 >= from;
+      if (v) {
+        const int4 r = *reinterpret_cast<const int4*>(other + (size_t)b * other_r + 2 * g);
+        v = meet(d, mod::join(docs_of(make_int2(r.x, r.y)), docs_of(make_int2(r.z, r.w))));
+      }
+      w += __builtin_popcountll(__builtin_amdgcn_ballot_w64(v));
+    }
+    if (lane == 0) work[i] = w;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += 1024) {
+    const int w = work[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += work[j] > w || (work[j] == w && j < i);
+    (isq ? a.oq : a.ok)[rank] = i;
   }
 }
 
@@ -461,8 +537,8 @@ __global__ __launch_bounds__(256) void mod_join_kernel(JoinArgs a) {
 
 }  // namespace
 
-hipError_t launch_mod_ranges(const ModCall& c, float* ws, ModRanges* out, hipStream_t stream) {
-  *out = ModRanges{nullptr, nullptr};
+hipError_t launch_mod_ranges(const ModCall& c, float* ws, bool q_order, bool k_order, ModRanges* out, hipStream_t stream) {
+  *out = ModRanges{nullptr, nullptr, nullptr, nullptr};
   if (!c.s.k_doc) return hipSuccess;
   RangeArgs a;
   a.k = c.s.k_doc;
@@ -474,9 +550,24 @@ hipError_t launch_mod_ranges(const ModCall& c, float* ws, ModRanges* out, hipStr
   a.nq = (int)(mod_ranges(c.Lq) / 2);
   a.kr = reinterpret_cast<int2*>(ws);
   a.qr = a.kr + (size_t)c.B * mod_ranges(c.Lk);
-  *out = ModRanges{a.kr, a.qr};
+  out->k = a.kr;
+  out->q = a.qr;
   const unsigned waves = (unsigned)c.B * (unsigned)(a.nk + a.nq);
-  return launch_kernel(mod_ranges_kernel, (waves + 3) / 4, 256u, stream, a);
+  const hipError_t e = launch_kernel(mod_ranges_kernel, (waves + 3) / 4, 256u, stream, a);
+  OrderArgs o;
+  o.c = c;
+  o.r = *out;
+  o.nq = (int)mod_tiles(c.Lq);
+  o.nk = (int)mod_tiles(c.Lk);
+  o.oq = reinterpret_cast<int32_t*>(a.qr + (size_t)c.B * mod_ranges(c.Lq));
+  o.ok = o.oq + (size_t)c.B * o.nq;
+  q_order = q_order && (size_t)c.B * o.nq <= kOrderMost;
+  k_order = k_order && (size_t)c.B * o.nk <= kOrderMost;
+  if (e != hipSuccess || !(q_order || k_order)) return e;
+  o.first = q_order ? 0 : 1;
+  if (q_order) out->q_order = o.oq;
+  if (k_order) out->k_order = o.ok;
+  return launch_kernel(mod_order_kernel, (q_order && k_order) ? 2u : 1u, 1024u, stream, o);
 }
 
 namespace {
@@ -507,14 +598,17 @@ hipError_t launch_attn_mod_fwd(const ModFwd& f, hipStream_t stream) {
   a.v = f.v;
   a.o = f.o;
   a.lse = f.lse;
-  a.nqt = (c.Lq + BM - 1) / BM;
+  a.ntile = (c.Lq + BM - 1) / BM;
+  a.first_most = 0;
   a.runs = s.runs;
-  a.nwg = a.nqt * c.B * c.H * s.runs;
+  a.nwg = a.ntile * c.B * c.H * s.runs;
   a.kr = (int)mod_ranges(c.Lk);
   a.qr = (int)mod_ranges(c.Lq);
   a.po = s.runs > 1 ? f.ws + s.part : nullptr;
   a.pl = s.runs > 1 ? a.po + (size_t)s.runs * c.B * c.H * c.Lq * D : nullptr;
-  hipError_t e = launch_mod_ranges(c, f.ws, &a.r, stream);
+  // one round of workgroups needs no order
+  const int cus = device_cu_count();
+  hipError_t e = launch_mod_ranges(c, f.ws, !s.few && a.nwg > cus, false, &a.r, stream);
   if (e != hipSuccess) return e;
   if (s.few) return launch_mod_few(f, s, a.r, stream);
   const bool cap = c.s.cap > 0.f, bias = c.s.slopes != nullptr;

@@ -47,9 +47,12 @@ struct ModBwd {
 
 // ---- workspace: document ranges of every 32 tokens (keys, then queries; two
 // int32 a range, an even number of ranges a batch), then what a form adds.
-inline size_t mod_ranges(int L) { return ((size_t)L + 63) / 64 * 2; }
+// (With documents) also the order of the 256-row tiles, queries then keys.
+constexpr int kModRows = 256;
+__host__ __device__ inline size_t mod_ranges(int L) { return ((size_t)L + 63) / 64 * 2; }
+__host__ __device__ inline size_t mod_tiles(int L) { return ((size_t)L + kModRows - 1) / kModRows; }
 inline size_t mod_doc_floats(int B, int Lq, int Lk, bool docs) {
-  return docs ? (size_t)B * (mod_ranges(Lk) + mod_ranges(Lq)) * 2 : 0;
+  return docs ? (size_t)B * (mod_ranges(Lk) * 2 + mod_ranges(Lq) * 2 + mod_tiles(Lq) + mod_tiles(Lk)) : 0;
 }
 
 // ---- forward ----
@@ -57,7 +60,6 @@ inline size_t mod_doc_floats(int B, int Lq, int Lk, bool docs) {
 // Few rows (a group's query heads times the queries, at most kFewRows): the form
 // for single tokens (attn_mod_few.hip).  Otherwise tiles of 256 query rows, whose
 // keys may be cut into runs, one workgroup each, that a second launch joins.
-constexpr int kModRows = 256;
 constexpr int kModKeys = 64;
 constexpr int kFewRows = 32;
 
@@ -100,14 +102,16 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
     return r;
   }
   // 256-row workgroups, one a compute unit: 1.4 us a tile of 64 keys, 4 to start
-  // and end; the joining launch 4 us and its bytes.
+  // and end; the joining launch 4 us and its bytes.  How much of the keys a
+  // document leaves is not known here: a third is assumed, and a tile's keys are
+  // cut only where the tiles leave half of the compute units without one.
   const int64_t tiles = ((int64_t)Lk + kModKeys - 1) / kModKeys;
   const int64_t wgs = (int64_t)((Lq + kModRows - 1) / kModRows) * B * H;
   double best = 1e30;
   for (int s = 1; s <= 64 && s <= tiles; ++s) {
     const size_t need = r.part + (size_t)s * rows * 129;  // a run's rows: 128 outputs and a log-sum-exp each
-    if (s > 1 && need > max_floats) break;
-    const int64_t rounds = (wgs * s + cus - 1) / cus, per = (tiles + s - 1) / s;
+    if (s > 1 && (need > max_floats || (docs && wgs * s > cus))) break;
+    const int64_t rounds = (wgs * s + cus - 1) / cus, per = ((docs ? (tiles + 2) / 3 : tiles) + s - 1) / s;
     const double cost = rounds * (per * 1.4 + 4.0) + (s > 1 ? 4.0 + (double)s * rows * 1056 / 5e6 : 0.0);
     if (cost < best) {
       best = cost;
@@ -138,11 +142,11 @@ inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool doc
   r.part = up(r.least);
   if (B == 0 || H == 0 || Lq == 0 || Lk == 0) return r;
   const size_t run = 2 * (size_t)B * Lk * Hkv * 128;  // partial values of a run
-  const int64_t items = (int64_t)(H / Hkv) * ((Lq + 63) / 64), wgs = (int64_t)((Lk + 255) / 256) * B * Hkv;
+  const int64_t tiles = (Lq + 63) / 64, items = (int64_t)(H / Hkv) * (docs ? (tiles + 2) / 3 : tiles), wgs = (int64_t)((Lk + 255) / 256) * B * Hkv;
   double best = 1e30;
   for (int s = 1; s <= 32 && s <= items; ++s) {
     const size_t need = r.part + s * run;
-    if (s > 1 && (need > max_floats || s * run > ((size_t)96 << 20))) break;
+    if (s > 1 && (need > max_floats || s * run > ((size_t)96 << 20) || (docs && wgs * s > cus))) break;
     // in tiles' times (2 us): rounds x (tiles a run + start and end) + the launch and bytes of the sum
     const int64_t rounds = (wgs * s + cus - 1) / cus;
     const double cost = rounds * ((items + s - 1) / s + 2.0) + (s > 1 ? 3.0 + s * (run * 8 / 14e6) : 0.0);
@@ -160,9 +164,11 @@ __attribute__((weak)) hipError_t launch_attn_mod_bwd(const ModBwd& a, hipStream_
 
 // Between the attn_mod_*.hip files.
 struct ModRanges {
-  const int2 *k, *q;  // [B][mod_ranges(Lk)], [B][mod_ranges(Lq)], or null
+  const int2 *k, *q;              // [B][mod_ranges(Lk)], [B][mod_ranges(Lq)], or null
+  const int32_t *q_order, *k_order; // tiles b * mod_tiles + t of most work first, or null (in order)
 };
-hipError_t launch_mod_ranges(const ModCall& c, float* ws, ModRanges* out, hipStream_t stream);
+// Ranges (and, `order`: the tiles' orders) into ws.
+hipError_t launch_mod_ranges(const ModCall& c, float* ws, bool q_order, bool k_order, ModRanges* out, hipStream_t stream);
 hipError_t launch_mod_few(const ModFwd& a, const ModSplit& s, const ModRanges& r, hipStream_t stream);
 
 }  // namespace vidax

@@ -273,7 +273,7 @@ def test_runs_of_keys_are_joined(Lq, Lk):
     q, k, v = make(1, 2, 1, Lq, Lk, 27)
     s = masks("docs_valid_prefix", 1, Lq, Lk)
     need = vx.lib().vidax_attn_mod_fwd_workspace_floats(1, 2, 1, Lq, Lk, D, 1)
-    least = 2 * (2 * -(-Lk // 64) + 2 * -(-Lq // 64))
+    least = 4 * (-(-Lk // 64) + -(-Lq // 64)) + -(-Lk // 256) + -(-Lq // 256)
     assert need > least
     o, lse = check(q, k, v, what="runs", **s)
     o1, lse1 = check(q, k, v, what="one run", workspace=torch.empty(least, device="cuda"), **s)

@@ -10,6 +10,7 @@ there is no fallback implementation.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -412,24 +413,37 @@ def attn_fwd_naive(q, k, v, scale=None, kv_valid_len=None, rope: Rope | None = N
     return _attn("vidax_attn_fwd_naive", q, k, v, scale, kv_valid_len, rope, return_lse, out, stream)
 
 
-def _on(device, fn, *args):
-    """fn(*args) with that device current."""
-    import torch
-
-    if device.index == torch.cuda.current_device():
-        return fn(*args)
-    with torch.cuda.device(device):
-        return fn(*args)
+# The calls below are short enough on the device (5 us) for the binding to count:
+# plain addresses instead of pointer objects, the raw stream instead of a Stream.
 
 
 def _call(fn: str, device, stream, *args):
     """fn(*args, stream) with the tensors' device current and, by default, on that device's current stream."""
     import torch
 
-    s = torch.cuda.current_stream(device) if stream is None else stream
-    st = _on(device, getattr(lib(), fn), *args, ctypes.c_void_p(s.cuda_stream))
+    i = device.index
+    s = torch._C._cuda_getCurrentRawStream(i) if stream is None else stream.cuda_stream
+    f = getattr(_lib or lib(), fn)
+    if i == torch._C._cuda_getDevice():
+        st = f(*args, s)
+    else:
+        with torch.cuda.device(device):
+            st = f(*args, s)
     if st != VIDAX_OK:
         raise VidaxError(fn, st)
+
+
+@functools.lru_cache(maxsize=1024)
+def _floats(fn: str, device: int, *sizes) -> int:
+    """Workspace size by a function of the library (of the sizes and the device alone)."""
+    import torch
+
+    with torch.cuda.device(device):
+        return getattr(lib(), fn)(*sizes)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _check_dense(name, t, dtype, shape, device):
@@ -446,19 +460,20 @@ def _score_desc(score, q, Lk):
     """Descriptor of a Score for queries q [B, Lq, H, d] against Lk keys."""
     import torch
 
-    s = Score() if score is None else score
+    if score is None:
+        return ScoreDesc()
+    s, device, i32 = score, q.device, torch.int32
     B, Lq, H, _ = q.shape
     if (s.q_doc is None) != (s.k_doc is None):
         raise ValueError("q_doc and k_doc come together")
-    if s.slopes is not None:
-        _check_dense("slopes", s.slopes, torch.float32, (H,), q.device)
-    for n, shape in (("q_doc", (B, Lq)), ("k_doc", (B, Lk)), ("kv_valid_len", (B,)), ("prefix_len", (B,)),
-                     ("q_start", (B,))):
-        t = getattr(s, n)
+    d = ScoreDesc(s.causal, s.cap)
+    for n, t, dtype, shape in (("slopes", s.slopes, torch.float32, (H,)), ("q_doc", s.q_doc, i32, (B, Lq)),
+                               ("k_doc", s.k_doc, i32, (B, Lk)), ("kv_valid_len", s.kv_valid_len, i32, (B,)),
+                               ("prefix_len", s.prefix_len, i32, (B,)), ("q_start", s.q_start, i32, (B,))):
         if t is not None:
-            _check_dense(n, t, torch.int32, shape, q.device)
-    return ScoreDesc(int(s.causal), float(s.cap), *(None if t is None else t.data_ptr() for t in (
-        s.slopes, s.q_doc, s.k_doc, s.kv_valid_len, s.prefix_len, s.q_start)))
+            _check_dense(n, t, dtype, shape, device)
+            setattr(d, n, t.data_ptr())
+    return d
 
 
 def _check_mod_qkv(q, k, v):
@@ -499,10 +514,11 @@ def attn_mod_fwd(q, k, v, score: Score | None = None, scale=None, return_lse=Fal
     lse = torch.empty((B, H, Lq), dtype=torch.float32, device=q.device) if return_lse else None
     need = 0
     if workspace is None:
-        need = _on(q.device, lib().vidax_attn_mod_fwd_workspace_floats, B, H, Hkv, Lq, Lk, d, int(desc.k_doc is not None))
+        need = _floats("vidax_attn_mod_fwd_workspace_floats", q.device.index, B, H, Hkv, Lq, Lk, d, desc.k_doc is not None)
     ws = _workspace(workspace, need, q.device)
-    _call("vidax_attn_mod_fwd", q.device, stream, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), B, H, Hkv, Lq, Lk, d,
-          _SCALE_128 if scale is None else float(scale), ctypes.byref(desc), _ptr(ws), 0 if ws is None else ws.numel())
+    _call("vidax_attn_mod_fwd", q.device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _addr(lse), B, H,
+          Hkv, Lq, Lk, d, _SCALE_128 if scale is None else scale, ctypes.byref(desc), _addr(ws),
+          0 if ws is None else ws.numel())
     return (o, lse) if return_lse else o
 
 
@@ -528,11 +544,11 @@ def attn_mod_bwd(q, k, v, o, dout, lse, score: Score | None = None, scale=None, 
             _check_dense(n, t, ref.dtype, ref.shape, q.device)
     need = 0
     if workspace is None:
-        need = _on(q.device, lib().vidax_attn_mod_bwd_workspace_floats, B, H, Hkv, Lq, Lk, d, int(desc.k_doc is not None))
+        need = _floats("vidax_attn_mod_bwd_workspace_floats", q.device.index, B, H, Hkv, Lq, Lk, d, desc.k_doc is not None)
     ws = _workspace(workspace, need, q.device)
-    _call("vidax_attn_mod_bwd", q.device, stream, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(dout), _ptr(lse), _ptr(dq),
-          _ptr(dk), _ptr(dv), B, H, Hkv, Lq, Lk, d, _SCALE_128 if scale is None else float(scale), ctypes.byref(desc),
-          _ptr(ws), 0 if ws is None else ws.numel())
+    _call("vidax_attn_mod_bwd", q.device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), dout.data_ptr(),
+          lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, H, Hkv, Lq, Lk, d,
+          _SCALE_128 if scale is None else scale, ctypes.byref(desc), _addr(ws), 0 if ws is None else ws.numel())
     return dq, dk, dv
 
 
@@ -541,24 +557,25 @@ def attn_mod_bwd(q, k, v, o, dout, lse, score: Score | None = None, scale=None, 
 _NORMS = {None: 0, "layer": 1, "rms": 2}
 
 
-def _block_mod(name, t, B, L, C, device):
-    """(BlockMod, one row a token?) of a modulation [B, C], [B, 1, C] or [B, L, C]."""
+def _block_mod(name, m, t, B, L, C, device):
+    """Fills the BlockMod m from a modulation [B, C], [B, 1, C] or [B, L, C]; True: one row a token."""
     import torch
 
-    if t is None:
-        return BlockMod(None, 0, 0), None
-    if t.dtype != torch.float32 or t.device != device or (C > 1 and t.stride(-1) != 1):
+    shape, stride = t.shape, t.stride()
+    if t.dtype != torch.float32 or t.device != device or (C > 1 and stride[-1] != 1):
         raise ValueError(f"{name} must be a float32 tensor on {device} with dense channels")
-    if t.shape == (B, C):
-        return BlockMod(t.data_ptr(), t.stride(0) if B > 1 else 0, 0), False
-    if t.dim() != 3 or t.shape[0] != B or t.shape[1] not in (1, L) or t.shape[2] != C:
+    n = len(shape)
+    if not (n == 2 or (n == 3 and shape[1] in (1, L))) or shape[0] != B or shape[-1] != C:
         raise ValueError(f"{name} must be [B, C], [B, 1, C] or [B, L, C]")
-    token = t.shape[1] > 1
-    return BlockMod(t.data_ptr(), t.stride(0) if B > 1 else 0, t.stride(1) if token else 0), token
+    token = n == 3 and shape[1] > 1
+    m.p = t.data_ptr()
+    m.batch_stride = stride[0] if B > 1 else 0
+    m.token_stride = stride[1] if token else 0
+    return token
 
 
 def _block_desc(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha):
-    """(descriptor, gradients one row a token?)"""
+    """(descriptor, whether the modulations are one row a token: a set)"""
     import torch
 
     if x.dim() != 3 or not x.is_cuda or x.dtype not in (torch.bfloat16, torch.float32) or not x.is_contiguous():
@@ -566,16 +583,18 @@ def _block_desc(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alph
     if norm not in ("layer", "rms") or post not in _NORMS:
         raise ValueError("norm must be 'layer' or 'rms', post one of them or None")
     B, L, C = x.shape
+    device = x.device
     if y is not None:
-        _check_dense("y", y, torch.bfloat16, x.shape, x.device)
+        _check_dense("y", y, torch.bfloat16, x.shape, device)
+    d = BlockNormDesc(x.dtype == torch.float32, _NORMS[norm], _NORMS[post], 0, eps, alpha)
     for n, t in (("gain", gain), ("post_gain", post_gain)):
         if t is not None:
-            _check_dense(n, t, torch.float32, (C,), x.device)
-    mods = [_block_mod(n, t, B, L, C, x.device) for n, t in (("gate", gate), ("scale", scale), ("shift", shift))]
-    token = {f for _, f in mods if f is not None}
-    d = BlockNormDesc(x.dtype == torch.float32, _NORMS[norm], _NORMS[post], 0, float(eps), float(alpha),
-                      gain.data_ptr() if gain is not None else None,
-                      post_gain.data_ptr() if post_gain is not None else None, *(m for m, _ in mods))
+            _check_dense(n, t, torch.float32, (C,), device)
+            setattr(d, n, t.data_ptr())
+    token = set()
+    for n, t in (("gate", gate), ("scale", scale), ("shift", shift)):
+        if t is not None:
+            token.add(_block_mod(n, getattr(d, n), t, B, L, C, device))
     return d, token
 
 
@@ -605,7 +624,8 @@ def block_norm_fwd(x, y=None, gate=None, scale=None, shift=None, gain=None, post
             raise ValueError("out[0] may be None only where x' is x")
         _check_dense("out[1]", h, torch.bfloat16, x.shape, x.device)
     B, L, C = x.shape
-    _call("vidax_block_norm_fwd", x.device, stream, _ptr(x), _ptr(y), _ptr(xo), _ptr(h), B, L, C, ctypes.byref(d))
+    _call("vidax_block_norm_fwd", x.device, stream, x.data_ptr(), _addr(y), _addr(xo), h.data_ptr(), B, L, C,
+          ctypes.byref(d))
     return (x if xo is None else xo), h
 
 
@@ -639,8 +659,10 @@ def block_norm_bwd(dh, dx, x, y=None, gate=None, scale=None, shift=None, gain=No
             got[n] = torch.empty(t.shape, dtype=torch.float32, device=x.device)
     g = BlockNormGrads(*(got[n].data_ptr() if n in got else None for n, _ in BlockNormGrads._fields_))
     sums = (not d.per_token and len(token) > 0) or gain is not None or post_gain is not None
-    workspace = _workspace(workspace, lib().vidax_block_norm_bwd_workspace_floats(B, L, C) if sums else 0, x.device)
-    _call("vidax_block_norm_bwd", x.device, stream, _ptr(dh), _ptr(dx), _ptr(x), _ptr(y), _ptr(got["dx"]),
-          _ptr(got.get("dy")), ctypes.byref(g), _ptr(workspace), 0 if workspace is None else workspace.numel(), B, L, C,
-          ctypes.byref(d))
+    need = 0
+    if sums and workspace is None:
+        need = _floats("vidax_block_norm_bwd_workspace_floats", x.device.index, B, L, C)
+    ws = _workspace(workspace, need, x.device)
+    _call("vidax_block_norm_bwd", x.device, stream, dh.data_ptr(), _addr(dx), x.data_ptr(), _addr(y), got["dx"].data_ptr(),
+          _addr(got.get("dy")), ctypes.byref(g), _addr(ws), 0 if ws is None else ws.numel(), B, L, C, ctypes.byref(d))
     return got

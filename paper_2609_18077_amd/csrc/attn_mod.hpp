@@ -114,15 +114,15 @@ __device__ __forceinline__ bool same(const Docs& a, const Docs& b) {
 
 // Which 256-row tile t of (batch b, head h of `heads`) and which of its runs the
 // workgroup takes.  Neighbours in number go to different XCDs.
-//   Tiles of equal work: an XCD takes a stretch of a head's tiles, whose other
-// side then stays in its L2.
-//   Otherwise the most work first, all heads of a tile side by side: a late
-// start of a long tile would hold the launch up (16384 causal, 12 heads: 1172 us
-// with long and short tiles in turn, XCD by XCD; 845 so).
+//   Tiles of equal work, or one round of workgroups: an XCD takes a stretch of a
+// head's tiles, whose other side then stays in its L2.
+//   Otherwise (`sorted`) the most work first, all heads of a tile side by side: a
+// late start of a long tile would hold the launch up (16384 causal, 12 heads:
+// 1172 us with long and short tiles in turn, XCD by XCD; 842 so).
 template <typename A>
 __device__ __forceinline__ void place(const A& a, int heads, const int32_t* order, int& run, int& t, int& b, int& h) {
   const ModCall& c = a.c;
-  if (order || c.s.causal || c.s.kv_valid_len) {
+  if (a.sorted) {
     int i = blockIdx.x;
     run = i % a.runs;
     i /= a.runs;

@@ -42,7 +42,7 @@ struct BwdArgs {
   int kr, qr;         // ranges a batch
   int ntile, nwg;     // tiles of own rows a head, workgroups of the launched kernel
   int runs;           // key side: the stream is cut into runs, a workgroup each
-  int first_most;     // causal: the first tile of a head has the most work (else the last)
+  int sorted, first_most;  // see place(); causal: the first tile of a head has the most work (else the last)
   float* part;        // runs > 1: fp32 dK, dV of every run ([runs][B][Lk][Hkv][D], dV after dK)
 };
 
@@ -784,6 +784,7 @@ hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
   a.part = f.ws + s.part;
   a.kr = (int)mod_ranges(c.Lk);
   a.qr = (int)mod_ranges(c.Lq);
+  const bool uneven = c.s.k_doc || c.s.causal || c.s.kv_valid_len;
   const size_t qwg = mod_tiles(c.Lq) * c.B * c.H, kwg = mod_tiles(c.Lk) * c.B * c.Hkv * s.runs;
   hipError_t e = launch_mod_ranges(c, f.ws, qwg > (size_t)cus, kwg > (size_t)cus, &a.r, stream);
   if (e != hipSuccess) return e;
@@ -792,6 +793,7 @@ hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
     a.ntile = (c.Lq + BM - 1) / BM;
     a.nwg = a.ntile * c.B * c.H;
     a.runs = 1;
+    a.sorted = uneven && qwg > (size_t)cus;
     a.first_most = 0;
     const unsigned grid = (unsigned)a.nwg;
     e = cap ? (bias ? launch_kernel(mod_dq_kernel<true, true>, grid, (unsigned)NT, stream, a)
@@ -804,6 +806,7 @@ hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
     a.ntile = (c.Lk + BM - 1) / BM;
     a.nwg = a.ntile * c.B * c.Hkv * s.runs;
     a.runs = s.runs;
+    a.sorted = uneven && kwg > (size_t)cus;
     a.first_most = 1;
     const unsigned grid = (unsigned)a.nwg;
     e = cap ? (bias ? launch_kernel(mod_dkdv_kernel<true, true>, grid, (unsigned)NT, stream, a)

@@ -51,7 +51,7 @@ struct FwdArgs {
   float *po, *pl;  // partial outputs [runs][B][H][Lq][D] and log2-sum-exps [runs][B][H][Lq], or null
   ModRanges r;
   int ntile, nwg, runs;
-  int first_most;  // causal: the first tile of a head has the most work (else the last)
+  int sorted, first_most;  // see place(); causal: the first tile of a head has the most work (else the last)
   int kr, qr;      // document ranges a batch
 };
 
@@ -602,13 +602,12 @@ hipError_t launch_attn_mod_fwd(const ModFwd& f, hipStream_t stream) {
   a.first_most = 0;
   a.runs = s.runs;
   a.nwg = a.ntile * c.B * c.H * s.runs;
+  a.sorted = a.nwg > device_cu_count() && (c.s.k_doc || c.s.causal || c.s.kv_valid_len);
   a.kr = (int)mod_ranges(c.Lk);
   a.qr = (int)mod_ranges(c.Lq);
   a.po = s.runs > 1 ? f.ws + s.part : nullptr;
   a.pl = s.runs > 1 ? a.po + (size_t)s.runs * c.B * c.H * c.Lq * D : nullptr;
-  // one round of workgroups needs no order
-  const int cus = device_cu_count();
-  hipError_t e = launch_mod_ranges(c, f.ws, !s.few && a.nwg > cus, false, &a.r, stream);
+  hipError_t e = launch_mod_ranges(c, f.ws, !s.few && a.sorted, false, &a.r, stream);
   if (e != hipSuccess) return e;
   if (s.few) return launch_mod_few(f, s, a.r, stream);
   const bool cap = c.s.cap > 0.f, bias = c.s.slopes != nullptr;

@@ -18,8 +18,13 @@ constexpr int kStartLimit = 1 << 30;  // positions stay within +- 2^30 + L
 // log2 e, ku = |scale| / cap).
 struct Scores {
   float mul, ku;
+  float poly[5], limit; // capped, the forward's form of y (cap16_log2)
   uint32_t qxor, qand;  // applied to q's bf16 pairs: sign of scale, zero where it is 0
 };
+
+// tanh(u) = u (1 + k1 u^2 + ... + k4 u^8) up to 1.2e-7 of itself for |u| <= 1/2
+// (least squares on Chebyshev points).
+constexpr float kTanh[5] = {1.f, -3.333331048e-1f, 1.333051324e-1f, -5.339105427e-2f, 1.799921878e-2f};
 
 inline Scores make_scores(const ModCall& c) {
   Scores s;
@@ -28,38 +33,61 @@ inline Scores make_scores(const ModCall& c) {
   s.qand = a == 0.f ? 0u : 0xffffffffu;
   s.ku = c.s.cap > 0.f ? a / c.s.cap : 0.f;
   s.mul = c.s.cap > 0.f ? c.s.cap * kLog2e : a == 0.f ? 1.f : a * kLog2e;
+  // mul tanh(ku x) = x (p0 + p1 x^2 + ...) for |x| <= limit; never where a factor could overflow
+  float k = s.mul * s.ku;
+  for (int i = 0; i < 5; ++i, k *= s.ku * s.ku) s.poly[i] = kTanh[i] * k;
+  s.limit = s.ku == 0.f ? INFINITY : s.ku < 100.f ? 0.5f / s.ku : -1.f;
   return s;
 }
 
-// tanh of 16 products times ku, in place.  An odd polynomial of degree 9 where
-// the whole wave's block stays within 1/2 (its error there is 1.2e-7 of the value;
-// coefficients by least squares on Chebyshev points), else by the exponential,
-// whose absolute error of 1e-7 is then small against the block's largest score.
+// tanh of 16 products times ku, in place.  The odd polynomial where the whole
+// wave's block stays within 1/2, else the exponential, whose absolute error of 1e-7
+// is then small against the block's largest score.
 __device__ __forceinline__ float tanh_small(float u) {
   const float w = u * u;
-  float p = fmaf(w, 1.799921878e-2f, -5.339105427e-2f);
-  p = fmaf(w, p, 1.333051324e-1f);
-  p = fmaf(w, p, -3.333331048e-1f);
-  p = fmaf(w, p, 1.0f);
+  float p = fmaf(w, kTanh[4], kTanh[3]);
+  p = fmaf(w, p, kTanh[2]);
+  p = fmaf(w, p, kTanh[1]);
+  p = fmaf(w, p, kTanh[0]);
   return u * p;
 }
 __device__ __forceinline__ float tanh_any(float u) {
   const float e = __builtin_amdgcn_exp2f(u * (2.f * kLog2e));
   return fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f);
 }
-__device__ __forceinline__ void cap16(f32x16& s, float ku) {
+__device__ __forceinline__ float largest16(const f32x16& s) {
   float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    s[i] *= ku;
-    m = fmaxf(m, fabsf(s[i]));
-  }
-  if (__builtin_amdgcn_ballot_w64(!(m <= 0.5f)) == 0) {
+  for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(s[i]));
+  return m;
+}
+__device__ __forceinline__ void cap16(f32x16& s, float ku) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] *= ku;
+  if (__builtin_amdgcn_ballot_w64(!(largest16(s) <= 0.5f)) == 0) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = tanh_small(s[i]);
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = tanh_any(s[i]);
+  }
+}
+// The same as y = mul tanh(ku x), the factors folded into the polynomial: six
+// operations a score where tanh and its factors take eight.
+__device__ __forceinline__ void cap16_log2(f32x16& s, const Scores& c) {
+  if (__builtin_amdgcn_ballot_w64(!(largest16(s) <= c.limit)) == 0) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float w = s[i] * s[i];
+      float p = fmaf(w, c.poly[4], c.poly[3]);
+      p = fmaf(w, p, c.poly[2]);
+      p = fmaf(w, p, c.poly[1]);
+      p = fmaf(w, p, c.poly[0]);
+      s[i] *= p;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = c.mul * tanh_any(s[i] * c.ku);
   }
 }
 

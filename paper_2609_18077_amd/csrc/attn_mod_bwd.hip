@@ -41,9 +41,10 @@ struct BwdArgs {
   ModRanges r;
   int kr, qr;         // ranges a batch
   int ntile, nwg;     // tiles of own rows a head, workgroups of the launched kernel
-  int runs;           // key side: the stream is cut into runs, a workgroup each
+  int runs, quantum;  // key side: a stream of more than quantum tiles goes to several workgroups, runs at most
+  int32_t* counts;    // [B][tiles of keys]: how many
   int sorted, first_most;  // see place(); causal: the first tile of a head has the most work (else the last)
-  float* part;        // runs > 1: fp32 dK, dV of every run ([runs][B][Lk][Hkv][D], dV after dK)
+  float* part;        // fp32 dK, dV of every run of those tiles ([runs][B][Lk][Hkv][D], dV after dK)
 };
 
 // Rows 16 k2 .. + 15 of an accumulator as a bf16 B operand, in the accumulator's row order.
@@ -494,6 +495,19 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
     return Tile{64 * grp + i, __builtin_amdgcn_readlane(fl, i), __builtin_amdgcn_readlane(id, i)};
   };
 
+  // tiles to visit of a head, and into how many runs the stream is cut
+  int n = qa < qb ? qb - qa : 0;
+  if (docs && n > 0) {
+    n = 0;
+    for (int s = grp; 64 * s < qb; ++s) {
+      look(s);
+      n += __builtin_popcountll(visit);
+    }
+  }
+  const int cuts = max(1, min(a.runs, (int)(((int64_t)n * rep + a.quantum - 1) / a.quantum)));
+  if (run >= cuts) return;
+  if (run == 0 && hk == 0 && tid == 0) a.counts[b * a.ntile + kt] = cuts;
+
   f32x16 dk[4], dv[4];
 #pragma unroll
   for (int mb = 0; mb < 4; ++mb) dk[mb] = dv[mb] = f32x16{};
@@ -688,28 +702,18 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
   };
   Tile cur{-1, 0, 0}, nxt = cur;
   int cur_head = 0;
-  if (qa < qb) {
-    int n = qb - qa;  // tiles to visit of a head
-    if (docs) {
-      n = 0;
-      for (int s = grp; 64 * s < qb; ++s) {
-        look(s);
-        n += __builtin_popcountll(visit);
-      }
+  if (n > 0) {
+    const int64_t i0 = (int64_t)n * rep * run / cuts, i1 = (int64_t)n * rep * (run + 1) / cuts;
+    g = (int)(i0 / n);
+    left = (int)(i1 - i0);
+    int skip = (int)(i0 - (int64_t)g * n);
+    look(grp);
+    while (left > 0 && skip >= __builtin_popcountll(visit)) {
+      skip -= __builtin_popcountll(visit);
+      look(++grp);
     }
-    if (n > 0) {
-      const int64_t i0 = (int64_t)n * rep * run / a.runs, i1 = (int64_t)n * rep * (run + 1) / a.runs;
-      g = (int)(i0 / n);
-      left = (int)(i1 - i0);
-      int skip = (int)(i0 - (int64_t)g * n);
-      look(grp);
-      while (left > 0 && skip >= __builtin_popcountll(visit)) {
-        skip -= __builtin_popcountll(visit);
-        look(++grp);
-      }
-      for (; left > 0 && skip > 0; --skip) visit &= visit - 1;
-      cur = next();
-    }
+    for (; left > 0 && skip > 0; --skip) visit &= visit - 1;
+    cur = next();
   }
   if (cur.t >= 0) {
     copies(cur, Q0, O0);
@@ -738,21 +742,26 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
   if (cur.t >= 0)
     while (step(std::integral_constant<int, 0>()) && step(std::integral_constant<int, 1>())) {
     }
-  if (a.runs > 1) return partials_out();
+  if (cuts > 1) return partials_out();
   uint16_t* const area = KB + wave * 32 * D;  // read by this wave alone
   rows_out(a.dk, dk, c.scale, area);
   rows_out(a.dv, dv, 1.f, area);
 }
 
-// dK = scale * sum of the runs' partials, dV = their sum: 8 values a thread.
+// dK = scale * sum of the runs' partials, dV = their sum, for the tiles that were
+// cut: 8 values a thread.
 __global__ __launch_bounds__(256) void mod_reduce_kernel(BwdArgs a) {
-  const size_t n = (size_t)a.c.B * a.c.Lk * a.c.Hkv * D, groups = n / 8;
+  const int row = a.c.Hkv * D;  // values of a key
+  const size_t n = (size_t)a.c.B * a.c.Lk * row, groups = n / 8;
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < 2 * groups; i += (size_t)gridDim.x * 256) {
     const bool isk = i < groups;
-    const size_t e = (isk ? i : i - groups) * 8;
+    const size_t e = (isk ? i : i - groups) * 8, key = e / row;
+    const int b = (int)(key / a.c.Lk), cuts = a.counts[b * a.ntile + (int)(key - (size_t)b * a.c.Lk) / BM];
+    if (cuts == 1) continue;  // written whole
     const float* src = a.part + (isk ? 0 : (size_t)a.runs * n) + e;
     float4 x0 = make_float4(0.f, 0.f, 0.f, 0.f), x1 = x0;
-    for (int r = 0; r < a.runs; ++r) {
+#pragma unroll 4
+    for (int r = 0; r < cuts; ++r) {
       const float4 u = *reinterpret_cast<const float4*>(src + (size_t)r * n);
       const float4 v = *reinterpret_cast<const float4*>(src + (size_t)r * n + 4);
       x0.x += u.x; x0.y += u.y; x0.z += u.z; x0.w += u.w;
@@ -773,7 +782,8 @@ __global__ __launch_bounds__(256) void mod_reduce_kernel(BwdArgs a) {
 hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
   const ModCall& c = f.c;
   const int cus = device_cu_count();
-  const ModBwdSplit s = mod_bwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr, cus, f.ws_floats);
+  const ModBwdSplit s = mod_bwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr, c.s.causal != 0, cus,
+                                      f.ws_floats);
   BwdArgs a;
   a.c = c;
   a.sc = make_scores(c);
@@ -781,7 +791,9 @@ hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
   a.dq = f.dq; a.dk = f.dk; a.dv = f.dv;
   a.delta = f.ws + s.delta;
   a.empty = reinterpret_cast<int32_t*>(f.ws + s.empty);
+  a.counts = reinterpret_cast<int32_t*>(f.ws + s.counts);
   a.part = f.ws + s.part;
+  a.quantum = s.quantum;
   a.kr = (int)mod_ranges(c.Lk);
   a.qr = (int)mod_ranges(c.Lq);
   const bool uneven = c.s.k_doc || c.s.causal || c.s.kv_valid_len;

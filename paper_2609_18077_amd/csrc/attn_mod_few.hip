@@ -171,7 +171,6 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_mod_few_kernel(FewArgs a) {
   for (int mb = 0; mb < 4; ++mb) oacc[mb] = f32x16{};
   float mref = -INFINITY, lsum = 0.f;
   const float slope = c.s.slopes && live ? -c.s.slopes[hr] * kLog2e : 0.f;
-  const bool cap = a.sc.ku != 0.f;
 
   Tile cur{-1, false, false}, nxt = cur;
   if (t0 < t1) {
@@ -202,13 +201,13 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_mod_few_kernel(FewArgs a) {
     f32x16 s = f32x16{};
 #pragma unroll
     for (int st = 0; st < 8; ++st) s = mfma32(read_row(kb, off.row, st), qop[st], s);
-    if (cap) cap16(s, a.sc.ku);  // uniform
+    if (a.c.s.cap > 0.f) cap16_log2(s, a.sc);  // uniform
     // y; -inf for what the row does not see
     const float dist = (float)(pos - t.t * BN - 4 * hi);
     const int left = lim - t.t * BN - 4 * hi;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      s[e] *= a.sc.mul;
+      if (a.c.s.cap == 0.f) s[e] *= a.sc.mul;
       if (c.s.slopes) s[e] = fmaf(slope, fabsf(dist - (float)(8 * (e >> 2) + (e & 3))), s[e]);
     }
     if (!t.whole) {  // uniform

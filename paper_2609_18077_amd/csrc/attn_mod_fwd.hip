@@ -207,7 +207,7 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
 
   // y + n of element i of a block; dist: position minus the block's first key of this lane half
   auto logit = [&](float s, float n, float dist, int i) __attribute__((always_inline)) {
-    float y = fmaf(s, mul, n);
+    float y = CAP ? s + n : fmaf(s, mul, n);
     if (BIAS) y = fmaf(slope, fabsf(dist - (float)(8 * (i >> 2) + (i & 3))), y);
     return y;
   };
@@ -399,8 +399,8 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
     // of what it sees) does the other on whatever is there, unseen.
     if (cur.mine() || nxt.mine()) {
       if (CAP) {
-        cap16(scur[0], a.sc.ku);
-        cap16(scur[1], a.sc.ku);
+        cap16_log2(scur[0], a.sc);
+        cap16_log2(scur[1], a.sc);
       }
       if (!(cur.mine() && cur.whole())) mask(scur, cur, Kd[P]);
       qk(kn, snext);

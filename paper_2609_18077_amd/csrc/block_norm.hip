@@ -22,7 +22,10 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kMaxWaves = 8;  // of a workgroup: a lane may then hold 256 registers
+// Waves of a workgroup: 8, so that a lane may hold 256 registers; 10 where it
+// needs few (168 then): a row of 5120 channels with one chunk a lane.
+constexpr int kMaxWaves = 10;
+constexpr int kWaves = 8;
 
 // Eight values of the stream (bf16: 16 bytes, fp32: 32) as they lie in memory.
 template <bool F32>
@@ -201,7 +204,7 @@ struct FwdArgs {
 
 // TOKEN: the modulations change from row to row
 template <bool F32, int NC, bool TOKEN>
-__global__ __launch_bounds__(64 * kMaxWaves) void block_norm_fwd_kernel(FwdArgs f) {
+__global__ __launch_bounds__(64 * kWaves) void block_norm_fwd_kernel(FwdArgs f) {
   __shared__ __attribute__((aligned(16))) float slots[2][kMaxWaves][4];
   const BlockNorm& n = f.a.n;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -336,7 +339,7 @@ struct BwdArgs {
 
 // TOKEN: every token has modulations (and gradients of them) of its own
 template <bool F32, int NC, bool TOKEN>
-__global__ __launch_bounds__(64 * kMaxWaves) void block_norm_bwd_kernel(BwdArgs f) {
+__global__ __launch_bounds__(64 * (NC == 1 ? kMaxWaves : kWaves)) void block_norm_bwd_kernel(BwdArgs f) {
   __shared__ __attribute__((aligned(16))) float slots[2][kMaxWaves][4];
   __shared__ __attribute__((aligned(16))) float cols[8 * 64 * 8];  // column sums between the groups
   const BlockNorm& n = f.a.n;
@@ -596,7 +599,7 @@ void fwd_row(int C, int& chunks, int& waves) {
   int best = 1 << 30;
   for (int nc = 4; nc >= 1; --nc) {
     const int w = (n + 64 * nc - 1) / (64 * nc);
-    if (w > kMaxWaves || (nc == 4 && n <= 64 * 3 * kMaxWaves)) continue;
+    if (w > kWaves || (nc == 4 && n <= 64 * 3 * kWaves)) continue;
     const int idle = w * 64 * nc - n;
     if (idle < best) {
       best = idle;

@@ -50,9 +50,10 @@ struct BlockNormBwd {
 // Shape of the backward: workgroups of `groups` groups of `waves` waves, a row
 // each at a time; a workgroup takes `rows` consecutive rows of a batch (a run),
 // `runs` of them a batch.
-//   One chunk of 8 channels a lane up to C = 4096, two up to 8192, four beyond:
-// a lane holds about ten values a channel (row, gradients, modulations, column
-// sums).
+//   One chunk of 8 channels a lane up to C = 5120 (ten waves), two up to 8192, four
+// beyond: a lane holds about ten values a channel (row, gradients, modulations,
+// column sums).  7803 tokens x 5120, fp32, modulations a token: two chunks, five
+// waves 475 us; one chunk, ten waves XXX.
 //   About 512 runs in all: the column sums of a run are written once and read
 // once by the reduction, 12 bytes a channel each way (512 runs against 65536
 // rows: 1.6 % of the bytes); at least 4 rows a group, so that the loads of one
@@ -63,7 +64,7 @@ struct BlockShape {
 inline BlockShape block_bwd_shape(int B, int L, int C) {
   BlockShape s;
   const int n = C / 8;
-  s.chunks = n > 1024 ? 4 : n > 512 ? 2 : 1;
+  s.chunks = n > 1024 ? 4 : n > 640 ? 2 : 1;
   s.waves = (n + 64 * s.chunks - 1) / (64 * s.chunks);
   s.groups = s.waves >= 8 ? 1 : 8 / s.waves;
   const int64_t want = B > 0 ? (512 + B - 1) / B : 1;  // runs a batch

@@ -124,36 +124,68 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
 
 // ---- backward ----
 //
-// D, the flags of rows that see nothing, and where the key side has few
-// workgroups the fp32 partial dK and dV of its runs.
+// D, the flags of rows that see nothing, and the key side's partial sums.  A
+// workgroup of the key side streams the query tiles (64 rows) that may see its 256
+// keys, for every query head of its group.  Tiles of more than `quantum` of these
+// are given to ceil(stream / quantum) workgroups (`runs` at most) whose fp32 dK and
+// dV a further launch adds.  Chosen is the least time, in units of one tile's (4
+// us): rounds of equal workgroups, or of unequal ones, the longest first, the mean
+// load or the longest of them; 2 to start and end a workgroup; 2 for the further launch; the
+// partial sums written and read, 20 MB in a tile's time.  (2 x 2049 causal, 16 heads
+// on 4, cap and bias: three runs of every tile 205 + 10 us, eight at most XXX.)
 struct ModBwdSplit {
-  int runs;
-  size_t delta, empty, part;  // first values of these in the workspace (document ranges at 0)
-  size_t least, floats;       // values of the workspace: for one run, for `runs`
+  int runs, quantum;
+  size_t delta, empty, counts, part;  // first values of these in the workspace (document ranges at 0)
+  size_t least, floats;               // values of the workspace: for one run, for `runs`
 };
 
-inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, int cus, size_t max_floats) {
+inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, bool causal, int cus, size_t max_floats) {
   auto up = [](size_t x) { return (x + 63) / 64 * 64; };
   ModBwdSplit r;
   r.runs = 1;
+  r.quantum = 1 << 30;
   r.delta = up(mod_doc_floats(B, Lq, Lk, docs));
   r.empty = up(r.delta + (size_t)B * H * Lq);
-  r.least = r.floats = r.empty + (size_t)B * mod_ranges(Lq);
+  r.counts = r.empty + (size_t)B * mod_ranges(Lq);
+  r.least = r.floats = r.counts + (size_t)B * mod_tiles(Lk);
   r.part = up(r.least);
   if (B == 0 || H == 0 || Lq == 0 || Lk == 0) return r;
+  const int rep = H / Hkv, qt = (Lq + 63) / 64, kt = (int)mod_tiles(Lk);
+  const int64_t heads = (int64_t)B * Hkv;
+  // tiles of the stream of key tile t: how much a document leaves is not known here (a third is taken)
+  auto stream = [&](int t) {
+    const int64_t first = causal ? (int64_t)t * kModRows - (Lk - Lq) : 0;
+    int64_t n = first > 0 ? qt - first / 64 : qt;
+    if (n < 0) n = 0;
+    return rep * (docs ? (n + 2) / 3 : n);
+  };
+  const int64_t longest = stream(0);
   const size_t run = 2 * (size_t)B * Lk * Hkv * 128;  // partial values of a run
-  const int64_t tiles = (Lq + 63) / 64, items = (int64_t)(H / Hkv) * (docs ? (tiles + 2) / 3 : tiles), wgs = (int64_t)((Lk + 255) / 256) * B * Hkv;
   double best = 1e30;
-  for (int s = 1; s <= 32 && s <= items; ++s) {
+  for (int s = 1; s <= 16 && s <= longest; ++s) {
     const size_t need = r.part + s * run;
-    if (s > 1 && (need > max_floats || s * run > ((size_t)96 << 20) || (docs && wgs * s > cus))) break;
-    // in tiles' times (2 us): rounds x (tiles a run + start and end) + the launch and bytes of the sum
-    const int64_t rounds = (wgs * s + cus - 1) / cus;
-    const double cost = rounds * ((items + s - 1) / s + 2.0) + (s > 1 ? 3.0 + s * (run * 8 / 14e6) : 0.0);
+    if (s > 1 && (need > max_floats || s * run > ((size_t)96 << 20))) break;
+    const int64_t q = (longest + s - 1) / s;
+    int64_t total = 0, wgs = 0, partial = 0;
+    for (int t = 0; t < kt; ++t) {
+      const int64_t n = stream(t), w = n > q ? (n + q - 1) / q : 1;
+      total += n;
+      wgs += w;
+      if (w > 1) partial += w;
+    }
+    total *= heads;
+    wgs *= heads;
+    partial *= heads;
+    const double mean = 1.05 * (double)(total + 2 * wgs) / cus;
+    const double load = !causal && !docs ? (double)((wgs + cus - 1) / cus) * (q + 2) : mean > q + 2 ? mean : q + 2.0;
+    const double cost = load + (s > 1 ? 2.0 + partial * (2.0 * 2 * kModRows * 128 * 4 / 20e6) : 0.0);
     if (cost < best) {
       best = cost;
       r.runs = s;
-      if (s > 1) r.floats = need;
+      if (s > 1) {
+        r.quantum = (int)q;
+        r.floats = need;
+      }
     }
   }
   return r;

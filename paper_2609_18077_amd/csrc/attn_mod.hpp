@@ -151,19 +151,20 @@ template <typename A>
 __device__ __forceinline__ void place(const A& a, int heads, const int32_t* order, int& run, int& t, int& b, int& h) {
   const ModCall& c = a.c;
   if (a.sorted) {
-    int i = blockIdx.x;
-    run = i % a.runs;
-    i /= a.runs;
+    // run by run: run r is there for the first so many tiles (a.in_run)
+    const int n = order ? heads : c.B * heads, i = blockIdx.x / n, bh = blockIdx.x - i * n;
+    int x = i;
+    run = 0;
+    while (run + 1 < a.runs && x >= a.in_run[run]) x -= a.in_run[run++];
     if (order) {
-      h = i % heads;
-      const int x = __builtin_amdgcn_readfirstlane(order[i / heads]);
-      b = x / a.ntile;
-      t = x - b * a.ntile;
+      const int y = __builtin_amdgcn_readfirstlane(order[x]);
+      b = y / a.ntile;
+      t = y - b * a.ntile;
+      h = bh;
     } else {
-      const int n = c.B * heads, bh = i % n;
       b = bh / heads;
       h = bh - b * heads;
-      t = a.first_most ? i / n : a.ntile - 1 - i / n;
+      t = a.first_most ? x : a.ntile - 1 - x;
     }
     return;
   }

@@ -42,6 +42,7 @@ struct BwdArgs {
   int kr, qr;         // ranges a batch
   int ntile, nwg;     // tiles of own rows a head, workgroups of the launched kernel
   int runs, quantum;  // key side: a stream of more than quantum tiles goes to several workgroups, runs at most
+  int in_run[kMostRuns];   // see place()
   int32_t* counts;    // [B][tiles of keys]: how many
   int sorted, first_most;  // see place(); causal: the first tile of a head has the most work (else the last)
   float* part;        // fp32 dK, dV of every run of those tiles ([runs][B][Lk][Hkv][D], dV after dK)
@@ -796,6 +797,7 @@ hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
   a.quantum = s.quantum;
   a.kr = (int)mod_ranges(c.Lk);
   a.qr = (int)mod_ranges(c.Lq);
+  const bool docs = c.s.k_doc != nullptr;
   const bool uneven = c.s.k_doc || c.s.causal || c.s.kv_valid_len;
   const size_t qwg = mod_tiles(c.Lq) * c.B * c.H, kwg = mod_tiles(c.Lk) * c.B * c.Hkv * s.runs;
   hipError_t e = launch_mod_ranges(c, f.ws, qwg > (size_t)cus, kwg > (size_t)cus, &a.r, stream);
@@ -805,6 +807,7 @@ hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
     a.ntile = (c.Lq + BM - 1) / BM;
     a.nwg = a.ntile * c.B * c.H;
     a.runs = 1;
+    a.in_run[0] = a.r.q_order ? a.ntile * c.B : a.ntile;
     a.sorted = uneven && qwg > (size_t)cus;
     a.first_most = 0;
     const unsigned grid = (unsigned)a.nwg;
@@ -816,9 +819,22 @@ hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
   }
   if (c.Lk > 0) {
     a.ntile = (c.Lk + BM - 1) / BM;
-    a.nwg = a.ntile * c.B * c.Hkv * s.runs;
     a.runs = s.runs;
-    a.sorted = uneven && kwg > (size_t)cus;
+    // Workgroups that would find no part of their tile's stream are not launched
+    // where the host knows: with them between the others, some shader engines got
+    // more workgroups than compute units (2 x 2049 causal, 16 heads on 4: 256
+    // workgroups that stream at most 22 tiles 148 us; XXX without).
+    const bool known = !docs && !c.s.kv_valid_len && !c.s.prefix_len && !c.s.q_start;
+    int tiles = 0;
+    for (int r = 0; r < s.runs; ++r) {
+      int n = a.ntile;
+      if (known)
+        while (n > 0 && r > 0 && mod_stream(n - 1, c.H / c.Hkv, c.Lq, c.Lk, c.s.causal) <= (int64_t)r * s.quantum) --n;
+      a.in_run[r] = a.r.k_order ? n * c.B : n;
+      tiles += n;
+    }
+    a.nwg = tiles * c.B * c.Hkv;
+    a.sorted = uneven && (kwg > (size_t)cus || s.runs > 1);
     a.first_most = 1;
     const unsigned grid = (unsigned)a.nwg;
     e = cap ? (bias ? launch_kernel(mod_dkdv_kernel<true, true>, grid, (unsigned)NT, stream, a)

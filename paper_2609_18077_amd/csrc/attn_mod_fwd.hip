@@ -51,6 +51,7 @@ struct FwdArgs {
   float *po, *pl;  // partial outputs [runs][B][H][Lq][D] and log2-sum-exps [runs][B][H][Lq], or null
   ModRanges r;
   int ntile, nwg, runs;
+  int in_run[kMostRuns];   // see place()
   int sorted, first_most;  // see place(); causal: the first tile of a head has the most work (else the last)
   int kr, qr;      // document ranges a batch
 };
@@ -588,7 +589,7 @@ hipError_t launch_mod_join(const ModFwd& f, const ModSplit& s, hipStream_t strea
 
 hipError_t launch_attn_mod_fwd(const ModFwd& f, hipStream_t stream) {
   const ModCall& c = f.c;
-  const ModSplit s = mod_fwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr,
+  const ModSplit s = mod_fwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr, c.s.causal != 0,
                                    c.s.kv_valid_len || c.s.q_start, device_cu_count(), f.ws_floats);
   FwdArgs a;
   a.c = c;
@@ -610,6 +611,7 @@ hipError_t launch_attn_mod_fwd(const ModFwd& f, hipStream_t stream) {
   hipError_t e = launch_mod_ranges(c, f.ws, !s.few && a.sorted, false, &a.r, stream);
   if (e != hipSuccess) return e;
   if (s.few) return launch_mod_few(f, s, a.r, stream);
+  for (int r = 0; r < kMostRuns; ++r) a.in_run[r] = a.r.q_order ? a.ntile * c.B : a.ntile;
   const bool cap = c.s.cap > 0.f, bias = c.s.slopes != nullptr;
   e = cap ? (bias ? launch_kernel(attn_mod_fwd_kernel<true, true>, (unsigned)a.nwg, (unsigned)NT, stream, a)
                   : launch_kernel(attn_mod_fwd_kernel<true, false>, (unsigned)a.nwg, (unsigned)NT, stream, a))

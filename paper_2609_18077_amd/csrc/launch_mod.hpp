@@ -62,6 +62,7 @@ inline size_t mod_doc_floats(int B, int Lq, int Lk, bool docs) {
 // keys may be cut into runs, one workgroup each, that a second launch joins.
 constexpr int kModKeys = 64;
 constexpr int kFewRows = 32;
+constexpr int kMostRuns = 16;
 
 struct ModSplit {
   bool few;
@@ -71,7 +72,8 @@ struct ModSplit {
   size_t floats;  // values of the workspace
 };
 
-inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, bool lengths, int cus, size_t max_floats) {
+inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, bool causal, bool lengths, int cus,
+                              size_t max_floats) {
   ModSplit r;
   r.runs = 1;
   r.units = 0;
@@ -101,18 +103,31 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
     }
     return r;
   }
-  // 256-row workgroups, one a compute unit: 1.4 us a tile of 64 keys, 4 to start
-  // and end; the joining launch 4 us and its bytes.  How much of the keys a
-  // document leaves is not known here: a third is assumed, and a tile's keys are
-  // cut only where the tiles leave half of the compute units without one.
-  const int64_t tiles = ((int64_t)Lk + kModKeys - 1) / kModKeys;
-  const int64_t wgs = (int64_t)((Lq + kModRows - 1) / kModRows) * B * H;
+  // 256-row workgroups, one a compute unit, 2 us a tile of 64 keys.  Equal ones run
+  // in rounds; unequal ones (causal, documents), the longest first, end with the
+  // mean load or the longest of them.  4 us to start and end; the joining launch 4
+  // us and the runs' bytes at 5 TB/s.  How much of the keys a document leaves is not
+  // known here: a third is assumed, and a tile's keys are cut only where the tiles
+  // leave half of the compute units without one.
+  const int64_t tiles = ((int64_t)Lk + kModKeys - 1) / kModKeys, qt = (int64_t)mod_tiles(Lq);
+  const int64_t wgs = qt * B * H;
+  int64_t total = tiles * qt;  // of a head
+  if (causal) {
+    total = 0;
+    for (int64_t t = 0; t < qt; ++t) {
+      const int64_t last = (int64_t)Lk - Lq + ((t + 1) * kModRows < Lq ? (t + 1) * kModRows : Lq);  // keys seen by the last row
+      total += last <= 0 ? 0 : last >= Lk ? tiles : (last + kModKeys - 1) / kModKeys;
+    }
+  }
+  if (docs) total = (total + 2) / 3;
   double best = 1e30;
-  for (int s = 1; s <= 64 && s <= tiles; ++s) {
+  for (int s = 1; s <= kMostRuns && s <= tiles; ++s) {
     const size_t need = r.part + (size_t)s * rows * 129;  // a run's rows: 128 outputs and a log-sum-exp each
     if (s > 1 && (need > max_floats || (docs && wgs * s > cus))) break;
-    const int64_t rounds = (wgs * s + cus - 1) / cus, per = ((docs ? (tiles + 2) / 3 : tiles) + s - 1) / s;
-    const double cost = rounds * (per * 1.4 + 4.0) + (s > 1 ? 4.0 + (double)s * rows * 1056 / 5e6 : 0.0);
+    const int64_t rounds = (wgs * s + cus - 1) / cus;
+    const double per = (double)(docs ? (tiles + 2) / 3 : tiles) / s, mean = 1.05 * (double)total * B * H / cus;
+    const double load = docs || causal ? (mean > per ? mean : per) : rounds * (double)((tiles + s - 1) / s);
+    const double cost = load * 2.0 + rounds * 4.0 + (s > 1 ? 4.0 + (double)s * rows * 1056 / 5e6 : 0.0);
     if (cost < best) {
       best = cost;
       r.runs = s;
@@ -129,8 +144,8 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
 // keys, for every query head of its group.  Tiles of more than `quantum` of these
 // are given to ceil(stream / quantum) workgroups (`runs` at most) whose fp32 dK and
 // dV a further launch adds.  Chosen is the least time, in units of one tile's (4
-// us): rounds of equal workgroups, or of unequal ones, the longest first, the mean
-// load or the longest of them; 2 to start and end a workgroup; 2 for the further launch; the
+// us): rounds of equal workgroups; one round of unequal ones, or the mean load and
+// half a run where they are more; 2 to start and end a workgroup; 2 for the further launch; the
 // partial sums written and read, 20 MB in a tile's time.  (2 x 2049 causal, 16 heads
 // on 4, cap and bias: three runs of every tile 205 + 10 us, eight at most XXX.)
 struct ModBwdSplit {
@@ -138,6 +153,13 @@ struct ModBwdSplit {
   size_t delta, empty, counts, part;  // first values of these in the workspace (document ranges at 0)
   size_t least, floats;               // values of the workspace: for one run, for `runs`
 };
+
+// Tiles of the stream of key tile t, where queries stand at their default positions.
+inline int64_t mod_stream(int t, int rep, int Lq, int Lk, bool causal) {
+  const int64_t qt = (Lq + 63) / 64, first = causal ? (int64_t)t * kModRows - (Lk - Lq) : 0;
+  const int64_t n = first > 0 ? qt - first / 64 : qt;
+  return n > 0 ? rep * n : 0;
+}
 
 inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, bool causal, int cus, size_t max_floats) {
   auto up = [](size_t x) { return (x + 63) / 64 * 64; };
@@ -150,22 +172,20 @@ inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool doc
   r.least = r.floats = r.counts + (size_t)B * mod_tiles(Lk);
   r.part = up(r.least);
   if (B == 0 || H == 0 || Lq == 0 || Lk == 0) return r;
-  const int rep = H / Hkv, qt = (Lq + 63) / 64, kt = (int)mod_tiles(Lk);
+  const int kt = (int)mod_tiles(Lk);
   const int64_t heads = (int64_t)B * Hkv;
-  // tiles of the stream of key tile t: how much a document leaves is not known here (a third is taken)
+  // how much of a stream a document leaves is not known here: a third is taken
   auto stream = [&](int t) {
-    const int64_t first = causal ? (int64_t)t * kModRows - (Lk - Lq) : 0;
-    int64_t n = first > 0 ? qt - first / 64 : qt;
-    if (n < 0) n = 0;
-    return rep * (docs ? (n + 2) / 3 : n);
+    const int64_t n = mod_stream(t, H / Hkv, Lq, Lk, causal);
+    return docs ? (n + 2) / 3 : n;
   };
   const int64_t longest = stream(0);
   const size_t run = 2 * (size_t)B * Lk * Hkv * 128;  // partial values of a run
   double best = 1e30;
-  for (int s = 1; s <= 16 && s <= longest; ++s) {
+  auto consider = [&](int64_t q) {  // runs of at most q tiles
+    const int s = (int)((longest + q - 1) / q);
     const size_t need = r.part + s * run;
-    if (s > 1 && (need > max_floats || s * run > ((size_t)96 << 20))) break;
-    const int64_t q = (longest + s - 1) / s;
+    if (s > 1 && (s > kMostRuns || need > max_floats || s * run > ((size_t)96 << 20))) return;
     int64_t total = 0, wgs = 0, partial = 0;
     for (int t = 0; t < kt; ++t) {
       const int64_t n = stream(t), w = n > q ? (n + q - 1) / q : 1;
@@ -176,18 +196,30 @@ inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool doc
     total *= heads;
     wgs *= heads;
     partial *= heads;
-    const double mean = 1.05 * (double)(total + 2 * wgs) / cus;
-    const double load = !causal && !docs ? (double)((wgs + cus - 1) / cus) * (q + 2) : mean > q + 2 ? mean : q + 2.0;
-    const double cost = load + (s > 1 ? 2.0 + partial * (2.0 * 2 * kModRows * 128 * 4 / 20e6) : 0.0);
+    const int64_t rounds = (wgs + cus - 1) / cus;
+    const double load = (!causal && !docs) || rounds == 1 ? (double)rounds * (q + 2)
+                                                           : (double)(total + 2 * wgs) / cus + 0.5 * total / wgs;
+    const double cost = (load > q + 2 ? load : q + 2) + (s > 1 ? 2.0 + partial * (2.0 * 2 * kModRows * 128 * 4 / 20e6) : 0.0);
     if (cost < best) {
       best = cost;
       r.runs = s;
-      if (s > 1) {
-        r.quantum = (int)q;
-        r.floats = need;
-      }
+      r.quantum = s > 1 ? (int)q : 1 << 30;
+      r.floats = s > 1 ? need : r.least;
     }
+  };
+  if (longest == 0) return r;
+  consider(longest);
+  for (int s = 2; s <= kMostRuns && s <= longest; ++s) consider((longest + s - 1) / s);
+  // and the shortest runs that one round has room for
+  int64_t lo = 1, hi = longest;
+  while (lo < hi) {
+    const int64_t q = (lo + hi) / 2;
+    int64_t wgs = 0;
+    for (int t = 0; t < kt; ++t) wgs += stream(t) > q ? (stream(t) + q - 1) / q : 1;
+    if (wgs * heads <= cus) hi = q;
+    else lo = q + 1;
   }
+  consider(lo);
   return r;
 }
 

@@ -530,7 +530,10 @@ size_t vidax_attn_mod_fwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, in
   vidax::ModCall c;
   Buf s[6];
   if (mod_common(B, H, Hkv, Lq, Lk, d, 1.0f, nullptr, &c, s) != VIDAX_OK || B == 0 || H == 0 || Lq == 0) return 0;
-  return vidax::mod_fwd_split(B, H, Hkv, Lq, Lk, docs != 0 && Lk > 0, true, vidax::device_cu_count(), SIZE_MAX).floats;
+  const int cus = vidax::device_cu_count();
+  const size_t x = vidax::mod_fwd_split(B, H, Hkv, Lq, Lk, docs != 0 && Lk > 0, false, true, cus, SIZE_MAX).floats;
+  const size_t y = vidax::mod_fwd_split(B, H, Hkv, Lq, Lk, docs != 0 && Lk > 0, true, true, cus, SIZE_MAX).floats;
+  return x > y ? x : y;  // (causal or not)
 }
 
 vidax_status vidax_block_norm_fwd(const void* x, const void* y, void* xo, void* h, int32_t B, int32_t L, int32_t C,

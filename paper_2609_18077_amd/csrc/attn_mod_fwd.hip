@@ -58,7 +58,7 @@ struct FwdArgs {
 
 // CAP, BIAS: the scores' modifiers.
 template <bool CAP, bool BIAS>
-__global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
+__device__ __forceinline__ void fwd_body(const FwdArgs& a) {
   __shared__ __attribute__((aligned(16))) uint16_t K0[TILE], K1[TILE], V0[TILE], V1[TILE];
   __shared__ __attribute__((aligned(16))) int Kd[2][BN];  // ids of the tiles' keys, where they differ
 
@@ -212,55 +212,84 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
     if (BIAS) y = fmaf(slope, fabsf(dist - (float)(8 * (i >> 2) + (i & 3))), y);
     return y;
   };
-  auto softmax_p = [&](const f32x16& s, bf16x8 pop[2], float tsum, float dist) __attribute__((always_inline)) {
-    float odd = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      uint32_t pw[4];
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(logit(s[8 * ks + e], nm, dist, 8 * ks + e));
-        const float p1 = __builtin_amdgcn_exp2f(logit(s[8 * ks + e + 1], nm, dist, 8 * ks + e + 1));
-        pw[e >> 1] = pack_bf16x2(p0, p1);  // one rounding of the weights: 2^-9 of each, independent
-        tsum += p0;
-        odd += p1;
-      }
-      pop[ks] = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
-    }
-    return tsum + odd;
+  // P of elements i, i + 1 of a block (one rounding of the weights, 2^-9 of each,
+  // independent; the sum adds them before it)
+  auto exps = [&](const f32x16& s, int i, float dist, uint32_t pw[8], float& sum) __attribute__((always_inline)) {
+    const float p0 = __builtin_amdgcn_exp2f(logit(s[i], nm, dist, i));
+    const float p1 = __builtin_amdgcn_exp2f(logit(s[i + 1], nm, dist, i + 1));
+    pw[i >> 1] = pack_bf16x2(p0, p1);
+    sum += p0;
+    sum += p1;
   };
-  auto softmax_blk = [&](f32x16& s, bf16x8 pop[2], float dist) __attribute__((always_inline)) {
-    float tsum = softmax_p(s, pop, 0.f, dist);
-    if (__builtin_amdgcn_ballot_w64(!(tsum < kSumLimit)) != 0) {
-      float m = logit(s[0], 0.f, dist, 0);
+  // The block's sum is not below 2^64 for some row: new references, the output and
+  // sum rescaled, the block's weights formed again
+  auto reset = [&](const f32x16& s, float dist, uint32_t pw[8], float& sum) __attribute__((always_inline)) {
+    float m = logit(s[0], 0.f, dist, 0);
 #pragma unroll
-      for (int i = 1; i < 16; ++i) m = fmaxf(m, logit(s[i], 0.f, dist, i));
-      const float mnew = fmaxf(mref, wave_half_max(m));
-      const bool set = mnew > -INFINITY;
-      const float alpha = set ? __builtin_amdgcn_exp2f(mref - mnew) : 1.f;
-      lsum *= alpha;
+    for (int i = 1; i < 16; ++i) m = fmaxf(m, logit(s[i], 0.f, dist, i));
+    const float mnew = fmaxf(mref, wave_half_max(m));
+    const bool set = mnew > -INFINITY;
+    const float alpha = set ? __builtin_amdgcn_exp2f(mref - mnew) : 1.f;
+    lsum *= alpha;
 #pragma unroll
-      for (int mb = 0; mb < 4; ++mb)
+    for (int mb = 0; mb < 4; ++mb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
-      mref = mnew;
-      nm = set ? -mnew : kUnset;
-      tsum = softmax_p(s, pop, 0.f, dist);
-    }
-    lsum += tsum;
+      for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
+    mref = mnew;
+    nm = set ? -mnew : kUnset;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) exps(s, i, dist, pw, sum);
   };
-  auto pv_blk = [&](const uint16_t* vb, const bf16x8 pop[2], int blk) __attribute__((always_inline)) {
-#pragma unroll
-    for (int k2 = 0; k2 < 2; ++k2) {
-      const int ks = 2 * blk + k2;
-#pragma unroll
-      for (int mb = 0; mb < 4; ++mb) {
-        const i16x4 lo = lds_read_tr16(vb + (4 * ks + mb) * BLK + voff);
-        const i16x4 hi4 = lds_read_tr16(vb + (4 * ks + mb) * BLK + BLK / 2 + voff);
-        const bf16x8 vop = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
-        oacc[mb] = mfma32(vop, pop[k2], oacc[mb]);
+  // The scores of the next tile (K in kb) and the softmax and PV of this one (V in
+  // vb), hand-scheduled: a slot a product, each also issuing the operand reads of
+  // the product three slots on and its share of the exponentials.
+  auto products = [&](f32x16 s[2], f32x16 sn[2], const uint16_t* kb, const uint16_t* vb, int t) __attribute__((always_inline)) {
+    const float dist = BIAS ? (float)(bt.start + qrow - t * BN - 4 * hi) : 0.f;
+    bf16x8 op[32];
+    auto read_op = [&](auto N) __attribute__((always_inline)) {
+      constexpr int n = decltype(N)::value;
+      if constexpr (n < 16) {
+        op[n] = *reinterpret_cast<const bf16x8*>(kb + n * BLK + koff);
+      } else if constexpr (n < 32) {
+        const i16x4 lo = lds_read_tr16(vb + (n - 16) * BLK + voff);
+        const i16x4 up = lds_read_tr16(vb + (n - 16) * BLK + BLK / 2 + voff);
+        op[n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
       }
-    }
+    };
+    uint32_t pw[2][8];
+    float sum[2] = {0.f, 0.f};
+    auto p_op = [&](int blk, int k2) __attribute__((always_inline)) {
+      return __builtin_bit_cast(bf16x8, make_uint4(pw[blk][4 * k2], pw[blk][4 * k2 + 1], pw[blk][4 * k2 + 2], pw[blk][4 * k2 + 3]));
+    };
+    for_slots<3>(read_op);
+    SLOT();
+    for_slots<16>([&](auto N) __attribute__((always_inline)) {  // scores; exponentials of block 0
+      constexpr int n = decltype(N)::value;
+      sn[n & 1] = mfma32(op[n], qreg[n >> 1], n < 2 ? f32x16{} : sn[n & 1]);
+      read_op(std::integral_constant<int, n + 3>());
+      if constexpr ((n & 1) == 0) exps(s[0], n, dist, pw[0], sum[0]);
+      SLOT();
+    });
+    if (__builtin_amdgcn_ballot_w64(!(sum[0] < kSumLimit)) != 0) reset(s[0], dist, pw[0], sum[0]);
+    lsum += sum[0];
+    SLOT();
+    for_slots<8>([&](auto N) __attribute__((always_inline)) {  // PV of block 0; exponentials of block 1
+      constexpr int n = decltype(N)::value;
+      oacc[n & 3] = mfma32(op[16 + n], p_op(0, n >> 2), oacc[n & 3]);
+      read_op(std::integral_constant<int, n + 19>());
+      exps(s[1], 2 * n, dist - 32.f, pw[1], sum[1]);
+      SLOT();
+    });
+    if (__builtin_amdgcn_ballot_w64(!(sum[1] < kSumLimit)) != 0) reset(s[1], dist - 32.f, pw[1], sum[1]);
+    lsum += sum[1];
+    SLOT();
+    for_slots<8>([&](auto N) __attribute__((always_inline)) {  // PV of block 1
+      constexpr int n = decltype(N)::value;
+      oacc[n & 3] = mfma32(op[24 + n], p_op(1, n >> 2), oacc[n & 3]);
+      read_op(std::integral_constant<int, n + 27>());
+      SLOT();
+    });
   };
   // -inf for what the lane's row does not see of the tile
   auto mask = [&](f32x16 s[2], const Tile& t, const int* ids) __attribute__((always_inline)) {
@@ -284,15 +313,6 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
         }
     }
   };
-  auto softmax_pv = [&](f32x16 s[2], const uint16_t* vb, int t) __attribute__((always_inline)) {
-    bf16x8 pop0[2], pop1[2];
-    const float dist = BIAS ? (float)(bt.start + qrow - t * BN - 4 * hi) : 0.f;
-    softmax_blk(s[0], pop0, dist);
-    pv_blk(vb, pop0, 0);
-    softmax_blk(s[1], pop1, dist - 32.f);
-    pv_blk(vb, pop1, 1);
-  };
-
   // ---- output, whole rows through the staging area; empty rows: o = 0, lse = -inf
   const size_t nrow = (size_t)c.B * c.H * c.Lq, orow = ((size_t)b * c.H + h) * c.Lq;
   auto store_o = [&]() __attribute__((always_inline)) {
@@ -381,35 +401,32 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
   if (docs && tid < BN) Kd[0][tid] = kid;
   __builtin_amdgcn_s_waitcnt(0);  // this wave's copies have landed in LDS
   __syncthreads();
+  Tile aft = next();  // (known a step ahead: its keys are the first thing a step copies)
   f32x16 sa[2], sb[2];
   qk(K0, sa);
   __syncthreads();  // the first step refills K0
   // Step on the tile `cur` (parity of its buffers at compile time); false after the last
   auto step = [&](auto parity, f32x16 scur[2], f32x16 snext[2]) __attribute__((always_inline)) {
     constexpr int P = decltype(parity)::value;
-    const Tile aft = next();
     if (aft.t >= 0) dma_k(aft.t, P ? K1 : K0);
     if (nxt.t >= 0) {
       load_ids(nxt);
       dma_v(nxt, P ? V0 : V1);
     }
-    const uint16_t* const kn = P ? K0 : K1;
-    const uint16_t* const vc = P ? V1 : V0;
-    // One stretch of code for the products of the next tile and the softmax of this
-    // one, so that they overlap: a wave that needs only one of the two (at the ends
-    // of what it sees) does the other on whatever is there, unseen.
+    // A wave that needs only the products of the next tile or the softmax of this one
+    // (at the ends of what it sees) does the other on whatever is there, unseen.
     if (cur.mine() || nxt.mine()) {
       if (CAP) {
         cap16_log2(scur[0], a.sc);
         cap16_log2(scur[1], a.sc);
       }
       if (!(cur.mine() && cur.whole())) mask(scur, cur, Kd[P]);
-      qk(kn, snext);
-      softmax_pv(scur, vc, cur.t);
+      products(scur, snext, P ? K0 : K1, P ? V1 : V0, cur.t);
     }
     if (docs && !nxt.one() && tid < BN) Kd[1 - P][tid] = kid;
     cur = nxt;
     nxt = aft;
+    aft = next();
     __builtin_amdgcn_s_waitcnt(0);  // this wave's copies have landed
     __syncthreads();
     return cur.t >= 0;
@@ -417,6 +434,11 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
   while (step(std::integral_constant<int, 0>(), sa, sb) && step(std::integral_constant<int, 1>(), sb, sa)) {
   }
   store_o();
+}
+
+template <bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
+  fwd_body<CAP, BIAS>(a);
 }
 
 // Ranges of document ids of every 32 tokens: a wave takes 64 tokens of a batch.

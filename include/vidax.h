@@ -367,7 +367,7 @@ size_t vidax_attn_mod_fwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, in
  *              the query stream into runs that work side by side, their fp32 sums
  *              added in a further launch (at most 384 MiB); with fewer it takes the
  *              runs that fit; VIDAX_ERR_INVALID_ARG below what one run needs,
- *              B H Lq + B (2 ceil(Lq / 64) + ceil(Lk / 256)) + 192 values and, with
+ *              2 B H Lq + B (2 ceil(Lq / 64) + ceil(Lk / 256)) + 256 values and, with
  *              documents, those of the forward more.
  * Same call, same bits: no atomics.  Products on bf16 inputs (P and ds rounded to
  * bf16) with fp32 accumulation.  Pointers, sizes and overlap as for the forward

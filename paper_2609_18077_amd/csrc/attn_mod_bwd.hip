@@ -36,7 +36,7 @@ struct BwdArgs {
   const uint16_t *q, *k, *v, *o, *dout;
   const float* lse;
   uint16_t *dq, *dk, *dv;
-  float* delta;       // [B, H, Lq]
+  float *delta, *nlse;  // [B, H, Lq]: -D, -lse log2 e (-inf for rows that see nothing)
   int32_t* empty;     // [B][qr]: whether a row of these 32 sees nothing
   ModRanges r;
   int kr, qr;         // ranges a batch
@@ -87,6 +87,13 @@ __device__ __forceinline__ void each_hidden(int from, int to, const int* ids, in
       if (d.w != own) hide(4 * g + 3);
     }
   }
+}
+// The 4-byte values of 64-row tile t (of L rows at base; zero behind) into LDS, one wave.
+template <typename T>
+__device__ __forceinline__ void copy_row(const T* base, int t, int L, T* dst, int lane) {
+  const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+      (void*)(base + (size_t)t * BN), (short)0, __builtin_amdgcn_readfirstlane(min(L - t * BN, BN) * 4), kBufferFlags);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)dst, 4, lane * 4, 0, 0, 0);
 }
 // 64-row tile `t` of rows [0, limit) of a buffer: later rows read as zero.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const uint16_t* base, int t, int limit, int tok) {
@@ -232,7 +239,10 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
       for (int p = 0; p < 4; ++p) sum[p & 1] = dot2(xw[p], yw[p], sum[p & 1]);
     }
     dl = wave_half_sum(sum[0] + sum[1]);
-    if (qlive && hi == 0) a.delta[lrow] = dl;
+    if (qlive && hi == 0) {
+      a.delta[lrow] = -dl;
+      a.nlse[lrow] = -lse2;
+    }
     const uint64_t bad = __builtin_amdgcn_ballot_w64(qlive && none);
     if (h == 0 && lane == 0 && wrow < c.Lq) a.empty[(size_t)b * a.qr + (wrow >> 5)] = bad != 0;
   }
@@ -255,7 +265,8 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
   const uint16_t* const kbh = a.k + (size_t)b * c.Lk * ktok + (size_t)hk * D;
   const uint16_t* const vbh = a.v + (size_t)b * c.Lk * ktok + (size_t)hk * D;
   // the wave's copies 2 wave, 2 wave + 1 of a tile (4 rows each)
-  auto copies = [&](const Tile& t, uint16_t* kb, uint16_t* vb) __attribute__((always_inline)) {
+  auto copies = [&](const Tile& t, uint16_t* kb, uint16_t* vb, int* ids) __attribute__((always_inline)) {
+    if (docs && !t.one() && wave == 0) copy_row(c.s.k_doc + (size_t)b * c.Lk, t.t, c.Lk, ids, lane);
     const __amdgpu_buffer_rsrc_t rk = tile_rsrc(kbh, t.t, gmax, ktok), rv = tile_rsrc(vbh, t.t, gmax, ktok);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -269,14 +280,7 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_ptr)(vb + (2 * wave + u) * 512), 16, g, 0, 0, 0);
     }
   };
-  // ids of a tile's keys, with the copies; into LDS at the end of the step
-  int kid = 0;
-  auto load_ids = [&](const Tile& t) __attribute__((always_inline)) {
-    if (docs && !t.one() && tid < BN) kid = c.s.k_doc[(size_t)b * c.Lk + min(t.t * BN + tid, c.Lk - 1)];
-  };
-  load_ids(cur);
-  copies(cur, K0, V0);
-  if (docs && tid < BN) Kd[0][tid] = kid;
+  copies(cur, K0, V0, Kd[0]);
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
 
@@ -390,12 +394,8 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
     const uint16_t* const kt = P ? K1 : K0;
     const uint16_t* const vt = P ? V1 : V0;
     nxt = next();
-    if (nxt.t >= 0) {
-      load_ids(nxt);
-      copies(nxt, P ? K0 : K1, P ? V0 : V1);
-    }
+    if (nxt.t >= 0) copies(nxt, P ? K0 : K1, P ? V0 : V1, Kd[1 - P]);
     if (cur.mine()) products(cur, kt, vt, Kd[P]);
-    if (docs && !nxt.one() && tid < BN) Kd[1 - P][tid] = kid;
     cur = nxt;
     __builtin_amdgcn_s_waitcnt(0);  // this wave's copies have landed
     __syncthreads();
@@ -573,9 +573,8 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
     }
   }
   const size_t qbase = (size_t)b * c.Lq * qtok;
-  float lrow = INFINITY, drow = 0.f;
-  int qid = 0;
-  auto copies = [&](const Tile& t, uint16_t* qs, uint16_t* os) __attribute__((always_inline)) {
+  // (rows past Lq: zeros everywhere, which add nothing)
+  auto copies = [&](const Tile& t, uint16_t* qs, uint16_t* os, int buf) __attribute__((always_inline)) {
     const size_t hoff = qbase + (size_t)(hk * rep + head) * D;
     const size_t lbase = ((size_t)b * c.H + hk * rep + head) * c.Lq;
     const __amdgpu_buffer_rsrc_t rq = tile_rsrc(a.q + hoff, t.t, c.Lq, qtok), ro = tile_rsrc(a.dout + hoff, t.t, c.Lq, qtok);
@@ -590,20 +589,9 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_ptr)(qs + (2 * wave + u) * 512), 16, off, 0, 0, 0);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(ro, (lds_ptr)(os + (2 * wave + u) * 512), 16, off, 0, 0, 0);
     }
-    if (tid < BN) {
-      const int r = t.t * BN + tid;
-      lrow = r < c.Lq ? a.lse[lbase + r] : INFINITY;
-      drow = r < c.Lq ? a.delta[lbase + r] : 0.f;
-      if (lrow == -INFINITY) lrow = INFINITY;  // P = 0
-      if (docs && !t.one()) qid = c.s.q_doc[(size_t)b * c.Lq + min(r, c.Lq - 1)];
-    }
-  };
-  auto put_rows = [&](int buf) __attribute__((always_inline)) {
-    if (tid < BN) {
-      Lt[buf][tid] = -lrow * kLog2e;
-      Dt[buf][tid] = -drow;
-      if (docs) Qd[buf][tid] = qid;
-    }
+    if (wave == 0) copy_row(a.nlse + lbase, t.t, c.Lq, Lt[buf], lane);
+    if (wave == 1) copy_row(a.delta + lbase, t.t, c.Lq, Dt[buf], lane);
+    if (wave == 2 && docs && !t.one()) copy_row(c.s.q_doc + (size_t)b * c.Lq, t.t, c.Lq, Qd[buf], lane);
   };
   const RowOffsets off = row_offsets(lane);
   const float mul = a.sc.mul, ku = a.sc.ku;
@@ -717,8 +705,7 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
     cur = next();
   }
   if (cur.t >= 0) {
-    copies(cur, Q0, O0);
-    put_rows(0);
+    copies(cur, Q0, O0, 0);
   }
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
@@ -728,14 +715,13 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
     const uint16_t* const ot = P ? O1 : O0;
     cur_head = head;
     nxt = next();
-    if (nxt.t >= 0) copies(nxt, P ? Q0 : Q1, P ? O0 : O1);
+    if (nxt.t >= 0) copies(nxt, P ? Q0 : Q1, P ? O0 : O1, 1 - P);
     if (cur.mine()) {
       const float slope = BIAS ? -c.s.slopes[hk * rep + cur_head] * kLog2e : 0.f;
 #pragma unroll
       for (int blk = 0; blk < 2; ++blk) block(blk, par, cur, qt, ot, slope);
     }
     cur = nxt;
-    if (nxt.t >= 0) put_rows(1 - P);
     __builtin_amdgcn_s_waitcnt(0);  // this wave's copies have landed
     __syncthreads();
     return cur.t >= 0;
@@ -791,6 +777,7 @@ hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
   a.q = f.q; a.k = f.k; a.v = f.v; a.o = f.o; a.dout = f.dout; a.lse = f.lse;
   a.dq = f.dq; a.dk = f.dk; a.dv = f.dv;
   a.delta = f.ws + s.delta;
+  a.nlse = f.ws + s.nlse;
   a.empty = reinterpret_cast<int32_t*>(f.ws + s.empty);
   a.counts = reinterpret_cast<int32_t*>(f.ws + s.counts);
   a.part = f.ws + s.part;

@@ -390,15 +390,17 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a) {
   take_q();
   __syncthreads();  // every wave has its queries out of the K/V buffers
   // ids of a tile's keys, in LDS for the step that masks it
-  int kid = 0;
-  auto load_ids = [&](const Tile& t) __attribute__((always_inline)) {
-    if (docs && !t.one() && tid < BN) kid = c.s.k_doc[(size_t)b * c.Lk + min(t.t * BN + tid, c.Lk - 1)];
+  auto dma_ids = [&](const Tile& t, int* dst) __attribute__((always_inline)) {
+    if (!docs || t.one() || wave != 0) return;
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(c.s.k_doc + (size_t)b * c.Lk + t.t * BN), (short)0,
+        __builtin_amdgcn_readfirstlane(min(c.Lk - t.t * BN, BN) * 4), kBufferFlags);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)dst, 4, lane * 4, 0, 0, 0);
   };
-  load_ids(cur);
+  dma_ids(cur, Kd[0]);
   dma_k(cur.t, K0);
   dma_v(cur, V0);
   if (nxt.t >= 0) dma_k(nxt.t, K1);
-  if (docs && tid < BN) Kd[0][tid] = kid;
   __builtin_amdgcn_s_waitcnt(0);  // this wave's copies have landed in LDS
   __syncthreads();
   Tile aft = next();  // (known a step ahead: its keys are the first thing a step copies)
@@ -410,7 +412,7 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a) {
     constexpr int P = decltype(parity)::value;
     if (aft.t >= 0) dma_k(aft.t, P ? K1 : K0);
     if (nxt.t >= 0) {
-      load_ids(nxt);
+      dma_ids(nxt, Kd[1 - P]);
       dma_v(nxt, P ? V0 : V1);
     }
     // A wave that needs only the products of the next tile or the softmax of this one
@@ -423,7 +425,6 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a) {
       if (!(cur.mine() && cur.whole())) mask(scur, cur, Kd[P]);
       products(scur, snext, P ? K0 : K1, P ? V1 : V0, cur.t);
     }
-    if (docs && !nxt.one() && tid < BN) Kd[1 - P][tid] = kid;
     cur = nxt;
     nxt = aft;
     aft = next();

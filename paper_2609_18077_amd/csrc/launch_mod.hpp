@@ -139,7 +139,8 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
 
 // ---- backward ----
 //
-// D, the flags of rows that see nothing, and the key side's partial sums.  A
+// D and the log-sum-exps as the key side takes them, the flags of rows that see
+// nothing, and the key side's partial sums.  A
 // workgroup of the key side streams the query tiles (64 rows) that may see its 256
 // keys, for every query head of its group.  Tiles of more than `quantum` of these
 // are given to ceil(stream / quantum) workgroups (`runs` at most) whose fp32 dK and
@@ -150,7 +151,7 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
 // on 4, cap and bias: three runs of every tile 205 + 10 us, eight at most XXX.)
 struct ModBwdSplit {
   int runs, quantum;
-  size_t delta, empty, counts, part;  // first values of these in the workspace (document ranges at 0)
+  size_t delta, nlse, empty, counts, part;  // first values of these in the workspace (document ranges at 0)
   size_t least, floats;               // values of the workspace: for one run, for `runs`
 };
 
@@ -167,7 +168,8 @@ inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool doc
   r.runs = 1;
   r.quantum = 1 << 30;
   r.delta = up(mod_doc_floats(B, Lq, Lk, docs));
-  r.empty = up(r.delta + (size_t)B * H * Lq);
+  r.nlse = up(r.delta + (size_t)B * H * Lq);
+  r.empty = up(r.nlse + (size_t)B * H * Lq);
   r.counts = r.empty + (size_t)B * mod_ranges(Lq);
   r.least = r.floats = r.counts + (size_t)B * mod_tiles(Lk);
   r.part = up(r.least);

@@ -109,7 +109,7 @@ def test_runs_of_queries_are_added_up(Lq, Lk, Hkv):
     q, k, v = make(B, H, Hkv, Lq, Lk, 27)
     s = masks("docs_valid_prefix", B, Lq, Lk)
     need = vx.lib().vidax_attn_mod_bwd_workspace_floats(B, H, Hkv, Lq, Lk, D, 1)
-    most = B * H * Lq + B * (2 * -(-Lq // 64) + -(-Lk // 256)) + 192 + B * (4 * (-(-Lk // 64) + -(-Lq // 64)) + -(-Lk // 256) + -(-Lq // 256))
+    most = 2 * B * H * Lq + B * (2 * -(-Lq // 64) + -(-Lk // 256)) + 256 + B * (4 * (-(-Lk // 64) + -(-Lq // 64)) + -(-Lk // 256) + -(-Lq // 256))
     assert need > most  # several runs
     o, lse, dout, got = check(q, k, v, what="runs", **s)
     ws = torch.empty(most, device="cuda")

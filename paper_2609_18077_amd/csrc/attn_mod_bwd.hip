@@ -810,7 +810,7 @@ hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
     // Workgroups that would find no part of their tile's stream are not launched
     // where the host knows: with them between the others, some shader engines got
     // more workgroups than compute units (2 x 2049 causal, 16 heads on 4: 256
-    // workgroups that stream at most 22 tiles 148 us; XXX without).
+    // workgroups that stream at most 22 tiles 148 us; 91 without).
     const bool known = !docs && !c.s.kv_valid_len && !c.s.prefix_len && !c.s.q_start;
     int tiles = 0;
     for (int r = 0; r < s.runs; ++r) {

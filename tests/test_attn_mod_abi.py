@@ -1,0 +1,216 @@
+"""Refusals of attention with score modifiers (the C ABI rejects what it cannot do
+before any launch), what the binding cannot express, and the host rules that choose
+the launches' shapes (launch_mod.hpp, launch_block.hpp, compiled for the host).  No
+GPU is needed."""
+
+import ctypes
+import os
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+
+import paper_2609_18077_amd as vx
+
+INV, UNS = 1, 2
+P = 1 << 40  # fake device addresses, far apart, never dereferenced
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+
+
+def _p(x):
+    return ctypes.c_void_p(x) if x else None
+
+
+def _desc(**s):
+    d = vx.ScoreDesc()
+    for n, x in s.items():
+        setattr(d, n, x)
+    return d
+
+
+BASE = dict(B=2, H=4, Hkv=2, Lq=8, Lk=8, d=128, scale=0.1)
+
+
+def _fwd(q=P, k=2 * P, v=3 * P, o=4 * P, lse=None, ws=None, wn=0, s=None, **n):
+    n = {**BASE, **n}
+    return vx.lib().vidax_attn_mod_fwd(_p(q), _p(k), _p(v), _p(o), _p(lse), n["B"], n["H"], n["Hkv"], n["Lq"], n["Lk"], n["d"],
+                                       n["scale"], ctypes.byref(_desc(**s)) if s is not None else None, _p(ws), wn, None)
+
+
+def _bwd(q=P, k=2 * P, v=3 * P, o=4 * P, g=5 * P, lse=6 * P, dq=7 * P, dk=8 * P, dv=9 * P, ws=10 * P, wn=1 << 20, s=None, **n):
+    n = {**BASE, **n}
+    return vx.lib().vidax_attn_mod_bwd(_p(q), _p(k), _p(v), _p(o), _p(g), _p(lse), _p(dq), _p(dk), _p(dv), n["B"], n["H"],
+                                       n["Hkv"], n["Lq"], n["Lk"], n["d"], n["scale"],
+                                       ctypes.byref(_desc(**s)) if s is not None else None, _p(ws), wn, None)
+
+
+SHARED = [dict(B=-1), dict(H=-1), dict(Hkv=-1), dict(Lq=-1), dict(Lk=-1), dict(d=-1), dict(Hkv=3), dict(Hkv=0), dict(H=0),
+          dict(scale=float("nan")), dict(scale=float("inf")), dict(q=P + 8), dict(k=0), dict(v=2 * P + 4), dict(q=0),
+          dict(s=dict(causal=2)), dict(s=dict(cap=-1.0)), dict(s=dict(cap=float("inf"))), dict(s=dict(cap=float("nan"))),
+          dict(scale=1.0, s=dict(cap=1e-44)), dict(s=dict(q_doc=11 * P)), dict(s=dict(k_doc=11 * P)),
+          dict(s=dict(prefix_len=11 * P)), dict(s=dict(kv_valid_len=11 * P + 2)), dict(s=dict(slopes=11 * P + 1)),
+          dict(s=dict(causal=1, prefix_len=11 * P + 3)), dict(s=dict(q_start=11 * P + 2)),
+          dict(s=dict(q_doc=11 * P + 2, k_doc=12 * P))]
+UNSUPPORTED = [dict(d=64), dict(H=64, Hkv=64, Lq=140000), dict(H=1 << 18, Hkv=1 << 18), dict(Lk=(1 << 28) + 1),
+               dict(B=1 << 15, Lq=1 << 15)]
+
+
+@pytest.mark.parametrize("call", [_fwd, _bwd])
+def test_shared_refusals(call):
+    for bad in SHARED:
+        assert call(**bad) == INV, bad
+    for bad in UNSUPPORTED:
+        assert call(**bad) == UNS, bad
+
+
+def test_forward_refusals():
+    assert _fwd(B=0, q=0, k=0, v=0, o=0) == 0
+    assert _fwd(Lq=0, q=0, o=0) == 0
+    for bad in (dict(o=0), dict(o=P), dict(o=P + 1024), dict(o=2 * P), dict(o=3 * P + 64), dict(lse=5 * P + 2), dict(lse=4 * P),
+                dict(lse=P), dict(ws=5 * P + 8, wn=64), dict(ws=4 * P, wn=64), dict(ws=2 * P + 64, wn=64),
+                dict(s=dict(kv_valid_len=4 * P)), dict(lse=5 * P, s=dict(q_start=5 * P + 16)),
+                dict(s=dict(q_doc=11 * P, k_doc=12 * P)),                               # documents need a workspace
+                dict(s=dict(q_doc=11 * P, k_doc=12 * P), ws=5 * P, wn=19),              # 2 (4 + 4 + 1 + 1) values
+                dict(s=dict(q_doc=11 * P, k_doc=12 * P), ws=12 * P, wn=64)):
+        assert _fwd(**bad) == INV, bad
+
+
+def test_backward_refusals():
+    assert _bwd(B=0) == 0
+    for n in ("o", "g", "lse", "dq", "dk", "dv", "ws"):
+        assert _bwd(**{n: 0}) == INV, n
+    for bad in (dict(dq=P), dict(dk=7 * P + 64), dict(dv=8 * P), dict(dq=6 * P), dict(ws=5 * P), dict(ws=8 * P + 64, wn=1 << 20),
+                dict(o=4 * P + 2), dict(lse=6 * P + 2), dict(wn=2 * 2 * 4 * 8), dict(s=dict(kv_valid_len=9 * P)),
+                dict(wn=1 << 61)):
+        assert _bwd(**bad) == INV, bad
+
+
+def test_workspace_sizes():
+    f, b = vx.lib().vidax_attn_mod_fwd_workspace_floats, vx.lib().vidax_attn_mod_bwd_workspace_floats
+    assert f(2, 4, 3, 8, 8, 128, 0) == b(2, 4, 3, 8, 8, 128, 0) == f(2, 4, 2, 8, 8, 64, 0) == f(-1, 4, 2, 8, 8, 128, 1) == 0
+    assert f(0, 4, 2, 8, 8, 128, 1) == 0
+    assert f(1, 1, 1, 70, 500, 128, 1) >= 4 * (2 + 8) + 1 + 2  # what documents need
+    assert b(1, 2, 1, 300, 300, 128, 0) >= 2 * 2 * 300
+
+
+def test_binding_refuses_what_it_cannot_express():
+    import torch
+
+    q = torch.zeros((1, 4, 2, 128), dtype=torch.bfloat16)
+    for call in (lambda: vx.attn_mod_fwd(q, q, q), lambda: vx.attn_mod_bwd(q, q, q, q, q, q)):
+        with pytest.raises(ValueError, match="device tensor"):
+            call()
+    with pytest.raises(ValueError, match="together"):
+        vx._score_desc(vx.Score(q_doc=q), q, 4)
+    ids = torch.zeros((1, 4), dtype=torch.int32)
+    for s in (vx.Score(q_doc=ids, k_doc=ids[:, :3]), vx.Score(q_doc=ids.long(), k_doc=ids), vx.Score(kv_valid_len=ids),
+              vx.Score(slopes=torch.zeros(3)), vx.Score(q_start=ids[0, :2])):
+        with pytest.raises(ValueError):
+            vx._score_desc(s, q, 4)
+
+
+# ------------------------------------------------------- launch rules ----
+
+SOURCE = r"""
+#include "launch_block.hpp"
+#include "launch_mod.hpp"
+using namespace vidax;
+extern "C" void fwd(int B, int H, int Hkv, int Lq, int Lk, int docs, int causal, int lens, int cus, size_t most, int64_t* o) {
+  const ModSplit s = mod_fwd_split(B, H, Hkv, Lq, Lk, docs, causal, lens, cus, most);
+  o[0] = s.few; o[1] = s.runs; o[2] = s.units; o[3] = s.part; o[4] = s.floats;
+}
+extern "C" void bwd(int B, int H, int Hkv, int Lq, int Lk, int docs, int causal, int cus, size_t most, int64_t* o) {
+  const ModBwdSplit s = mod_bwd_split(B, H, Hkv, Lq, Lk, docs, causal, cus, most);
+  o[0] = s.runs; o[1] = s.quantum; o[2] = s.delta; o[3] = s.nlse; o[4] = s.empty; o[5] = s.counts; o[6] = s.part;
+  o[7] = s.least; o[8] = s.floats;
+}
+extern "C" void block(int B, int L, int C, int64_t* o) {
+  const BlockShape s = block_bwd_shape(B, L, C);
+  o[0] = s.chunks; o[1] = s.waves; o[2] = s.groups; o[3] = s.rows; o[4] = s.runs;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def rules(tmp_path_factory):
+    if not os.path.exists(HIPCC):
+        pytest.skip("hipcc is not available")
+    d = tmp_path_factory.mktemp("mod_rules")
+    src, lib = d / "rules.cpp", d / "librules.so"
+    src.write_text(SOURCE)
+    res = subprocess.run([HIPCC, "--offload-arch=gfx950", "--offload-host-only", "-O1", "-std=c++17", "-fPIC", "-shared",
+                          "-x", "hip", "-I", os.path.join(ROOT, "paper_2609_18077_amd", "csrc"), str(src), "-o",
+                          str(lib)], capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, res.stderr[-4000:]
+    lib = ctypes.CDLL(str(lib))
+
+    def call(name, *a):
+        out = (ctypes.c_int64 * 10)()
+        f = getattr(lib, name)
+        f.argtypes = [ctypes.c_int] * (len(a) - (name != "block")) + [ctypes.c_size_t] * (name != "block") + [ctypes.c_void_p]
+        f.restype = None
+        f(*a, out)
+        return list(out)
+
+    return call
+
+
+def _shapes():
+    rng = np.random.default_rng(71)
+    for _ in range(400):
+        Hkv = int(rng.integers(1, 20))
+        yield (int(rng.integers(1, 20)), Hkv * int(rng.integers(1, 9)), Hkv, int(np.exp(rng.uniform(0, 10.5))),
+               int(np.exp(rng.uniform(0, 10.5))))
+
+
+ALL = 1 << 62
+
+
+def test_forward_split_fits_its_workspace(rules):
+    for B, H, Hkv, Lq, Lk in _shapes():
+        for docs in (0, 1):
+            doc = B * (4 * (-(-Lk // 64) + -(-Lq // 64)) + -(-Lk // 256) + -(-Lq // 256)) if docs else 0
+            for causal in (0, 1):
+                few, runs, units, part, floats = rules("fwd", B, H, Hkv, Lq, Lk, docs, causal, 1, 256, ALL)[:5]
+                assert few == (H // Hkv * Lq <= 32) and 1 <= runs <= 16 and runs <= -(-Lk // 64)
+                assert units == 0 or (few and units * Hkv <= 256)
+                slots = (units + B) * H * Lq if units else runs * B * H * Lq if runs > 1 else 0
+                assert floats == (part + 129 * slots if slots else doc) and part >= doc and part % 64 == 0
+                # with less it takes what fits, down to one run
+                tight = rules("fwd", B, H, Hkv, Lq, Lk, docs, causal, 1, 256, floats)[:5]
+                assert tight[4] <= floats
+                least = rules("fwd", B, H, Hkv, Lq, Lk, docs, causal, 1, 256, doc)[:5]
+                assert least[1] == 1 and least[2] == 0 and least[4] == doc
+
+
+def test_backward_split_fits_its_workspace(rules):
+    for B, H, Hkv, Lq, Lk in _shapes():
+        for docs in (0, 1):
+            for causal in (0, 1):
+                runs, quantum, delta, nlse, empty, counts, part, least, floats = rules("bwd", B, H, Hkv, Lq, Lk, docs, causal, 256,
+                                                                                       ALL)[:9]
+                doc = B * (4 * (-(-Lk // 64) + -(-Lq // 64)) + -(-Lk // 256) + -(-Lq // 256)) if docs else 0
+                rows = B * H * Lq
+                assert doc <= delta and delta + rows <= nlse and nlse + rows <= empty
+                assert empty + B * 2 * -(-Lq // 64) <= counts and counts + B * -(-Lk // 256) <= least <= part
+                assert all(x % 64 == 0 for x in (delta, nlse, empty, part))
+                assert least <= doc + 2 * rows + B * (2 * -(-Lq // 64) + -(-Lk // 256)) + 256  # as the header says
+                assert 1 <= runs <= 16 and floats == (part + runs * 2 * B * Lk * Hkv * 128 if runs > 1 else least)
+                assert runs == 1 or 2 * runs * B * Lk * Hkv * 128 <= 96 << 20
+                if not docs:  # the longest stream's runs cover it
+                    longest = H // Hkv * (-(-Lq // 64) - (max(Lq - Lk, 0) // 64 if causal else 0))
+                    assert runs * quantum >= longest
+                one = rules("bwd", B, H, Hkv, Lq, Lk, docs, causal, 256, least)[:9]
+                assert one[0] == 1 and one[8] == least
+
+
+def test_block_runs_cover_every_token(rules):
+    rng = np.random.default_rng(72)
+    for _ in range(500):
+        B, L, C = int(rng.integers(1, 600)), int(np.exp(rng.uniform(0, 12))), 8 * int(np.exp(rng.uniform(0, 7.6)))
+        chunks, waves, groups, rows, runs = rules("block", B, L, C)[:5]
+        assert waves * 64 * chunks * 8 >= C and (waves - 1) * 64 * chunks * 8 < C  # every wave has a channel
+        assert waves * groups <= (10 if chunks == 1 else 8) and (groups == 1 or waves * groups <= 8)
+        assert (runs - 1) * rows < L <= runs * rows

@@ -145,8 +145,8 @@ __device__ __forceinline__ bool same(const Docs& a, const Docs& b) {
 //   Tiles of equal work, or one round of workgroups: an XCD takes a stretch of a
 // head's tiles, whose other side then stays in its L2.
 //   Otherwise (`sorted`) the most work first, all heads of a tile side by side: a
-// late start of a long tile would hold the launch up (16384 causal, 12 heads:
-// 1172 us with long and short tiles in turn, XCD by XCD; 842 so).
+// late start of a long tile would hold the launch up (16384 causal, 12 heads, the
+// kernel of then: 1172 us with long and short tiles in turn, XCD by XCD; 842 so).
 template <typename A>
 __device__ __forceinline__ void place(const A& a, int heads, const int32_t* order, int& run, int& t, int& b, int& h) {
   const ModCall& c = a.c;
@@ -174,6 +174,129 @@ __device__ __forceinline__ void place(const A& a, int heads, const int32_t* orde
   t = x - bh * a.ntile;
   b = bh / heads;
   h = bh - b * heads;
+}
+
+// ---- equal pieces of all the key tiles of all query tiles (no documents)
+//
+// The query tiles' key tiles, behind one another (batch, head, query tile, key
+// tile), are one sequence, cut into `pieces` of equal weight, a workgroup each; a
+// piece may end one query tile, hold some whole and begin another.  A query tile
+// that is cut leaves partial results, at most two a piece (slots 2 p: a part that
+// does not begin the tile, 2 p + 1: one that does), which a further launch joins.
+struct Pieces {
+  int n;         // 0: not in pieces
+  int slot_rows; // rows of a slot
+  int32_t* cut;  // [B][H][tiles][2]: first (-1: not cut) and last piece of a tile
+};
+struct Part {
+  int b, h, t;    // query tile
+  int n, lo, hi;  // its key tiles, and this part of them
+  int piece;
+  __device__ __forceinline__ bool whole() const { return lo == 0 && hi == n; }
+  __device__ __forceinline__ int slot() const { return 2 * piece + (lo == 0); }
+};
+
+// Key tiles of query tile t.
+__device__ __forceinline__ int key_tiles(const ModCall& c, const Batch& bt, int t) {
+  return (key_limit(bt, c.s.causal, bt.start + min((t + 1) * kModRows, c.Lq) - 1) + kModKeys - 1) / kModKeys;
+}
+__device__ __forceinline__ int tile_weight(const ModCall& c, const Batch& bt, int t) {
+  return kTileStart + key_tiles(c, bt, t) * key_weight(min(c.Lq - t * kModRows, kModRows));
+}
+
+// f(part) for every part of piece p, in order.  All waves alike.
+template <typename F>
+__device__ __forceinline__ void each_part(const ModCall& c, int pieces, int p, F&& f) {
+  const int lane = threadIdx.x & 63, nt = (int)mod_tiles(c.Lq);
+  const bool lens = c.s.kv_valid_len || c.s.q_start || c.s.prefix_len;
+  auto head_weight = [&](const Batch& bt) {
+    int w = 0;
+    for (int t = lane; t < nt; t += 64) w += tile_weight(c, bt, t);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) w += __shfl_xor(w, m);
+    return __builtin_amdgcn_readfirstlane(w);
+  };
+  Batch bt = batch_of(c, 0);
+  int hw = head_weight(bt);
+  int64_t total = (int64_t)hw * c.H * c.B;
+  if (lens) {
+    total = (int64_t)hw * c.H;
+    for (int b = 1; b < c.B; ++b) total += (int64_t)head_weight(batch_of(c, b)) * c.H;
+  }
+  int64_t per = (total + pieces - 1) / pieces;
+  if (per < kLeastPiece) per = kLeastPiece;
+  const int64_t pos = p * per, end = pos + per < total ? pos + per : total;
+  if (pos >= end) return;
+  // the tile at pos
+  int64_t S = 0;  // where the tile begins
+  int b = 0;
+  if (lens) {
+    while (pos >= S + (int64_t)hw * c.H) {  // (ends: pos < total)
+      S += (int64_t)hw * c.H;
+      bt = batch_of(c, ++b);
+      hw = head_weight(bt);
+    }
+  } else {
+    b = (int)(pos / ((int64_t)hw * c.H));
+    bt = batch_of(c, b);
+    S = (int64_t)hw * c.H * b;
+  }
+  int h = (int)((pos - S) / hw);
+  S += (int64_t)h * hw;
+  int t = 0;
+  {
+    const int rem = (int)(pos - S);
+    int before = 0;
+    for (int t0 = 0; t0 < nt; t0 += 64) {
+      const int w = t0 + lane < nt ? tile_weight(c, bt, t0 + lane) : 0;
+      int x = w;
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) {
+        const int y = __shfl_up(x, m);
+        if (lane >= m) x += y;
+      }
+      const uint64_t over = __builtin_amdgcn_ballot_w64(before + x > rem);
+      if (over != 0) {
+        const int i = __builtin_ctzll(over);
+        t = t0 + i;
+        S += before + __builtin_amdgcn_readlane(x - w, i);
+        break;
+      }
+      before += __builtin_amdgcn_readlane(x, 63);
+    }
+  }
+  for (;;) {
+    const int n = key_tiles(c, bt, t), u = key_weight(min(c.Lq - t * kModRows, kModRows));
+    // the key tile at a position; not within two of either end
+    auto key_at = [&](int64_t x) {
+      const int64_t y = x - S - kTileStart;
+      if (y >= (int64_t)n * u) return n;
+      const int k = y <= 0 ? 0 : (int)y / u;
+      return k < 2 ? 0 : k > n - 2 ? n : k;
+    };
+    const Part part{b, h, t, n, key_at(pos), key_at(end), p};
+    if (part.lo < part.hi || (n == 0 && pos <= S)) f(part);
+    S += kTileStart + n * u;
+    if (S >= end) return;
+    if (++t == nt) {
+      t = 0;
+      if (++h == c.H) {
+        h = 0;
+        bt = batch_of(c, ++b);
+      }
+    }
+  }
+}
+// What the join has to know of a tile, noted by whoever begins or ends it.
+__device__ __forceinline__ void note_cut(const Pieces& x, const ModCall& c, const Part& part) {
+  int32_t* const p = x.cut + (((size_t)part.b * c.H + part.h) * mod_tiles(c.Lq) + part.t) * 2;
+  if (part.lo == 0) p[0] = part.whole() ? -1 : part.piece;
+  else if (part.hi == part.n) p[1] = part.piece;
+}
+// Pieces of one head to one XCD (its K and V in that L2).
+__device__ __forceinline__ int piece_of(int block, int n) {
+  const int q = n >> 3, r = n & 7, x = block & 7;
+  return x * q + min(x, r) + (block >> 3);
 }
 
 // A tile of the streamed side, as a workgroup or wave meets it (uniform).

@@ -22,7 +22,8 @@
 //     read as zeros, so that nothing that lies there reaches the output.
 //   Sums add the fp32 probabilities, not their bf16 roundings: the log-sum-exp is
 //     then good to fp32, and costs eight additions a block more.
-//   Few tiles of rows: the keys are cut into runs, a workgroup each, whose
+//   Few tiles of rows, or uneven ones: the keys are cut into runs, or all tiles'
+//     keys into pieces of equal weight (attn_mod.hpp), a workgroup each, whose
 //     normalised fp32 outputs and log-sum-exps a second launch joins.
 #include "attn_mod.hpp"
 #include "launch.hpp"
@@ -48,7 +49,10 @@ struct FwdArgs {
   const uint16_t *q, *k, *v;
   uint16_t* o;
   float* lse;
-  float *po, *pl;  // partial outputs [runs][B][H][Lq][D] and log2-sum-exps [runs][B][H][Lq], or null
+  // partial outputs [runs][B][H][Lq][D] and log2-sum-exps [runs][B][H][Lq], or null;
+  // in pieces: [slots][slot_rows][D] and [slots][slot_rows]
+  float *po, *pl;
+  Pieces pieces;
   ModRanges r;
   int ntile, nwg, runs;
   int in_run[kMostRuns];   // see place()
@@ -56,9 +60,9 @@ struct FwdArgs {
   int kr, qr;      // document ranges a batch
 };
 
-// CAP, BIAS: the scores' modifiers.
-template <bool CAP, bool BIAS>
-__device__ __forceinline__ void fwd_body(const FwdArgs& a) {
+// CAP, BIAS: the scores' modifiers.  PIECES: the part of a query tile's keys given.
+template <bool CAP, bool BIAS, bool PIECES>
+__device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
   __shared__ __attribute__((aligned(16))) uint16_t K0[TILE], K1[TILE], V0[TILE], V1[TILE];
   __shared__ __attribute__((aligned(16))) int Kd[2][BN];  // ids of the tiles' keys, where they differ
 
@@ -72,7 +76,14 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a) {
   const int qbytes = qtok * 2, kbytes = ktok * 2;
 
   int b, h, qt, run;
-  place(a, c.H, a.r.q_order, run, qt, b, h);
+  if constexpr (PIECES) {
+    b = part.b;
+    h = part.h;
+    qt = part.t;
+    run = 0;
+  } else {
+    place(a, c.H, a.r.q_order, run, qt, b, h);
+  }
   const int hk = h / (c.H / c.Hkv);
   const Batch bt = batch_of(c, b);
   const int row0 = qt * BM;                     // of the workgroup
@@ -88,7 +99,7 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a) {
   int lim = qlive ? key_limit(bt, c.s.causal, bt.start + qrow) : 0;
   int qd = 0;
   Docs wdoc{0, 0, false}, gdoc{0, 0, false};
-  const bool docs = a.r.k != nullptr;
+  const bool docs = !PIECES && a.r.k != nullptr;
   if (docs) {
     if (qlive) qd = c.s.q_doc[(size_t)b * c.Lq + qrow];
     if (qd < 0) lim = 0;
@@ -103,16 +114,16 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a) {
   const int wmax = wlast >= wrow ? key_limit(bt, c.s.causal, bt.start + wlast) : 0;
   const int wmin = wlast >= wrow ? key_limit(bt, c.s.causal, bt.start + wrow) : 0;
   const int gmax = key_limit(bt, c.s.causal, bt.start + glast);
-  const int ntiles = (gmax + BN - 1) / BN;
+  const int ntiles = PIECES ? part.hi : (gmax + BN - 1) / BN, tile0 = PIECES ? part.lo : 0;
 
   // ---- the next tile to visit: a group of 64 tiles is looked at together, lane
   // l at tile 64 g + l.
-  int grp = 0, left = INT32_MAX;  // group; tiles left of this run
+  int grp = tile0 >> 6, left = INT32_MAX;  // group; tiles left of this run
   uint64_t visit = 0;             // tiles that some row of the workgroup may see
   int fl = 0, id = 0;             // of the lane's tile
   auto look = [&](int g) __attribute__((always_inline)) {
     const int t = 64 * g + lane;
-    bool v = t < ntiles;
+    bool v = t >= tile0 && t < ntiles;
     fl = (t * BN < wmax ? Tile::kMine : 0) | (t * BN + BN <= wmin ? Tile::kWhole : 0) | Tile::kOne;
     if (docs && v) {
       const int4 r = *reinterpret_cast<const int4*>(a.r.k + (size_t)b * a.kr + 2 * t);
@@ -319,9 +330,10 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a) {
     const float l = wave_half_sum(lsum);
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     const float lse2 = l == 0.f ? -INFINITY : mref + __log2f(l);
-    if (a.po) {  // fp32 rows of this run
+    if (PIECES ? !part.whole() : a.po != nullptr) {  // fp32 rows of this run or part
       if (qlive) {
-        float* const p = a.po + ((size_t)run * nrow + orow + qrow) * D;
+        const size_t prow = PIECES ? (size_t)part.slot() * a.pieces.slot_rows + (qrow - row0) : (size_t)run * nrow + orow + qrow;
+        float* const p = a.po + prow * D;
 #pragma unroll
         for (int mb = 0; mb < 4; ++mb)
 #pragma unroll
@@ -329,7 +341,7 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a) {
             *reinterpret_cast<float4*>(p + 32 * mb + 8 * g + 4 * hi) =
                 make_float4(oacc[mb][4 * g] * inv, oacc[mb][4 * g + 1] * inv, oacc[mb][4 * g + 2] * inv,
                             oacc[mb][4 * g + 3] * inv);
-        if (hi == 0) a.pl[(size_t)run * nrow + orow + qrow] = lse2;
+        if (hi == 0) a.pl[prow] = lse2;
       }
       return;
     }
@@ -358,7 +370,9 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a) {
 
   Tile cur{-1, 0, 0}, nxt = cur;
   if (ntiles > 0) {
-    if (a.runs > 1) {  // this run's part of the tiles to visit
+    if (PIECES) {
+      look(grp);
+    } else if (a.runs > 1) {  // this run's part of the tiles to visit
       int n = ntiles;
       if (docs) {
         n = 0;
@@ -439,7 +453,19 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a) {
 
 template <bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
-  fwd_body<CAP, BIAS>(a);
+  fwd_body<CAP, BIAS, false>(a, Part{});
+}
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ void pieces_body(const FwdArgs& a) {
+  each_part(a.c, a.pieces.n, piece_of(blockIdx.x, a.pieces.n), [&](const Part& part) __attribute__((always_inline)) {
+    if (threadIdx.x == 0) note_cut(a.pieces, a.c, part);
+    fwd_body<CAP, BIAS, true>(a, part);
+    __syncthreads();  // (the staging areas)
+  });
+}
+template <bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT) void attn_mod_pieces_kernel(FwdArgs a) {
+  pieces_body<CAP, BIAS>(a);
 }
 
 // Ranges of document ids of every 32 tokens: a wave takes 64 tokens of a batch.
@@ -475,7 +501,7 @@ __global__ __launch_bounds__(256) void mod_ranges_kernel(RangeArgs a) {
 // The order in which the 256-row tiles of the queries (block 0 + first) or keys (1)
 // are handed out: most tiles of the other side to visit first.  Documents make
 // tiles of very different work; in their own order the last ones to start held
-// the launch up (five clips in 16380 tokens, 12 heads, forward: 683 us; sorted 371).  A wave
+// the launch up (five clips in 16380 tokens, 12 heads, forward: 683 us; sorted 517).  A wave
 // counts a tile's work, 64 tiles of the other side at a time; ranks by counting.
 constexpr size_t kOrderMost = 4096;
 struct OrderArgs {
@@ -522,6 +548,45 @@ __global__ __launch_bounds__(1024) void mod_order_kernel(OrderArgs a) {
     int rank = 0;
     for (int j = 0; j < n; ++j) rank += work[j] > w || (work[j] == w && j < i);
     (isq ? a.oq : a.ok)[rank] = i;
+  }
+}
+
+// Joins the parts of the tiles that pieces have cut: 16 rows a workgroup, a wave four.
+struct PieceJoinArgs {
+  const float *po, *pl;
+  uint16_t* o;
+  float* lse;
+  Pieces pieces;
+  int H, Lq, ntile;
+};
+__global__ __launch_bounds__(256) void mod_piece_join_kernel(PieceJoinArgs a) {
+  const int tile = blockIdx.x >> 4, sub = blockIdx.x & 15;
+  const int p0 = __builtin_amdgcn_readfirstlane(a.pieces.cut[2 * tile]);
+  if (p0 < 0) return;
+  const int p1 = __builtin_amdgcn_readfirstlane(a.pieces.cut[2 * tile + 1]);
+  const int bh = tile / a.ntile, row0 = (tile - bh * a.ntile) * BM + 16 * sub + 4 * (threadIdx.x >> 6);
+  const int b = bh / a.H, h = bh - b * a.H, lane = threadIdx.x & 63;
+  for (int i = row0; i < min(row0 + 4, a.Lq); ++i) {
+    auto at = [&](int p) { return (size_t)(2 * p + (p == p0)) * a.pieces.slot_rows + (i & (BM - 1)); };
+    float m = -INFINITY;
+#pragma unroll 4
+    for (int p = p0; p <= p1; ++p) m = fmaxf(m, a.pl[at(p)]);
+    float x = 0.f, y = 0.f, l = 0.f;
+    if (m > -INFINITY) {
+#pragma unroll 4
+      for (int p = p0; p <= p1; ++p) {
+        const float w = __builtin_amdgcn_exp2f(a.pl[at(p)] - m);
+        const float2 v = *reinterpret_cast<const float2*>(a.po + at(p) * D + 2 * lane);
+        l += w;  // (a part that saw nothing wrote zeros: weight 0)
+        x = fmaf(w, v.x, x);
+        y = fmaf(w, v.y, y);
+      }
+      const float inv = 1.0f / l;
+      x *= inv;
+      y *= inv;
+    }
+    *reinterpret_cast<uint32_t*>(a.o + (((size_t)b * a.Lq + i) * a.H + h) * D + 2 * lane) = pack_bf16x2(x, y);
+    if (a.lse && lane == 0) a.lse[(size_t)bh * a.Lq + i] = m > -INFINITY ? (m + __log2f(l)) * kLn2 : -INFINITY;
   }
 }
 
@@ -634,6 +699,19 @@ hipError_t launch_attn_mod_fwd(const ModFwd& f, hipStream_t stream) {
   hipError_t e = launch_mod_ranges(c, f.ws, !s.few && a.sorted, false, &a.r, stream);
   if (e != hipSuccess) return e;
   if (s.few) return launch_mod_few(f, s, a.r, stream);
+  if (s.pieces) {
+    a.po = f.ws + s.part;
+    a.pl = a.po + (size_t)2 * s.pieces * s.slot_rows * D;
+    a.pieces = Pieces{s.pieces, s.slot_rows, reinterpret_cast<int32_t*>(f.ws + s.cut)};
+    const bool cap = c.s.cap > 0.f, bias = c.s.slopes != nullptr;
+    e = cap ? (bias ? launch_kernel(attn_mod_pieces_kernel<true, true>, (unsigned)s.pieces, (unsigned)NT, stream, a)
+                    : launch_kernel(attn_mod_pieces_kernel<true, false>, (unsigned)s.pieces, (unsigned)NT, stream, a))
+            : (bias ? launch_kernel(attn_mod_pieces_kernel<false, true>, (unsigned)s.pieces, (unsigned)NT, stream, a)
+                    : launch_kernel(attn_mod_pieces_kernel<false, false>, (unsigned)s.pieces, (unsigned)NT, stream, a));
+    if (e != hipSuccess) return e;
+    const PieceJoinArgs j{a.po, a.pl, f.o, f.lse, a.pieces, c.H, c.Lq, a.ntile};
+    return launch_kernel(mod_piece_join_kernel, (unsigned)(a.ntile * c.B * c.H * 16), 256u, stream, j);
+  }
   for (int r = 0; r < kMostRuns; ++r) a.in_run[r] = a.r.q_order ? a.ntile * c.B : a.ntile;
   const bool cap = c.s.cap > 0.f, bias = c.s.slopes != nullptr;
   e = cap ? (bias ? launch_kernel(attn_mod_fwd_kernel<true, true>, (unsigned)a.nwg, (unsigned)NT, stream, a)

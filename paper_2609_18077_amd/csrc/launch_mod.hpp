@@ -64,9 +64,20 @@ constexpr int kModKeys = 64;
 constexpr int kFewRows = 32;
 constexpr int kMostRuns = 16;
 
+// Or all key tiles of all query tiles are cut into `pieces` of equal weight
+// (attn_mod.hpp): tiles of unequal work, or not a whole number of rounds of them.
+constexpr int kTileStart = 8;  // weight of starting and ending a query tile; see key_weight
+// Weight of a key tile for a query tile of so many rows: one or two waves a SIMD.
+__host__ __device__ inline int key_weight(int rows) { return rows > 128 ? 4 : 3; }
+// Four key tiles: every piece between a tile's first and last then holds some of it.
+constexpr int kLeastPiece = 16;
+
 struct ModSplit {
   bool few;
   int runs;       // of the 256-row form
+  int pieces;     // of the 256-row form; 0: a workgroup takes a tile (or one of its runs)
+  int slot_rows;  // rows of a piece's partial result
+  size_t cut;     // first value of the table of cut tiles
   int units;      // of the form for few rows; 0: a workgroup takes a whole batch
   size_t part;    // first value of the partial results in the workspace
   size_t floats;  // values of the workspace
@@ -76,7 +87,7 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
                               size_t max_floats) {
   ModSplit r;
   r.runs = 1;
-  r.units = 0;
+  r.units = r.pieces = 0;
   r.floats = mod_doc_floats(B, Lq, Lk, docs);
   r.part = (r.floats + 63) / 64 * 64;
   r.few = Hkv > 0 && (int64_t)(H / Hkv) * Lq <= kFewRows;
@@ -106,33 +117,58 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
   // 256-row workgroups, one a compute unit, 2 us a tile of 64 keys.  Equal ones run
   // in rounds; unequal ones (causal, documents), the longest first, end with the
   // mean load or the longest of them.  4 us to start and end; the joining launch 4
-  // us and the runs' bytes at 5 TB/s.  How much of the keys a document leaves is not
-  // known here: a third is assumed, and a tile's keys are cut only where the tiles
-  // leave half of the compute units without one.
+  // us and the partial results' bytes at 5 TB/s.
   const int64_t tiles = ((int64_t)Lk + kModKeys - 1) / kModKeys, qt = (int64_t)mod_tiles(Lq);
   const int64_t wgs = qt * B * H;
-  int64_t total = tiles * qt;  // of a head
-  if (causal) {
-    total = 0;
-    for (int64_t t = 0; t < qt; ++t) {
+  if (qt > 4096) return r;  // (rounds enough)
+  int64_t total = tiles * qt, weight = 0;  // of a head
+  for (int64_t t = 0; t < qt; ++t) {
+    int64_t n = tiles;
+    if (causal) {
       const int64_t last = (int64_t)Lk - Lq + ((t + 1) * kModRows < Lq ? (t + 1) * kModRows : Lq);  // keys seen by the last row
-      total += last <= 0 ? 0 : last >= Lk ? tiles : (last + kModKeys - 1) / kModKeys;
+      n = last <= 0 ? 0 : last >= Lk ? tiles : (last + kModKeys - 1) / kModKeys;
+      total -= tiles - n;
+    }
+    weight += kTileStart + n * key_weight((int)(Lq - t * kModRows < kModRows ? Lq - t * kModRows : kModRows));
+  }
+  auto direct = [&](int s) {
+    const int64_t rounds = (wgs * s + cus - 1) / cus;
+    const double per = (double)(docs ? (tiles + 2) / 3 : tiles) / s;
+    const double mean = 1.05 * (double)(docs ? (total + 2) / 3 : total) * B * H / cus;
+    const double load = docs || causal ? (mean > per ? mean : per) : rounds * (double)((tiles + s - 1) / s);
+    return load * 2.0 + rounds * 4.0 + (s > 1 ? 4.0 + (double)s * rows * 1056 / 5e6 : 0.0);
+  };
+  double best = direct(1);
+  // How much of the keys a document leaves is not known here: a third is assumed, and
+  // a tile's keys are cut only where the tiles leave half of the compute units without
+  // one.
+  for (int s = 2; s <= kMostRuns && s <= tiles && (!docs || wgs * s <= cus); ++s) {
+    const size_t need = r.part + (size_t)s * rows * 129;  // a run's rows: 128 outputs and a log-sum-exp each
+    if (need > max_floats) break;
+    if (direct(s) < best) {
+      best = direct(s);
+      r.runs = s;
+      r.floats = need;
     }
   }
-  if (docs) total = (total + 2) / 3;
-  double best = 1e30;
-  for (int s = 1; s <= kMostRuns && s <= tiles; ++s) {
-    const size_t need = r.part + (size_t)s * rows * 129;  // a run's rows: 128 outputs and a log-sum-exp each
-    if (s > 1 && (need > max_floats || (docs && wgs * s > cus))) break;
-    const int64_t rounds = (wgs * s + cus - 1) / cus;
-    const double per = (double)(docs ? (tiles + 2) / 3 : tiles) / s, mean = 1.05 * (double)total * B * H / cus;
-    const double load = docs || causal ? (mean > per ? mean : per) : rounds * (double)((tiles + s - 1) / s);
-    const double cost = load * 2.0 + rounds * 4.0 + (s > 1 ? 4.0 + (double)s * rows * 1056 / 5e6 : 0.0);
-    if (cost < best) {
-      best = cost;
-      r.runs = s;
-      if (s > 1) r.floats = need;
-    }
+  // Pieces, one a compute unit and 16 key tiles at least: 12 us to find and start
+  // them.  A workgroup finds its own by going over the tiles' weights, 64 at a time:
+  // not where they are too many for that to be short.  Pieces of a head read its keys
+  // at different places; where K and V of a head are more than an L2 (4 MB) that costs
+  // 15 %.  (12 heads, 6144 plain: seven runs 303 us, pieces 261; causal 175 and 155;
+  // 1560 rows on 32760 keys: three runs 346, pieces 413.)
+  const int64_t all = weight * B * H, most = all / (4 * kLeastPiece);
+  const int n = (int)(most < cus ? most : cus);
+  if (docs || n < 2 || (qt + 63) / 64 * B > 64 || weight > INT32_MAX) return r;
+  r.slot_rows = (Lq < kModRows ? Lq + 31 : kModRows) / 32 * 32;
+  const int64_t parts = n + (wgs < n ? wgs : n);
+  const size_t cut = r.part + (size_t)2 * n * r.slot_rows * 129, need = cut + 2 * (size_t)wgs;
+  const double cost = (double)all / n / 4 * 2.0 * (Lk > 8192 ? 1.15 : 1.0) + 16.0 + (double)parts * r.slot_rows * 1056 / 5e6;
+  if (need <= max_floats && cost < best) {
+    r.runs = 1;
+    r.pieces = n;
+    r.cut = cut;
+    r.floats = need;
   }
   return r;
 }

@@ -120,6 +120,7 @@ using namespace vidax;
 extern "C" void fwd(int B, int H, int Hkv, int Lq, int Lk, int docs, int causal, int lens, int cus, size_t most, int64_t* o) {
   const ModSplit s = mod_fwd_split(B, H, Hkv, Lq, Lk, docs, causal, lens, cus, most);
   o[0] = s.few; o[1] = s.runs; o[2] = s.units; o[3] = s.part; o[4] = s.floats;
+  o[5] = s.pieces; o[6] = s.slot_rows; o[7] = s.cut;
 }
 extern "C" void bwd(int B, int H, int Hkv, int Lq, int Lk, int docs, int causal, int cus, size_t most, int64_t* o) {
   const ModBwdSplit s = mod_bwd_split(B, H, Hkv, Lq, Lk, docs, causal, cus, most);
@@ -169,20 +170,78 @@ ALL = 1 << 62
 
 
 def test_forward_split_fits_its_workspace(rules):
+    cuts = 0
     for B, H, Hkv, Lq, Lk in _shapes():
         for docs in (0, 1):
             doc = B * (4 * (-(-Lk // 64) + -(-Lq // 64)) + -(-Lk // 256) + -(-Lq // 256)) if docs else 0
             for causal in (0, 1):
-                few, runs, units, part, floats = rules("fwd", B, H, Hkv, Lq, Lk, docs, causal, 1, 256, ALL)[:5]
+                few, runs, units, part, floats, pieces, rows, cut = rules("fwd", B, H, Hkv, Lq, Lk, docs, causal, 1, 256, ALL)[:8]
                 assert few == (H // Hkv * Lq <= 32) and 1 <= runs <= 16 and runs <= -(-Lk // 64)
                 assert units == 0 or (few and units * Hkv <= 256)
                 slots = (units + B) * H * Lq if units else runs * B * H * Lq if runs > 1 else 0
-                assert floats == (part + 129 * slots if slots else doc) and part >= doc and part % 64 == 0
+                assert part >= doc and part % 64 == 0
+                if pieces:
+                    cuts += 1
+                    assert not docs and not few and runs == 1 and 2 <= pieces <= 256 and rows == min(256, -(-Lq // 32) * 32)
+                    assert cut == part + 2 * pieces * rows * 129 and floats == cut + 2 * B * H * -(-Lq // 256)
+                else:
+                    assert floats == (part + 129 * slots if slots else doc)
                 # with less it takes what fits, down to one run
                 tight = rules("fwd", B, H, Hkv, Lq, Lk, docs, causal, 1, 256, floats)[:5]
                 assert tight[4] <= floats
-                least = rules("fwd", B, H, Hkv, Lq, Lk, docs, causal, 1, 256, doc)[:5]
-                assert least[1] == 1 and least[2] == 0 and least[4] == doc
+                least = rules("fwd", B, H, Hkv, Lq, Lk, docs, causal, 1, 256, doc)[:6]
+                assert least[1] == 1 and least[2] == 0 and least[4] == doc and least[5] == 0
+    assert cuts > 20
+    from tests.test_gpu_attn_mod import PIECES
+
+    for B, H, Hkv, Lq, Lk, mask in PIECES:
+        assert rules("fwd", B, H, Hkv, Lq, Lk, 0, mask not in ("all", "valid"), 1, 256, ALL)[5] > 0
+
+
+def _parts(n_tiles, rows, heads, pieces, p):
+    """What each_part (attn_mod.hpp) gives piece p, in words: the tiles' weights behind one another, cut evenly."""
+    unit = [4 if r > 128 else 3 for r in rows]
+    head = [[8 + n * u for n, u in zip(ns, unit)] for ns in n_tiles]
+    total = sum(sum(w) for w in head) * heads
+    per = max(-(-total // pieces), 16)
+    pos, end = p * per, min(p * per + per, total)
+    at = 0
+    for b, ws in enumerate(head):
+        for h in range(heads):
+            for t, w in enumerate(ws):
+                n, u = n_tiles[b][t], unit[t]
+
+                def key(x):
+                    y = x - at - 8
+                    k = min(max(y, 0) // u, n)
+                    return n if y >= n * u else 0 if k < 2 else n if k > n - 2 else k
+
+                if pos < end and at < end and at + w > pos:
+                    lo, hi = key(pos), key(end)
+                    if lo < hi or (n == 0 and pos <= at):
+                        yield b, h, t, n, lo, hi
+                at += w
+
+
+def test_pieces_cover_every_tile_once():
+    rng = np.random.default_rng(73)
+    for _ in range(300):
+        B, H, Lq, pieces = (int(rng.integers(1, x)) for x in (5, 5, 1500, 40))
+        rows = [min(256, Lq - r) for r in range(0, Lq, 256)]
+        most = int(rng.choice([1, 2, 3, 4, 6, 41, 301]))
+        n = [[int(x) for x in rng.integers(0, most, len(rows))] for _ in range(B)]
+        got = {}
+        for p in range(pieces):
+            mine = list(_parts(n, rows, H, pieces, p))
+            for i, (b, h, t, k, lo, hi) in enumerate(mine):
+                got.setdefault((b, h, t), []).append((p, lo, hi))
+                # two slots a piece are enough
+                assert lo == 0 or i == 0
+                assert hi == k or i == len(mine) - 1
+        assert len(got) == B * H * len(rows)
+        for (b, _, t), x in got.items():
+            assert x[0][1] == 0 and x[-1][2] == n[b][t]
+            assert all(a[2] == c[1] and a[0] + 1 == c[0] for a, c in zip(x, x[1:]))  # one behind the other, none left out
 
 
 def test_backward_split_fits_its_workspace(rules):

@@ -87,7 +87,11 @@ def check(q, k, v, scale=None, what="", workspace=None, **s):
     score, spec = dev_score(**s)
     o, lse = vx.attn_mod_fwd(q, k, v, score, scale=scale, return_lse=True, workspace=workspace)
     torch.cuda.synchronize()
-    sc = SCALE if scale is None else float(np.float32(scale))
+    return compare(o, lse, q, k, v, SCALE if scale is None else float(np.float32(scale)), spec, what)
+
+
+def compare(o, lse, q, k, v, sc, spec, what):
+    """An output and log-sum-exps against the reference; (o, lse)."""
     qn, kn, vn = f64(q), f64(k), f64(v)
     ro, rl = oracle.attn_mod_ref(qn, kn, vn, sc, spec)
     mag, _ = oracle.attn_mod_ref(qn, kn, np.abs(vn), sc, spec)
@@ -281,6 +285,55 @@ def test_runs_of_keys_are_joined(Lq, Lk):
     assert torch.equal(lse == -math.inf, lse1 == -math.inf)
     with pytest.raises(vx.VidaxError):
         check(q, k, v, workspace=torch.empty(least - 1, device="cuda"), **s)
+
+
+# Sizes whose query tiles are cut into pieces of equal weight on 256 compute units
+PIECES = [(3, 16, 4, 296, 3993, "all"), (3, 16, 4, 532, 2375, "valid"), (2, 8, 2, 2814, 2526, "causal"),
+          (1, 8, 2, 4001, 4001, "prefix"), (3, 4, 1, 2934, 5374, "lengths")]
+
+
+@pytest.mark.parametrize("B,H,Hkv,Lq,Lk,mask", PIECES)
+def test_pieces_of_tiles_are_joined(B, H, Hkv, Lq, Lk, mask):
+    """Checked on two heads of every batch; (2814 on 2526: rows and a tile that see nothing)."""
+    import torch
+
+    q, k, v = make(B, H, Hkv, Lq, Lk, Lq + Lk)
+    s = dict(cap=20.0, slopes=list(0.01 * np.arange(H))) if mask in ("lengths", "prefix") else {}
+    if mask != "all" and mask != "valid":
+        s["causal"] = True
+    if mask == "valid":
+        s["kv_valid_len"] = [0, Lk, 700][:B]
+    if mask == "prefix":
+        s["prefix_len"] = [1500]
+    if mask == "lengths":
+        s |= dict(q_start=[-1000, 300, Lk - Lq], kv_valid_len=[1900, 3000, Lk], prefix_len=[0, 900, 70])
+    score, spec = dev_score(**s)
+    o, lse = vx.attn_mod_fwd(q, k, v, score, return_lse=True)
+    again = vx.attn_mod_fwd(q, k, v, score, return_lse=True, workspace=torch.full((1 << 25,), float("nan"), device="cuda"))
+    assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
+    for h in (0, H - 1):
+        hs, ks = slice(h, h + 1), slice(h * Hkv // H, h * Hkv // H + 1)
+        one = oracle.ScoreSpec(**{**s, **({"slopes": np.asarray(s["slopes"], np.float32)[hs].astype(np.float64)} if "slopes" in s else {})})
+        compare(o[:, :, hs], lse[:, hs], q[:, :, hs], k[:, :, ks], v[:, :, ks], SCALE, one, f"pieces {Lq}x{Lk} {mask} head {h}")
+
+
+def test_pieces_in_a_graph():
+    import torch
+
+    q, k, v = make(1, 8, 2, 4001, 4001, 5)
+    score, _ = dev_score(causal=True)
+    ws = torch.empty(1 << 25, device="cuda")
+    out = torch.empty_like(q)
+    vx.attn_mod_fwd(q, k, v, score, out=out, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        vx.attn_mod_fwd(q, k, v, score, out=out, workspace=ws)
+    for n in range(3):
+        q.copy_(make(1, 8, 2, 4001, 4001, n)[0])
+        ws.fill_(float("nan"))
+        graph.replay()
+        assert torch.equal(out, vx.attn_mod_fwd(q, k, v, score)), n
 
 
 def test_rows_and_keys_beside_the_call_stay():

@@ -45,6 +45,8 @@ struct BwdArgs {
   int in_run[kMostRuns];   // see place()
   int32_t* counts;    // [B][tiles of keys]: how many
   int sorted, first_most;  // see place(); causal: the first tile of a head has the most work (else the last)
+  float* dqp;         // dq in pieces: partial sums [slots][slot_rows][D]
+  Pieces pieces;
   float* part;        // fp32 dK, dV of every run of those tiles ([runs][B][Lk][Hkv][D], dV after dK)
 };
 
@@ -103,15 +105,22 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const uint16_t* base
 
 // ------------------------------------------------------------------- dQ ----
 
-template <bool CAP, bool BIAS>
-__device__ __forceinline__ void dq_body(const BwdArgs& a) {
+// PIECES: the part of a query tile's keys given.
+template <bool CAP, bool BIAS, bool PIECES>
+__device__ __forceinline__ void dq_body(const BwdArgs& a, const Part& part) {
   __shared__ __attribute__((aligned(1024))) uint16_t K0[TILE], K1[TILE], V0[TILE], V1[TILE];
   __shared__ __attribute__((aligned(16))) int Kd[2][BN];  // ids of the tiles' keys
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const ModCall& c = a.c;
   int b, h, qt, run;
-  place(a, c.H, a.r.q_order, run, qt, b, h);
+  if constexpr (PIECES) {
+    b = part.b;
+    h = part.h;
+    qt = part.t;
+  } else {
+    place(a, c.H, a.r.q_order, run, qt, b, h);
+  }
   const int hk = h / (c.H / c.Hkv);
   const int qtok = c.H * D, qbytes = qtok * 2, ktok = c.Hkv * D, kbytes = ktok * 2;
   const Batch bt = batch_of(c, b);
@@ -126,7 +135,7 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
   int lim = qlive ? key_limit(bt, c.s.causal, bt.start + qrow) : 0;
   int qd = 0;
   Docs wdoc{0, 0, false}, gdoc{0, 0, false};
-  const bool docs = a.r.k != nullptr;
+  const bool docs = !PIECES && a.r.k != nullptr;
   if (docs) {
     if (qlive) qd = c.s.q_doc[(size_t)b * c.Lq + qrow];
     if (qd < 0) lim = 0;
@@ -141,13 +150,13 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
   const int wmax = wlast >= wrow ? key_limit(bt, c.s.causal, bt.start + wlast) : 0;
   const int wmin = wlast >= wrow ? key_limit(bt, c.s.causal, bt.start + wrow) : 0;
   const int gmax = key_limit(bt, c.s.causal, bt.start + glast);
-  const int end_tile = (gmax + BN - 1) / BN;
+  const int end_tile = PIECES ? part.hi : (gmax + BN - 1) / BN, tile0 = PIECES ? part.lo : 0;
 
-  int grp = 0, fl = 0, id = 0;
+  int grp = tile0 >> 6, fl = 0, id = 0;
   uint64_t visit = 0;
   auto look = [&](int g) __attribute__((always_inline)) {
     const int t = 64 * g + lane;
-    bool v = t < end_tile;
+    bool v = t >= tile0 && t < end_tile;
     fl = (t * BN < wmax ? Tile::kMine : 0) | (t * BN + BN <= wmin ? Tile::kWhole : 0) | Tile::kOne;
     if (docs && v) {
       const int4 r = *reinterpret_cast<const int4*>(a.r.k + (size_t)b * a.kr + 2 * t);
@@ -195,6 +204,20 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
 #pragma unroll
   for (int mb = 0; mb < 4; ++mb) acc[mb] = f32x16{};
   auto rows_out = [&](float mul) __attribute__((always_inline)) {
+    if (PIECES && !part.whole()) {  // fp32 rows of this part
+      if (!qlive) return;
+      float* const p = a.dqp + ((size_t)part.slot() * a.pieces.slot_rows + (qrow - row0)) * D;
+      if (none) mul = 0.f;
+#pragma unroll
+      for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          float4 x = make_float4(acc[mb][4 * g] * mul, acc[mb][4 * g + 1] * mul, acc[mb][4 * g + 2] * mul, acc[mb][4 * g + 3] * mul);
+          if (none) x = make_float4(0.f, 0.f, 0.f, 0.f);
+          *reinterpret_cast<float4*>(p + 32 * mb + 8 * g + 4 * hi) = x;
+        }
+      return;
+    }
 #pragma unroll
     for (int mb = 0; mb < 4; ++mb)
 #pragma unroll
@@ -239,12 +262,13 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
       for (int p = 0; p < 4; ++p) sum[p & 1] = dot2(xw[p], yw[p], sum[p & 1]);
     }
     dl = wave_half_sum(sum[0] + sum[1]);
-    if (qlive && hi == 0) {
+    const bool first = !PIECES || part.lo == 0;  // of the tile's parts
+    if (first && qlive && hi == 0) {
       a.delta[lrow] = -dl;
       a.nlse[lrow] = -lse2;
     }
     const uint64_t bad = __builtin_amdgcn_ballot_w64(qlive && none);
-    if (h == 0 && lane == 0 && wrow < c.Lq) a.empty[(size_t)b * a.qr + (wrow >> 5)] = bad != 0;
+    if (first && h == 0 && lane == 0 && wrow < c.Lq) a.empty[(size_t)b * a.qr + (wrow >> 5)] = bad != 0;
   }
   __builtin_amdgcn_s_waitcnt(0);
   own_rows(qop);
@@ -255,7 +279,7 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
 
   Tile cur{-1, 0, 0}, nxt = cur;
   if (end_tile > 0) {
-    look(0);
+    look(grp);
     cur = next();
   }
   if (cur.t < 0) {  // nothing to see: dQ = 0
@@ -408,7 +432,46 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a) {
 
 template <bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT) void mod_dq_kernel(BwdArgs a) {
-  dq_body<CAP, BIAS>(a);
+  dq_body<CAP, BIAS, false>(a, Part{});
+}
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ void dq_pieces_body(const BwdArgs& a) {
+  each_part(a.c, a.pieces.n, piece_of(blockIdx.x, a.pieces.n), [&](const Part& part) __attribute__((always_inline)) {
+    if (threadIdx.x == 0) note_cut(a.pieces, a.c, part);
+    dq_body<CAP, BIAS, true>(a, part);
+    __syncthreads();  // (the staging areas)
+  });
+}
+template <bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT) void mod_dq_pieces_kernel(BwdArgs a) {
+  dq_pieces_body<CAP, BIAS>(a);
+}
+
+// dQ of the tiles that pieces have cut, the sum of their parts: 16 rows a
+// workgroup, 8 values of a row a thread.
+__global__ __launch_bounds__(256) void mod_dq_join_kernel(BwdArgs a) {
+  const int tile = blockIdx.x >> 4, sub = blockIdx.x & 15;
+  const int p0 = __builtin_amdgcn_readfirstlane(a.pieces.cut[2 * tile]);
+  if (p0 < 0) return;
+  const int p1 = __builtin_amdgcn_readfirstlane(a.pieces.cut[2 * tile + 1]);
+  const int bh = tile / a.ntile, r = 16 * sub + (threadIdx.x >> 4), i = (tile - bh * a.ntile) * BM + r;
+  if (i >= a.c.Lq) return;
+  const int b = bh / a.c.H, h = bh - b * a.c.H, ch = 8 * (threadIdx.x & 15);
+  float4 x0 = make_float4(0.f, 0.f, 0.f, 0.f), x1 = x0;
+#pragma unroll 4
+  for (int p = p0; p <= p1; ++p) {
+    const float* const src = a.dqp + ((size_t)(2 * p + (p == p0)) * a.pieces.slot_rows + r) * D + ch;
+    const float4 u = *reinterpret_cast<const float4*>(src);
+    const float4 v = *reinterpret_cast<const float4*>(src + 4);
+    x0.x += u.x; x0.y += u.y; x0.z += u.z; x0.w += u.w;
+    x1.x += v.x; x1.y += v.y; x1.z += v.z; x1.w += v.w;
+  }
+  uint4 o;
+  o.x = pack_bf16x2(x0.x, x0.y);
+  o.y = pack_bf16x2(x0.z, x0.w);
+  o.z = pack_bf16x2(x1.x, x1.y);
+  o.w = pack_bf16x2(x1.z, x1.w);
+  *reinterpret_cast<uint4*>(a.dq + (((size_t)b * a.c.Lq + i) * a.c.H + h) * D + ch) = o;
 }
 
 // ------------------------------------------------------------- dK and dV ----
@@ -797,11 +860,22 @@ hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
     a.in_run[0] = a.r.q_order ? a.ntile * c.B : a.ntile;
     a.sorted = uneven && qwg > (size_t)cus;
     a.first_most = 0;
-    const unsigned grid = (unsigned)a.nwg;
-    e = cap ? (bias ? launch_kernel(mod_dq_kernel<true, true>, grid, (unsigned)NT, stream, a)
-                    : launch_kernel(mod_dq_kernel<true, false>, grid, (unsigned)NT, stream, a))
-            : (bias ? launch_kernel(mod_dq_kernel<false, true>, grid, (unsigned)NT, stream, a)
-                    : launch_kernel(mod_dq_kernel<false, false>, grid, (unsigned)NT, stream, a));
+    unsigned grid = (unsigned)a.nwg;
+    if (s.dq.n) {
+      a.dqp = f.ws + s.part;
+      a.pieces = Pieces{s.dq.n, s.dq.slot_rows, reinterpret_cast<int32_t*>(f.ws + s.dq.cut)};
+      grid = (unsigned)s.dq.n;
+      e = cap ? (bias ? launch_kernel(mod_dq_pieces_kernel<true, true>, grid, (unsigned)NT, stream, a)
+                      : launch_kernel(mod_dq_pieces_kernel<true, false>, grid, (unsigned)NT, stream, a))
+              : (bias ? launch_kernel(mod_dq_pieces_kernel<false, true>, grid, (unsigned)NT, stream, a)
+                      : launch_kernel(mod_dq_pieces_kernel<false, false>, grid, (unsigned)NT, stream, a));
+      if (e == hipSuccess) e = launch_kernel(mod_dq_join_kernel, (unsigned)a.nwg * 16u, 256u, stream, a);
+    } else {
+      e = cap ? (bias ? launch_kernel(mod_dq_kernel<true, true>, grid, (unsigned)NT, stream, a)
+                      : launch_kernel(mod_dq_kernel<true, false>, grid, (unsigned)NT, stream, a))
+              : (bias ? launch_kernel(mod_dq_kernel<false, true>, grid, (unsigned)NT, stream, a)
+                      : launch_kernel(mod_dq_kernel<false, false>, grid, (unsigned)NT, stream, a));
+    }
     if (e != hipSuccess) return e;
   }
   if (c.Lk > 0) {

@@ -699,15 +699,15 @@ hipError_t launch_attn_mod_fwd(const ModFwd& f, hipStream_t stream) {
   hipError_t e = launch_mod_ranges(c, f.ws, !s.few && a.sorted, false, &a.r, stream);
   if (e != hipSuccess) return e;
   if (s.few) return launch_mod_few(f, s, a.r, stream);
-  if (s.pieces) {
+  if (s.pieces.n) {
     a.po = f.ws + s.part;
-    a.pl = a.po + (size_t)2 * s.pieces * s.slot_rows * D;
-    a.pieces = Pieces{s.pieces, s.slot_rows, reinterpret_cast<int32_t*>(f.ws + s.cut)};
+    a.pl = a.po + (size_t)2 * s.pieces.n * s.pieces.slot_rows * D;
+    a.pieces = Pieces{s.pieces.n, s.pieces.slot_rows, reinterpret_cast<int32_t*>(f.ws + s.pieces.cut)};
     const bool cap = c.s.cap > 0.f, bias = c.s.slopes != nullptr;
-    e = cap ? (bias ? launch_kernel(attn_mod_pieces_kernel<true, true>, (unsigned)s.pieces, (unsigned)NT, stream, a)
-                    : launch_kernel(attn_mod_pieces_kernel<true, false>, (unsigned)s.pieces, (unsigned)NT, stream, a))
-            : (bias ? launch_kernel(attn_mod_pieces_kernel<false, true>, (unsigned)s.pieces, (unsigned)NT, stream, a)
-                    : launch_kernel(attn_mod_pieces_kernel<false, false>, (unsigned)s.pieces, (unsigned)NT, stream, a));
+    e = cap ? (bias ? launch_kernel(attn_mod_pieces_kernel<true, true>, (unsigned)s.pieces.n, (unsigned)NT, stream, a)
+                    : launch_kernel(attn_mod_pieces_kernel<true, false>, (unsigned)s.pieces.n, (unsigned)NT, stream, a))
+            : (bias ? launch_kernel(attn_mod_pieces_kernel<false, true>, (unsigned)s.pieces.n, (unsigned)NT, stream, a)
+                    : launch_kernel(attn_mod_pieces_kernel<false, false>, (unsigned)s.pieces.n, (unsigned)NT, stream, a));
     if (e != hipSuccess) return e;
     const PieceJoinArgs j{a.po, a.pl, f.o, f.lse, a.pieces, c.H, c.Lq, a.ntile};
     return launch_kernel(mod_piece_join_kernel, (unsigned)(a.ntile * c.B * c.H * 16), 256u, stream, j);

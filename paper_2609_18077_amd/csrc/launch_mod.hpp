@@ -72,12 +72,57 @@ __host__ __device__ inline int key_weight(int rows) { return rows > 128 ? 4 : 3;
 // Four key tiles: every piece between a tile's first and last then holds some of it.
 constexpr int kLeastPiece = 16;
 
+struct ModPieces {
+  int n;          // 0: a workgroup takes a tile (or one of its runs)
+  int slot_rows;  // rows of a partial result
+  size_t cut;     // first value of the table of cut tiles in the workspace
+  size_t floats;  // values of the workspace
+  double us;
+};
+
+// Key tiles of query tile t, where queries stand at their default positions, and of all.
+inline int64_t mod_row_tiles(int64_t t, int Lq, int Lk, bool causal) {
+  const int64_t tiles = ((int64_t)Lk + kModKeys - 1) / kModKeys;
+  if (!causal) return tiles;
+  const int64_t last = (int64_t)Lk - Lq + ((t + 1) * kModRows < Lq ? (t + 1) * kModRows : Lq);  // keys seen by the last row
+  return last <= 0 ? 0 : last >= Lk ? tiles : (last + kModKeys - 1) / kModKeys;
+}
+inline int64_t mod_key_tiles(int Lq, int Lk, bool causal) {
+  int64_t n = 0;
+  for (int64_t t = 0; t < (int64_t)mod_tiles(Lq); ++t) n += mod_row_tiles(t, Lq, Lk, causal);
+  return n;
+}
+
+// Pieces, one a compute unit and 16 key tiles at least, 2 us a tile: 16 us to find and
+// start them and for the joining launch, and the partial rows' (of `row` floats) bytes
+// at 5 TB/s.  A workgroup finds its own by going over the tiles' weights, 64 at a time:
+// not where they are too many for that to be short.  Pieces of a head read its keys at
+// different places; where K and V of a head are more than an L2 (4 MB) that costs 15 %.
+// (Forward, 12 heads, 6144 plain: seven runs 303 us, pieces 260; causal 177 and 154;
+// 1560 rows on 32760 keys: three runs 346, pieces 413.)
+inline ModPieces mod_pieces(int B, int H, int Lq, int Lk, bool causal, int cus, size_t first, int row) {
+  ModPieces p{0, 0, 0, 0, 0.0};
+  const int64_t qt = (int64_t)mod_tiles(Lq), wgs = qt * B * H;
+  if ((qt + 63) / 64 * B > 64) return p;
+  int64_t weight = 0;  // of a head
+  for (int64_t t = 0; t < qt; ++t)
+    weight += kTileStart + mod_row_tiles(t, Lq, Lk, causal) * key_weight((int)(Lq - t * kModRows < kModRows ? Lq - t * kModRows : kModRows));
+  const int64_t all = weight * B * H, most = all / (4 * kLeastPiece);
+  const int n = (int)(most < cus ? most : cus);
+  if (n < 2 || weight > INT32_MAX) return p;
+  p.n = n;
+  p.slot_rows = (Lq < kModRows ? Lq + 31 : kModRows) / 32 * 32;
+  p.cut = first + (size_t)2 * n * p.slot_rows * row;
+  p.floats = p.cut + 2 * (size_t)wgs;
+  const int64_t parts = n + (wgs < n ? wgs : n);
+  p.us = (double)all / n / 4 * 2.0 * (Lk > 8192 ? 1.15 : 1.0) + 16.0 + (double)parts * p.slot_rows * row * 8 / 5e6;
+  return p;
+}
+
 struct ModSplit {
   bool few;
   int runs;       // of the 256-row form
-  int pieces;     // of the 256-row form; 0: a workgroup takes a tile (or one of its runs)
-  int slot_rows;  // rows of a piece's partial result
-  size_t cut;     // first value of the table of cut tiles
+  ModPieces pieces;  // of the 256-row form
   int units;      // of the form for few rows; 0: a workgroup takes a whole batch
   size_t part;    // first value of the partial results in the workspace
   size_t floats;  // values of the workspace
@@ -87,7 +132,8 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
                               size_t max_floats) {
   ModSplit r;
   r.runs = 1;
-  r.units = r.pieces = 0;
+  r.units = 0;
+  r.pieces.n = 0;
   r.floats = mod_doc_floats(B, Lq, Lk, docs);
   r.part = (r.floats + 63) / 64 * 64;
   r.few = Hkv > 0 && (int64_t)(H / Hkv) * Lq <= kFewRows;
@@ -121,16 +167,7 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
   const int64_t tiles = ((int64_t)Lk + kModKeys - 1) / kModKeys, qt = (int64_t)mod_tiles(Lq);
   const int64_t wgs = qt * B * H;
   if (qt > 4096) return r;  // (rounds enough)
-  int64_t total = tiles * qt, weight = 0;  // of a head
-  for (int64_t t = 0; t < qt; ++t) {
-    int64_t n = tiles;
-    if (causal) {
-      const int64_t last = (int64_t)Lk - Lq + ((t + 1) * kModRows < Lq ? (t + 1) * kModRows : Lq);  // keys seen by the last row
-      n = last <= 0 ? 0 : last >= Lk ? tiles : (last + kModKeys - 1) / kModKeys;
-      total -= tiles - n;
-    }
-    weight += kTileStart + n * key_weight((int)(Lq - t * kModRows < kModRows ? Lq - t * kModRows : kModRows));
-  }
+  const int64_t total = mod_key_tiles(Lq, Lk, causal);  // of a head
   auto direct = [&](int s) {
     const int64_t rounds = (wgs * s + cus - 1) / cus;
     const double per = (double)(docs ? (tiles + 2) / 3 : tiles) / s;
@@ -151,24 +188,11 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
       r.floats = need;
     }
   }
-  // Pieces, one a compute unit and 16 key tiles at least: 12 us to find and start
-  // them.  A workgroup finds its own by going over the tiles' weights, 64 at a time:
-  // not where they are too many for that to be short.  Pieces of a head read its keys
-  // at different places; where K and V of a head are more than an L2 (4 MB) that costs
-  // 15 %.  (12 heads, 6144 plain: seven runs 303 us, pieces 261; causal 175 and 155;
-  // 1560 rows on 32760 keys: three runs 346, pieces 413.)
-  const int64_t all = weight * B * H, most = all / (4 * kLeastPiece);
-  const int n = (int)(most < cus ? most : cus);
-  if (docs || n < 2 || (qt + 63) / 64 * B > 64 || weight > INT32_MAX) return r;
-  r.slot_rows = (Lq < kModRows ? Lq + 31 : kModRows) / 32 * 32;
-  const int64_t parts = n + (wgs < n ? wgs : n);
-  const size_t cut = r.part + (size_t)2 * n * r.slot_rows * 129, need = cut + 2 * (size_t)wgs;
-  const double cost = (double)all / n / 4 * 2.0 * (Lk > 8192 ? 1.15 : 1.0) + 16.0 + (double)parts * r.slot_rows * 1056 / 5e6;
-  if (need <= max_floats && cost < best) {
+  const ModPieces p = docs ? ModPieces{0, 0, 0, 0, 0.0} : mod_pieces(B, H, Lq, Lk, causal, cus, r.part, 129);
+  if (p.n && p.floats <= max_floats && p.us < best) {
     r.runs = 1;
-    r.pieces = n;
-    r.cut = cut;
-    r.floats = need;
+    r.pieces = p;
+    r.floats = p.floats;
   }
   return r;
 }
@@ -188,7 +212,8 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
 struct ModBwdSplit {
   int runs, quantum;
   size_t delta, nlse, empty, counts, part;  // first values of these in the workspace (document ranges at 0)
-  size_t least, floats;               // values of the workspace: for one run, for `runs`
+  size_t least, floats;  // values of the workspace: for one run and whole query tiles, for this
+  ModPieces dq;          // of the query side (its partial sums lie where the key side's come later)
 };
 
 // Tiles of the stream of key tile t, where queries stand at their default positions.
@@ -209,6 +234,7 @@ inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool doc
   r.counts = r.empty + (size_t)B * mod_ranges(Lq);
   r.least = r.floats = r.counts + (size_t)B * mod_tiles(Lk);
   r.part = up(r.least);
+  r.dq.n = 0;
   if (B == 0 || H == 0 || Lq == 0 || Lk == 0) return r;
   const int kt = (int)mod_tiles(Lk);
   const int64_t heads = (int64_t)B * Hkv;
@@ -258,6 +284,18 @@ inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool doc
     else lo = q + 1;
   }
   consider(lo);
+  // Query side: 256-row workgroups with all of their keys (as in the forward, 2 us a
+  // tile and 4 to start and end), or pieces.
+  const int64_t qt = (int64_t)mod_tiles(Lq), wgs = qt * B * H;
+  if (docs || qt > 4096) return r;
+  const int64_t tiles = ((int64_t)Lk + kModKeys - 1) / kModKeys, rounds = (wgs + cus - 1) / cus;
+  const double mean = 1.05 * (double)mod_key_tiles(Lq, Lk, causal) * B * H / cus;
+  const double load = causal ? (mean > tiles ? mean : tiles) : (double)rounds * tiles;
+  const ModPieces p = mod_pieces(B, H, Lq, Lk, causal, cus, r.part, 128);
+  if (p.n && p.floats <= max_floats && p.us < load * 2.0 + rounds * 4.0) {
+    r.dq = p;
+    if (p.floats > r.floats) r.floats = p.floats;
+  }
   return r;
 }
 

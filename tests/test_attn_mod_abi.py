@@ -12,6 +12,7 @@ import numpy as np
 import pytest
 
 import paper_2609_18077_amd as vx
+from tests.test_gpu_attn_mod import PIECES
 
 INV, UNS = 1, 2
 P = 1 << 40  # fake device addresses, far apart, never dereferenced
@@ -120,12 +121,12 @@ using namespace vidax;
 extern "C" void fwd(int B, int H, int Hkv, int Lq, int Lk, int docs, int causal, int lens, int cus, size_t most, int64_t* o) {
   const ModSplit s = mod_fwd_split(B, H, Hkv, Lq, Lk, docs, causal, lens, cus, most);
   o[0] = s.few; o[1] = s.runs; o[2] = s.units; o[3] = s.part; o[4] = s.floats;
-  o[5] = s.pieces; o[6] = s.slot_rows; o[7] = s.cut;
+  o[5] = s.pieces.n; o[6] = s.pieces.slot_rows; o[7] = s.pieces.cut;
 }
 extern "C" void bwd(int B, int H, int Hkv, int Lq, int Lk, int docs, int causal, int cus, size_t most, int64_t* o) {
   const ModBwdSplit s = mod_bwd_split(B, H, Hkv, Lq, Lk, docs, causal, cus, most);
   o[0] = s.runs; o[1] = s.quantum; o[2] = s.delta; o[3] = s.nlse; o[4] = s.empty; o[5] = s.counts; o[6] = s.part;
-  o[7] = s.least; o[8] = s.floats;
+  o[7] = s.least; o[8] = s.floats; o[9] = s.dq.n; o[10] = s.dq.slot_rows; o[11] = s.dq.cut;
 }
 extern "C" void block(int B, int L, int C, int64_t* o) {
   const BlockShape s = block_bwd_shape(B, L, C);
@@ -148,7 +149,7 @@ def rules(tmp_path_factory):
     lib = ctypes.CDLL(str(lib))
 
     def call(name, *a):
-        out = (ctypes.c_int64 * 10)()
+        out = (ctypes.c_int64 * 12)()
         f = getattr(lib, name)
         f.argtypes = [ctypes.c_int] * (len(a) - (name != "block")) + [ctypes.c_size_t] * (name != "block") + [ctypes.c_void_p]
         f.restype = None
@@ -192,8 +193,6 @@ def test_forward_split_fits_its_workspace(rules):
                 least = rules("fwd", B, H, Hkv, Lq, Lk, docs, causal, 1, 256, doc)[:6]
                 assert least[1] == 1 and least[2] == 0 and least[4] == doc and least[5] == 0
     assert cuts > 20
-    from tests.test_gpu_attn_mod import PIECES
-
     for B, H, Hkv, Lq, Lk, mask in PIECES:
         assert rules("fwd", B, H, Hkv, Lq, Lk, 0, mask not in ("all", "valid"), 1, 256, ALL)[5] > 0
 
@@ -245,24 +244,34 @@ def test_pieces_cover_every_tile_once():
 
 
 def test_backward_split_fits_its_workspace(rules):
+    cuts = 0
     for B, H, Hkv, Lq, Lk in _shapes():
         for docs in (0, 1):
             for causal in (0, 1):
-                runs, quantum, delta, nlse, empty, counts, part, least, floats = rules("bwd", B, H, Hkv, Lq, Lk, docs, causal, 256,
-                                                                                       ALL)[:9]
+                (runs, quantum, delta, nlse, empty, counts, part, least, floats, pieces, slot_rows,
+                 cut) = rules("bwd", B, H, Hkv, Lq, Lk, docs, causal, 256, ALL)
                 doc = B * (4 * (-(-Lk // 64) + -(-Lq // 64)) + -(-Lk // 256) + -(-Lq // 256)) if docs else 0
                 rows = B * H * Lq
                 assert doc <= delta and delta + rows <= nlse and nlse + rows <= empty
                 assert empty + B * 2 * -(-Lq // 64) <= counts and counts + B * -(-Lk // 256) <= least <= part
                 assert all(x % 64 == 0 for x in (delta, nlse, empty, part))
                 assert least <= doc + 2 * rows + B * (2 * -(-Lq // 64) + -(-Lk // 256)) + 256  # as the header says
-                assert 1 <= runs <= 16 and floats == (part + runs * 2 * B * Lk * Hkv * 128 if runs > 1 else least)
+                need = part + runs * 2 * B * Lk * Hkv * 128 if runs > 1 else least
+                if pieces:
+                    cuts += 1
+                    assert not docs and pieces <= 256 and slot_rows == min(256, -(-Lq // 32) * 32)
+                    assert cut == part + 2 * pieces * slot_rows * 128
+                    need = max(need, cut + 2 * B * H * -(-Lq // 256))
+                assert 1 <= runs <= 16 and floats == need
                 assert runs == 1 or 2 * runs * B * Lk * Hkv * 128 <= 96 << 20
                 if not docs:  # the longest stream's runs cover it
                     longest = H // Hkv * (-(-Lq // 64) - (max(Lq - Lk, 0) // 64 if causal else 0))
                     assert runs * quantum >= longest
-                one = rules("bwd", B, H, Hkv, Lq, Lk, docs, causal, 256, least)[:9]
-                assert one[0] == 1 and one[8] == least
+                one = rules("bwd", B, H, Hkv, Lq, Lk, docs, causal, 256, least)
+                assert one[0] == 1 and one[8] == least and one[9] == 0
+    assert cuts > 20
+    for B, H, Hkv, Lq, Lk, mask in PIECES:
+        assert rules("bwd", B, H, Hkv, Lq, Lk, 0, mask != "all", 256, ALL)[9] > 0
 
 
 def test_block_runs_cover_every_token(rules):

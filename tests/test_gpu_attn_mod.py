@@ -292,14 +292,12 @@ PIECES = [(3, 16, 4, 296, 3993, "all"), (3, 16, 4, 532, 2375, "valid"), (2, 8, 2
           (1, 8, 2, 4001, 4001, "prefix"), (3, 4, 1, 2934, 5374, "lengths")]
 
 
-@pytest.mark.parametrize("B,H,Hkv,Lq,Lk,mask", PIECES)
-def test_pieces_of_tiles_are_joined(B, H, Hkv, Lq, Lk, mask):
-    """Checked on two heads of every batch; (2814 on 2526: rows and a tile that see nothing)."""
-    import torch
-
-    q, k, v = make(B, H, Hkv, Lq, Lk, Lq + Lk)
-    s = dict(cap=20.0, slopes=list(0.01 * np.arange(H))) if mask in ("lengths", "prefix") else {}
-    if mask != "all" and mask != "valid":
+def piece_score(B, H, Lq, Lk, mask):
+    """What changes the scores, and the slopes as float64 (or None)."""
+    s = {}
+    if mask in ("lengths", "prefix"):
+        s = dict(cap=20.0, slopes=list(0.01 * np.arange(H)))
+    if mask not in ("all", "valid"):
         s["causal"] = True
     if mask == "valid":
         s["kv_valid_len"] = [0, Lk, 700][:B]
@@ -307,13 +305,23 @@ def test_pieces_of_tiles_are_joined(B, H, Hkv, Lq, Lk, mask):
         s["prefix_len"] = [1500]
     if mask == "lengths":
         s |= dict(q_start=[-1000, 300, Lk - Lq], kv_valid_len=[1900, 3000, Lk], prefix_len=[0, 900, 70])
-    score, spec = dev_score(**s)
+    return s, np.asarray(s["slopes"], np.float32).astype(np.float64) if "slopes" in s else None
+
+
+@pytest.mark.parametrize("B,H,Hkv,Lq,Lk,mask", PIECES)
+def test_pieces_of_tiles_are_joined(B, H, Hkv, Lq, Lk, mask):
+    """Checked on two heads of every batch (2814 on 2526: rows and a tile that see nothing)."""
+    import torch
+
+    q, k, v = make(B, H, Hkv, Lq, Lk, Lq + Lk)
+    s, slopes = piece_score(B, H, Lq, Lk, mask)
+    score, _ = dev_score(**s)
     o, lse = vx.attn_mod_fwd(q, k, v, score, return_lse=True)
     again = vx.attn_mod_fwd(q, k, v, score, return_lse=True, workspace=torch.full((1 << 25,), float("nan"), device="cuda"))
     assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
     for h in (0, H - 1):
         hs, ks = slice(h, h + 1), slice(h * Hkv // H, h * Hkv // H + 1)
-        one = oracle.ScoreSpec(**{**s, **({"slopes": np.asarray(s["slopes"], np.float32)[hs].astype(np.float64)} if "slopes" in s else {})})
+        one = oracle.ScoreSpec(**{**s, "slopes": slopes[hs] if slopes is not None else None})
         compare(o[:, :, hs], lse[:, hs], q[:, :, hs], k[:, :, ks], v[:, :, ks], SCALE, one, f"pieces {Lq}x{Lk} {mask} head {h}")
 
 

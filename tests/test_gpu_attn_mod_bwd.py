@@ -18,7 +18,7 @@ import pytest
 import oracle
 import paper_2609_18077_amd as vx
 from tests.gpu_util import log
-from tests.test_gpu_attn_mod import D, HALF, MASKS, RMS, SCALE, deltas, dev_score, f64, make, masks
+from tests.test_gpu_attn_mod import D, HALF, MASKS, PIECES, RMS, SCALE, deltas, dev_score, f64, make, masks, piece_score
 
 pytestmark = pytest.mark.gpu
 
@@ -52,7 +52,11 @@ def check(q, k, v, scale=None, what="", workspace=None, dout=None, **s):
     o, lse = vx.attn_mod_fwd(q, k, v, score, scale=scale, return_lse=True)
     got = vx.attn_mod_bwd(q, k, v, o, dout, lse, score, scale=scale, workspace=workspace)
     torch.cuda.synchronize()
-    sc = SCALE if scale is None else float(np.float32(scale))
+    compare(got, o, dout, q, k, v, SCALE if scale is None else float(np.float32(scale)), spec, what)
+    return o, lse, dout, got
+
+
+def compare(got, o, dout, q, k, v, sc, spec, what):
     args = [f64(t) for t in (q, k, v)]
     ref = oracle.attn_mod_bwd_ref(*args, f64(dout), sc, spec, o_saved=f64(o))
     mags = _absolute(*args, f64(o), f64(dout), sc, spec)
@@ -68,7 +72,6 @@ def check(q, k, v, scale=None, what="", workspace=None, dout=None, **s):
         log(f"  {what} {n}: worst/bound {worst:.3f}, rel rms {rms:.2e}")
         assert worst <= 1, (what, n, worst)
         assert norm < 1e-20 or rms <= RMS, (what, n, rms)
-    return o, lse, dout, got
 
 
 @pytest.mark.parametrize("mask", MASKS)
@@ -118,6 +121,28 @@ def test_runs_of_queries_are_added_up(Lq, Lk, Hkv):
     score, _ = dev_score(**s)
     with pytest.raises(vx.VidaxError):
         vx.attn_mod_bwd(q, k, v, o, dout, lse, score, workspace=ws[:B * H * Lq])
+
+
+@pytest.mark.parametrize("B,H,Hkv,Lq,Lk,mask", PIECES)
+def test_pieces_of_tiles_are_added_up(B, H, Hkv, Lq, Lk, mask):
+    """Checked on two groups of heads of every batch."""
+    import torch
+
+    q, k, v = make(B, H, Hkv, Lq, Lk, Lq + Lk)
+    s, slopes = piece_score(B, H, Lq, Lk, mask)
+    score, _ = dev_score(**s)
+    dout = make(B, H, Hkv, Lq, 1, 7)[0]
+    o, lse = vx.attn_mod_fwd(q, k, v, score, return_lse=True)
+    got = vx.attn_mod_bwd(q, k, v, o, dout, lse, score)
+    ws = torch.full((vx.lib().vidax_attn_mod_bwd_workspace_floats(B, H, Hkv, Lq, Lk, D, 0),), float("nan"), device="cuda")
+    for a, b in zip(got, vx.attn_mod_bwd(q, k, v, o, dout, lse, score, workspace=ws)):
+        assert torch.equal(a, b)
+    rep = H // Hkv
+    for g in {0, Hkv - 1}:
+        hs, ks = slice(g * rep, g * rep + rep), slice(g, g + 1)
+        one = oracle.ScoreSpec(**{**s, "slopes": slopes[hs] if slopes is not None else None})
+        compare([got[0][:, :, hs], got[1][:, :, ks], got[2][:, :, ks]], o[:, :, hs], dout[:, :, hs], q[:, :, hs], k[:, :, ks],
+                v[:, :, ks], SCALE, one, f"pieces {Lq}x{Lk} {mask} group {g}")
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])

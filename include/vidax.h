@@ -326,9 +326,10 @@ typedef struct vidax_score_desc {
  *   workspace: fp32 device memory, 16-byte aligned.  With documents at least
  *          B (4 ceil(Lk / 64) + 4 ceil(Lq / 64) + ceil(Lk / 256) + ceil(Lq / 256))
  *          values (VIDAX_ERR_INVALID_ARG below); otherwise NULL is allowed.  With at least
- *          vidax_attn_mod_fwd_workspace_floats(...) values, calls of few query
- *          rows cut the keys into runs that work side by side; with fewer they
- *          take the runs that fit.  The result differs by fp32 rounding only.
+ *          vidax_attn_mod_fwd_workspace_floats(...) values, calls of few or uneven
+ *          query tiles cut their keys into parts that work side by side, and join
+ *          them in a further launch; with fewer they take the parts that fit.  The
+ *          result differs by fp32 rounding only.
  * What lies in k and v where no query of the call can see it (past
  * kv_valid_len, behind the last query's position, at keys of negative documents)
  * never reaches an output, whatever it holds; k and v of the other keys must be
@@ -363,10 +364,10 @@ size_t vidax_attn_mod_fwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, in
  *   lse      : fp32 [B, H, Lq], as the forward returned it with the same arguments
  *              (o is its output).
  *   workspace: fp32 device memory, required.  With
- *              vidax_attn_mod_bwd_workspace_floats(...) values the key side may cut
- *              the query stream into runs that work side by side, their fp32 sums
- *              added in a further launch (at most 384 MiB); with fewer it takes the
- *              runs that fit; VIDAX_ERR_INVALID_ARG below what one run needs,
+ *              vidax_attn_mod_bwd_workspace_floats(...) values calls of few or uneven
+ *              tiles are cut into parts that work side by side, their fp32 sums added
+ *              in further launches (at most 384 MiB); with fewer it takes what fits;
+ *              VIDAX_ERR_INVALID_ARG below what whole tiles need,
  *              2 B H Lq + B (2 ceil(Lq / 64) + ceil(Lk / 256)) + 256 values and, with
  *              documents, those of the forward more.
  * Same call, same bits: no atomics.  Products on bf16 inputs (P and ds rounded to

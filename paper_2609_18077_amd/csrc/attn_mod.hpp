@@ -176,52 +176,70 @@ __device__ __forceinline__ void place(const A& a, int heads, const int32_t* orde
   h = bh - b * heads;
 }
 
-// ---- equal pieces of all the key tiles of all query tiles (no documents)
+// ---- equal pieces of the streams of all 256-row tiles (no documents)
 //
-// The query tiles' key tiles, behind one another (batch, head, query tile, key
-// tile), are one sequence, cut into `pieces` of equal weight, a workgroup each; a
-// piece may end one query tile, hold some whole and begin another.  A query tile
-// that is cut leaves partial results, at most two a piece (slots 2 p: a part that
-// does not begin the tile, 2 p + 1: one that does), which a further launch joins.
+// The tiles that the workgroups' tiles visit, behind one another (batch, head, own
+// tile, visited tile), are one sequence, cut into pieces of equal weight, a
+// workgroup each; a piece may end one own tile, hold some whole and begin another.
+// An own tile that is cut leaves partial results, at most two a piece (slots 2 p: a
+// part that does not begin the tile, 2 p + 1: one that does), which a further launch
+// joins.
 struct Pieces {
   int n;         // 0: not in pieces
   int slot_rows; // rows of a slot
   int32_t* cut;  // [B][H][tiles][2]: first (-1: not cut) and last piece of a tile
 };
 struct Part {
-  int b, h, t;    // query tile
-  int n, lo, hi;  // its key tiles, and this part of them
+  int b, h, t;    // own tile
+  int n, lo, hi;  // the tiles it visits, and this part of them
   int piece;
   __device__ __forceinline__ bool whole() const { return lo == 0 && hi == n; }
   __device__ __forceinline__ int slot() const { return 2 * piece + (lo == 0); }
 };
 
-// Key tiles of query tile t.
-__device__ __forceinline__ int key_tiles(const ModCall& c, const Batch& bt, int t) {
-  return (key_limit(bt, c.s.causal, bt.start + min((t + 1) * kModRows, c.Lq) - 1) + kModKeys - 1) / kModKeys;
+// Own tiles of queries, which visit key tiles.
+struct QuerySide {
+  static __device__ __forceinline__ int length(const ModCall& c) { return c.Lq; }
+  static __device__ __forceinline__ int heads(const ModCall& c) { return c.H; }
+  static __device__ __forceinline__ int visits(const ModCall& c, const Batch& bt, int t) {
+    return (key_limit(bt, c.s.causal, bt.start + min((t + 1) * kModRows, c.Lq) - 1) + kModKeys - 1) / kModKeys;
+  }
+};
+// Own tiles of keys, which visit the query tiles [first_query_tile, end) of every
+// query head of theirs.
+__device__ __forceinline__ int first_query_tile(const ModCall& c, const Batch& bt, int key0) {
+  const int end = (c.Lq + kModKeys - 1) / kModKeys;
+  if (key0 >= key_limit(bt, c.s.causal, bt.start + c.Lq - 1)) return end;
+  return c.s.causal && key0 >= bt.prefix ? min(max(key0 - bt.start, 0) / kModKeys, end) : 0;
 }
-__device__ __forceinline__ int tile_weight(const ModCall& c, const Batch& bt, int t) {
-  return kTileStart + key_tiles(c, bt, t) * key_weight(min(c.Lq - t * kModRows, kModRows));
-}
+struct KeySide {
+  static __device__ __forceinline__ int length(const ModCall& c) { return c.Lk; }
+  static __device__ __forceinline__ int heads(const ModCall& c) { return c.Hkv; }
+  static __device__ __forceinline__ int visits(const ModCall& c, const Batch& bt, int t) {
+    return c.H / c.Hkv * ((c.Lq + kModKeys - 1) / kModKeys - first_query_tile(c, bt, t * kModRows));
+  }
+};
 
 // f(part) for every part of piece p, in order.  All waves alike.
-template <typename F>
+template <typename Side, typename F>
 __device__ __forceinline__ void each_part(const ModCall& c, int pieces, int p, F&& f) {
-  const int lane = threadIdx.x & 63, nt = (int)mod_tiles(c.Lq);
+  const int lane = threadIdx.x & 63, len = Side::length(c), heads = Side::heads(c), nt = (int)mod_tiles(len);
+  auto unit = [&](int t) { return key_weight(min(len - t * kModRows, kModRows)); };
+  auto tile_weight = [&](const Batch& bt, int t) { return kTileStart + Side::visits(c, bt, t) * unit(t); };
   const bool lens = c.s.kv_valid_len || c.s.q_start || c.s.prefix_len;
   auto head_weight = [&](const Batch& bt) {
     int w = 0;
-    for (int t = lane; t < nt; t += 64) w += tile_weight(c, bt, t);
+    for (int t = lane; t < nt; t += 64) w += tile_weight(bt, t);
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) w += __shfl_xor(w, m);
     return __builtin_amdgcn_readfirstlane(w);
   };
   Batch bt = batch_of(c, 0);
   int hw = head_weight(bt);
-  int64_t total = (int64_t)hw * c.H * c.B;
+  int64_t total = (int64_t)hw * heads * c.B;
   if (lens) {
-    total = (int64_t)hw * c.H;
-    for (int b = 1; b < c.B; ++b) total += (int64_t)head_weight(batch_of(c, b)) * c.H;
+    total = (int64_t)hw * heads;
+    for (int b = 1; b < c.B; ++b) total += (int64_t)head_weight(batch_of(c, b)) * heads;
   }
   int64_t per = (total + pieces - 1) / pieces;
   if (per < kLeastPiece) per = kLeastPiece;
@@ -231,15 +249,15 @@ __device__ __forceinline__ void each_part(const ModCall& c, int pieces, int p, F
   int64_t S = 0;  // where the tile begins
   int b = 0;
   if (lens) {
-    while (pos >= S + (int64_t)hw * c.H) {  // (ends: pos < total)
-      S += (int64_t)hw * c.H;
+    while (pos >= S + (int64_t)hw * heads) {  // (ends: pos < total)
+      S += (int64_t)hw * heads;
       bt = batch_of(c, ++b);
       hw = head_weight(bt);
     }
   } else {
-    b = (int)(pos / ((int64_t)hw * c.H));
+    b = (int)(pos / ((int64_t)hw * heads));
     bt = batch_of(c, b);
-    S = (int64_t)hw * c.H * b;
+    S = (int64_t)hw * heads * b;
   }
   int h = (int)((pos - S) / hw);
   S += (int64_t)h * hw;
@@ -248,7 +266,7 @@ __device__ __forceinline__ void each_part(const ModCall& c, int pieces, int p, F
     const int rem = (int)(pos - S);
     int before = 0;
     for (int t0 = 0; t0 < nt; t0 += 64) {
-      const int w = t0 + lane < nt ? tile_weight(c, bt, t0 + lane) : 0;
+      const int w = t0 + lane < nt ? tile_weight(bt, t0 + lane) : 0;
       int x = w;
 #pragma unroll
       for (int m = 1; m < 64; m <<= 1) {
@@ -266,21 +284,21 @@ __device__ __forceinline__ void each_part(const ModCall& c, int pieces, int p, F
     }
   }
   for (;;) {
-    const int n = key_tiles(c, bt, t), u = key_weight(min(c.Lq - t * kModRows, kModRows));
-    // the key tile at a position; not within two of either end
-    auto key_at = [&](int64_t x) {
+    const int n = Side::visits(c, bt, t), u = unit(t);
+    // the visited tile at a position; not within two of either end
+    auto tile_at = [&](int64_t x) {
       const int64_t y = x - S - kTileStart;
       if (y >= (int64_t)n * u) return n;
       const int k = y <= 0 ? 0 : (int)y / u;
       return k < 2 ? 0 : k > n - 2 ? n : k;
     };
-    const Part part{b, h, t, n, key_at(pos), key_at(end), p};
+    const Part part{b, h, t, n, tile_at(pos), tile_at(end), p};
     if (part.lo < part.hi || (n == 0 && pos <= S)) f(part);
     S += kTileStart + n * u;
     if (S >= end) return;
     if (++t == nt) {
       t = 0;
-      if (++h == c.H) {
+      if (++h == heads) {
         h = 0;
         bt = batch_of(c, ++b);
       }
@@ -288,8 +306,9 @@ __device__ __forceinline__ void each_part(const ModCall& c, int pieces, int p, F
   }
 }
 // What the join has to know of a tile, noted by whoever begins or ends it.
+template <typename Side>
 __device__ __forceinline__ void note_cut(const Pieces& x, const ModCall& c, const Part& part) {
-  int32_t* const p = x.cut + (((size_t)part.b * c.H + part.h) * mod_tiles(c.Lq) + part.t) * 2;
+  int32_t* const p = x.cut + (((size_t)part.b * Side::heads(c) + part.h) * mod_tiles(Side::length(c)) + part.t) * 2;
   if (part.lo == 0) p[0] = part.whole() ? -1 : part.piece;
   else if (part.hi == part.n) p[1] = part.piece;
 }

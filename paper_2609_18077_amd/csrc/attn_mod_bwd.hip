@@ -436,8 +436,8 @@ __global__ __launch_bounds__(NT) void mod_dq_kernel(BwdArgs a) {
 }
 template <bool CAP, bool BIAS>
 __device__ __forceinline__ void dq_pieces_body(const BwdArgs& a) {
-  each_part(a.c, a.pieces.n, piece_of(blockIdx.x, a.pieces.n), [&](const Part& part) __attribute__((always_inline)) {
-    if (threadIdx.x == 0) note_cut(a.pieces, a.c, part);
+  each_part<QuerySide>(a.c, a.pieces.n, piece_of(blockIdx.x, a.pieces.n), [&](const Part& part) __attribute__((always_inline)) {
+    if (threadIdx.x == 0) note_cut<QuerySide>(a.pieces, a.c, part);
     dq_body<CAP, BIAS, true>(a, part);
     __syncthreads();  // (the staging areas)
   });
@@ -476,8 +476,9 @@ __global__ __launch_bounds__(256) void mod_dq_join_kernel(BwdArgs a) {
 
 // ------------------------------------------------------------- dK and dV ----
 
-template <bool CAP, bool BIAS>
-__global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
+// PIECES: the part of a key tile's stream given.
+template <bool CAP, bool BIAS, bool PIECES>
+__device__ __forceinline__ void dkdv_body(const BwdArgs& a, const Part& part) {
   __shared__ __attribute__((aligned(1024))) uint16_t Q0[TILE], Q1[TILE], O0[TILE], O1[TILE];
   __shared__ __attribute__((aligned(16))) uint16_t KB[NW * 32 * D];
   __shared__ __attribute__((aligned(16))) float Lt[2][BN], Dt[2][BN];
@@ -486,7 +487,14 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const ModCall& c = a.c;
   int b, hk, kt, run;
-  place(a, c.Hkv, a.r.k_order, run, kt, b, hk);
+  if constexpr (PIECES) {
+    b = part.b;
+    hk = part.h;
+    kt = part.t;
+    run = 0;
+  } else {
+    place(a, c.Hkv, a.r.k_order, run, kt, b, hk);
+  }
   const int rep = c.H / c.Hkv;
   const int qtok = c.H * D, qbytes = qtok * 2, ktok = c.Hkv * D, kbytes = ktok * 2;
   const Batch bt = batch_of(c, b);
@@ -494,7 +502,7 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
   const int key0 = kt * BM, wkey = key0 + wave * 32, krow = wkey + l32;
   int kd = 0;
   Docs wdoc{0, 0, false}, gdoc{0, 0, false};
-  const bool docs = a.r.k != nullptr;
+  const bool docs = !PIECES && a.r.k != nullptr;
   if (docs) {
     if (krow < c.Lk) kd = c.s.k_doc[(size_t)b * c.Lk + krow];
     const int2* const kr = a.r.k + (size_t)b * a.kr;
@@ -512,9 +520,7 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
   // query tiles of a head that may see a key of the workgroup lie in [qa, qb); the
   // stream: those of the group's heads in turn, this run's part of it
   const int qb = (c.Lq + BN - 1) / BN;
-  int qa = 0;
-  if (c.s.causal && key0 >= bt.prefix) qa = min(max(key0 - bt.start, 0) / BN, qb);
-  if (key0 >= used) qa = qb;
+  const int qa = first_query_tile(c, bt, key0);
   // first row that sees the lane's key, by position (-2^31: all, prefix)
   const int rmin = !c.s.causal || krow < bt.prefix ? INT32_MIN : krow - bt.start;
   const int wrmax = !c.s.causal || wend - 1 < bt.prefix ? INT32_MIN : wend - 1 - bt.start;  // first row that sees all of the wave's
@@ -568,9 +574,14 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
       n += __builtin_popcountll(visit);
     }
   }
-  const int cuts = max(1, min(a.runs, (int)(((int64_t)n * rep + a.quantum - 1) / a.quantum)));
-  if (run >= cuts) return;
-  if (run == 0 && hk == 0 && tid == 0) a.counts[b * a.ntile + kt] = cuts;
+  int cuts = 1;
+  if constexpr (PIECES) {
+    cuts = part.whole() ? 1 : 2;
+  } else {
+    cuts = max(1, min(a.runs, (int)(((int64_t)n * rep + a.quantum - 1) / a.quantum)));
+    if (run >= cuts) return;
+    if (run == 0 && hk == 0 && tid == 0) a.counts[b * a.ntile + kt] = cuts;
+  }
 
   f32x16 dk[4], dv[4];
 #pragma unroll
@@ -578,8 +589,12 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
   auto partials_out = [&]() __attribute__((always_inline)) {
     if (krow >= c.Lk) return;
     const size_t rowoff = ((size_t)b * c.Lk + krow) * ktok + (size_t)hk * D, n = (size_t)c.B * c.Lk * ktok;
-    float* const pk = a.part + (size_t)run * n + rowoff;
-    float* const pv = a.part + (size_t)(a.runs + run) * n + rowoff;
+    float* pk = a.part + (size_t)run * n + rowoff;
+    float* pv = a.part + (size_t)(a.runs + run) * n + rowoff;
+    if constexpr (PIECES) {  // [slots][2][slot_rows][D]
+      pk = a.part + ((size_t)2 * part.slot() * a.pieces.slot_rows + (krow - key0)) * D;
+      pv = pk + (size_t)a.pieces.slot_rows * D;
+    }
 #pragma unroll
     for (int mb = 0; mb < 4; ++mb)
 #pragma unroll
@@ -755,7 +770,8 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
   Tile cur{-1, 0, 0}, nxt = cur;
   int cur_head = 0;
   if (n > 0) {
-    const int64_t i0 = (int64_t)n * rep * run / cuts, i1 = (int64_t)n * rep * (run + 1) / cuts;
+    const int64_t i0 = PIECES ? part.lo : (int64_t)n * rep * run / cuts;
+    const int64_t i1 = PIECES ? part.hi : (int64_t)n * rep * (run + 1) / cuts;
     g = (int)(i0 / n);
     left = (int)(i1 - i0);
     int skip = (int)(i0 - (int64_t)g * n);
@@ -798,6 +814,51 @@ __global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
   rows_out(a.dv, dv, 1.f, area);
 }
 
+template <bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT) void mod_dkdv_kernel(BwdArgs a) {
+  dkdv_body<CAP, BIAS, false>(a, Part{});
+}
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ void dkdv_pieces_body(const BwdArgs& a) {
+  each_part<KeySide>(a.c, a.pieces.n, piece_of(blockIdx.x, a.pieces.n), [&](const Part& part) __attribute__((always_inline)) {
+    if (threadIdx.x == 0) note_cut<KeySide>(a.pieces, a.c, part);
+    dkdv_body<CAP, BIAS, true>(a, part);
+    __syncthreads();  // (the tile buffers)
+  });
+}
+template <bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT) void mod_dkdv_pieces_kernel(BwdArgs a) {
+  dkdv_pieces_body<CAP, BIAS>(a);
+}
+
+// dK, dV of the tiles that pieces have cut, the sum of their parts: 16 rows of one
+// of them a workgroup, 8 values of a row a thread.
+__global__ __launch_bounds__(256) void mod_dkdv_join_kernel(BwdArgs a) {
+  const int tile = blockIdx.x >> 5, isv = blockIdx.x >> 4 & 1, sub = blockIdx.x & 15;
+  const int p0 = __builtin_amdgcn_readfirstlane(a.pieces.cut[2 * tile]);
+  if (p0 < 0) return;
+  const int p1 = __builtin_amdgcn_readfirstlane(a.pieces.cut[2 * tile + 1]);
+  const int bh = tile / a.ntile, r = 16 * sub + (threadIdx.x >> 4), j = (tile - bh * a.ntile) * BM + r;
+  if (j >= a.c.Lk) return;
+  const int b = bh / a.c.Hkv, h = bh - b * a.c.Hkv, ch = 8 * (threadIdx.x & 15);
+  float4 x0 = make_float4(0.f, 0.f, 0.f, 0.f), x1 = x0;
+#pragma unroll 4
+  for (int p = p0; p <= p1; ++p) {
+    const float* const src = a.part + ((size_t)(2 * (2 * p + (p == p0)) + isv) * a.pieces.slot_rows + r) * D + ch;
+    const float4 u = *reinterpret_cast<const float4*>(src);
+    const float4 v = *reinterpret_cast<const float4*>(src + 4);
+    x0.x += u.x; x0.y += u.y; x0.z += u.z; x0.w += u.w;
+    x1.x += v.x; x1.y += v.y; x1.z += v.z; x1.w += v.w;
+  }
+  const float m = isv ? 1.f : a.c.scale;
+  uint4 o;
+  o.x = pack_bf16x2(x0.x * m, x0.y * m);
+  o.y = pack_bf16x2(x0.z * m, x0.w * m);
+  o.z = pack_bf16x2(x1.x * m, x1.y * m);
+  o.w = pack_bf16x2(x1.z * m, x1.w * m);
+  *reinterpret_cast<uint4*>((isv ? a.dv : a.dk) + (((size_t)b * a.c.Lk + j) * a.c.Hkv + h) * D + ch) = o;
+}
+
 // dK = scale * sum of the runs' partials, dV = their sum, for the tiles that were
 // cut: 8 values a thread.
 __global__ __launch_bounds__(256) void mod_reduce_kernel(BwdArgs a) {
@@ -832,8 +893,8 @@ __global__ __launch_bounds__(256) void mod_reduce_kernel(BwdArgs a) {
 hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
   const ModCall& c = f.c;
   const int cus = device_cu_count();
-  const ModBwdSplit s = mod_bwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr, c.s.causal != 0, cus,
-                                      f.ws_floats);
+  const ModBwdSplit s = mod_bwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr, c.s.causal != 0,
+                                      c.s.kv_valid_len || c.s.prefix_len || c.s.q_start, cus, f.ws_floats);
   BwdArgs a;
   a.c = c;
   a.sc = make_scores(c);
@@ -878,7 +939,16 @@ hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
     }
     if (e != hipSuccess) return e;
   }
-  if (c.Lk > 0) {
+  if (c.Lk > 0 && s.dkdv.n) {
+    a.ntile = (c.Lk + BM - 1) / BM;
+    a.pieces = Pieces{s.dkdv.n, s.dkdv.slot_rows, reinterpret_cast<int32_t*>(f.ws + s.dkdv.cut)};
+    const unsigned grid = (unsigned)s.dkdv.n;
+    e = cap ? (bias ? launch_kernel(mod_dkdv_pieces_kernel<true, true>, grid, (unsigned)NT, stream, a)
+                    : launch_kernel(mod_dkdv_pieces_kernel<true, false>, grid, (unsigned)NT, stream, a))
+            : (bias ? launch_kernel(mod_dkdv_pieces_kernel<false, true>, grid, (unsigned)NT, stream, a)
+                    : launch_kernel(mod_dkdv_pieces_kernel<false, false>, grid, (unsigned)NT, stream, a));
+    if (e == hipSuccess) e = launch_kernel(mod_dkdv_join_kernel, (unsigned)(a.ntile * c.B * c.Hkv * 32), 256u, stream, a);
+  } else if (c.Lk > 0) {
     a.ntile = (c.Lk + BM - 1) / BM;
     a.runs = s.runs;
     // Workgroups that would find no part of their tile's stream are not launched

@@ -457,8 +457,8 @@ __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
 }
 template <bool CAP, bool BIAS>
 __device__ __forceinline__ void pieces_body(const FwdArgs& a) {
-  each_part(a.c, a.pieces.n, piece_of(blockIdx.x, a.pieces.n), [&](const Part& part) __attribute__((always_inline)) {
-    if (threadIdx.x == 0) note_cut(a.pieces, a.c, part);
+  each_part<QuerySide>(a.c, a.pieces.n, piece_of(blockIdx.x, a.pieces.n), [&](const Part& part) __attribute__((always_inline)) {
+    if (threadIdx.x == 0) note_cut<QuerySide>(a.pieces, a.c, part);
     fwd_body<CAP, BIAS, true>(a, part);
     __syncthreads();  // (the staging areas)
   });

@@ -93,29 +93,31 @@ inline int64_t mod_key_tiles(int Lq, int Lk, bool causal) {
   return n;
 }
 
-// Pieces, one a compute unit and 16 key tiles at least, 2 us a tile: 16 us to find and
+// Pieces, one a compute unit and 16 visited tiles at least: 16 us to find and
 // start them and for the joining launch, and the partial rows' (of `row` floats) bytes
 // at 5 TB/s.  A workgroup finds its own by going over the tiles' weights, 64 at a time:
 // not where they are too many for that to be short.  Pieces of a head read its keys at
 // different places; where K and V of a head are more than an L2 (4 MB) that costs 15 %.
 // (Forward, 12 heads, 6144 plain: seven runs 303 us, pieces 260; causal 177 and 154;
 // 1560 rows on 32760 keys: three runs 346, pieces 413.)
-inline ModPieces mod_pieces(int B, int H, int Lq, int Lk, bool causal, int cus, size_t first, int row) {
+// `own` rows in tiles of 256, of which tile t visits visits(t) tiles of `other` rows.
+template <typename F>
+inline ModPieces mod_pieces(int B, int heads, int own, int other, F&& visits, int cus, size_t first, int row, double tile_us) {
   ModPieces p{0, 0, 0, 0, 0.0};
-  const int64_t qt = (int64_t)mod_tiles(Lq), wgs = qt * B * H;
-  if ((qt + 63) / 64 * B > 64) return p;
+  const int64_t nt = (int64_t)mod_tiles(own), wgs = nt * B * heads;
+  if ((nt + 63) / 64 * B > 64) return p;
   int64_t weight = 0;  // of a head
-  for (int64_t t = 0; t < qt; ++t)
-    weight += kTileStart + mod_row_tiles(t, Lq, Lk, causal) * key_weight((int)(Lq - t * kModRows < kModRows ? Lq - t * kModRows : kModRows));
-  const int64_t all = weight * B * H, most = all / (4 * kLeastPiece);
+  for (int64_t t = 0; t < nt; ++t)
+    weight += kTileStart + visits(t) * key_weight((int)(own - t * kModRows < kModRows ? own - t * kModRows : kModRows));
+  const int64_t all = weight * B * heads, most = all / (4 * kLeastPiece);
   const int n = (int)(most < cus ? most : cus);
   if (n < 2 || weight > INT32_MAX) return p;
   p.n = n;
-  p.slot_rows = (Lq < kModRows ? Lq + 31 : kModRows) / 32 * 32;
+  p.slot_rows = (own < kModRows ? own + 31 : kModRows) / 32 * 32;
   p.cut = first + (size_t)2 * n * p.slot_rows * row;
   p.floats = p.cut + 2 * (size_t)wgs;
   const int64_t parts = n + (wgs < n ? wgs : n);
-  p.us = (double)all / n / 4 * 2.0 * (Lk > 8192 ? 1.15 : 1.0) + 16.0 + (double)parts * p.slot_rows * row * 8 / 5e6;
+  p.us = (double)all / n / 4 * tile_us * (other > 8192 ? 1.15 : 1.0) + 16.0 + (double)parts * p.slot_rows * row * 8 / 5e6;
   return p;
 }
 
@@ -188,7 +190,8 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
       r.floats = need;
     }
   }
-  const ModPieces p = docs ? ModPieces{0, 0, 0, 0, 0.0} : mod_pieces(B, H, Lq, Lk, causal, cus, r.part, 129);
+  if (docs) return r;
+  const ModPieces p = mod_pieces(B, H, Lq, Lk, [&](int64_t t) { return mod_row_tiles(t, Lq, Lk, causal); }, cus, r.part, 129, 2.0);
   if (p.n && p.floats <= max_floats && p.us < best) {
     r.runs = 1;
     r.pieces = p;
@@ -213,7 +216,7 @@ struct ModBwdSplit {
   int runs, quantum;
   size_t delta, nlse, empty, counts, part;  // first values of these in the workspace (document ranges at 0)
   size_t least, floats;  // values of the workspace: for one run and whole query tiles, for this
-  ModPieces dq;          // of the query side (its partial sums lie where the key side's come later)
+  ModPieces dq, dkdv;    // (the query side's partial sums lie where the key side's come later)
 };
 
 // Tiles of the stream of key tile t, where queries stand at their default positions.
@@ -223,7 +226,8 @@ inline int64_t mod_stream(int t, int rep, int Lq, int Lk, bool causal) {
   return n > 0 ? rep * n : 0;
 }
 
-inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, bool causal, int cus, size_t max_floats) {
+inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, bool causal, bool lengths, int cus,
+                                 size_t max_floats) {
   auto up = [](size_t x) { return (x + 63) / 64 * 64; };
   ModBwdSplit r;
   r.runs = 1;
@@ -234,7 +238,7 @@ inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool doc
   r.counts = r.empty + (size_t)B * mod_ranges(Lq);
   r.least = r.floats = r.counts + (size_t)B * mod_tiles(Lk);
   r.part = up(r.least);
-  r.dq.n = 0;
+  r.dq.n = r.dkdv.n = 0;
   if (B == 0 || H == 0 || Lq == 0 || Lk == 0) return r;
   const int kt = (int)mod_tiles(Lk);
   const int64_t heads = (int64_t)B * Hkv;
@@ -284,6 +288,19 @@ inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool doc
     else lo = q + 1;
   }
   consider(lo);
+  if (!docs && kt <= 4096) {
+    // Pieces: 4 us a tile.  Where the batches have lengths of their own the runs above
+    // are made for streams that are not there, and end unevenly.  (Both with the joining
+    // launch; 2 x 4001, 16 heads on 4, causal: runs 301 us, pieces 278; with prefixes of
+    // 1000 and 2300: 531 and 321; 2 x 2049 causal: 105 and 116.)
+    ModPieces p = mod_pieces(B, Hkv, Lk, Lq, [&](int64_t t) { return mod_stream((int)t, H / Hkv, Lq, Lk, causal); }, cus, r.part, 256, 4.0);
+    if (p.n && p.floats <= max_floats && p.us < best * 4.0 * (lengths ? 1.3 : 0.95)) {
+      r.dkdv = p;
+      r.runs = 1;
+      r.quantum = 1 << 30;
+      r.floats = p.floats;
+    }
+  }
   // Query side: 256-row workgroups with all of their keys (as in the forward, 2 us a
   // tile and 4 to start and end), or pieces.
   const int64_t qt = (int64_t)mod_tiles(Lq), wgs = qt * B * H;
@@ -291,7 +308,7 @@ inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool doc
   const int64_t tiles = ((int64_t)Lk + kModKeys - 1) / kModKeys, rounds = (wgs + cus - 1) / cus;
   const double mean = 1.05 * (double)mod_key_tiles(Lq, Lk, causal) * B * H / cus;
   const double load = causal ? (mean > tiles ? mean : tiles) : (double)rounds * tiles;
-  const ModPieces p = mod_pieces(B, H, Lq, Lk, causal, cus, r.part, 128);
+  const ModPieces p = mod_pieces(B, H, Lq, Lk, [&](int64_t t) { return mod_row_tiles(t, Lq, Lk, causal); }, cus, r.part, 128, 2.0);
   if (p.n && p.floats <= max_floats && p.us < load * 2.0 + rounds * 4.0) {
     r.dq = p;
     if (p.floats > r.floats) r.floats = p.floats;

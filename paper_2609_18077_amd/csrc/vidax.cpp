@@ -497,7 +497,7 @@ vidax_status vidax_attn_mod_bwd(const void* q, const void* k, const void* v, con
                        s[0], s[1], s[2], s[3], s[4], s[5]};
   if (any_overlap(outs, ins)) return VIDAX_ERR_INVALID_ARG;
   if (st != VIDAX_OK || (nq == 0 && nk == 0)) return st;
-  const size_t least = vidax::mod_bwd_split(B, H, Hkv, Lq, Lk, a.c.s.k_doc != nullptr, false, 1, 0).least;
+  const size_t least = vidax::mod_bwd_split(B, H, Hkv, Lq, Lk, a.c.s.k_doc != nullptr, false, false, 1, 0).least;
   if (workspace_floats < least) return VIDAX_ERR_INVALID_ARG;
   if (!vidax::launch_attn_mod_bwd) return VIDAX_ERR_LAUNCH;
   a.q = (const uint16_t*)q;
@@ -520,9 +520,12 @@ size_t vidax_attn_mod_bwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, in
   Buf s[6];
   if (mod_common(B, H, Hkv, Lq, Lk, d, 1.0f, nullptr, &c, s) != VIDAX_OK) return 0;
   const int cus = vidax::device_cu_count();
-  const size_t x = vidax::mod_bwd_split(B, H, Hkv, Lq, Lk, docs != 0, false, cus, SIZE_MAX).floats;
-  const size_t y = vidax::mod_bwd_split(B, H, Hkv, Lq, Lk, docs != 0, true, cus, SIZE_MAX).floats;
-  return x > y ? x : y;
+  size_t most = 0;
+  for (int i = 0; i < 4; ++i) {
+    const size_t n = vidax::mod_bwd_split(B, H, Hkv, Lq, Lk, docs != 0, i & 1, i & 2, cus, SIZE_MAX).floats;
+    if (n > most) most = n;
+  }
+  return most;
 }
 
 size_t vidax_attn_mod_fwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, int32_t Lq, int32_t Lk, int32_t d,

@@ -123,10 +123,11 @@ extern "C" void fwd(int B, int H, int Hkv, int Lq, int Lk, int docs, int causal,
   o[0] = s.few; o[1] = s.runs; o[2] = s.units; o[3] = s.part; o[4] = s.floats;
   o[5] = s.pieces.n; o[6] = s.pieces.slot_rows; o[7] = s.pieces.cut;
 }
-extern "C" void bwd(int B, int H, int Hkv, int Lq, int Lk, int docs, int causal, int cus, size_t most, int64_t* o) {
-  const ModBwdSplit s = mod_bwd_split(B, H, Hkv, Lq, Lk, docs, causal, cus, most);
+extern "C" void bwd(int B, int H, int Hkv, int Lq, int Lk, int docs, int causal, int lens, int cus, size_t most, int64_t* o) {
+  const ModBwdSplit s = mod_bwd_split(B, H, Hkv, Lq, Lk, docs, causal, lens, cus, most);
   o[0] = s.runs; o[1] = s.quantum; o[2] = s.delta; o[3] = s.nlse; o[4] = s.empty; o[5] = s.counts; o[6] = s.part;
   o[7] = s.least; o[8] = s.floats; o[9] = s.dq.n; o[10] = s.dq.slot_rows; o[11] = s.dq.cut;
+  o[12] = s.dkdv.n; o[13] = s.dkdv.slot_rows; o[14] = s.dkdv.cut;
 }
 extern "C" void block(int B, int L, int C, int64_t* o) {
   const BlockShape s = block_bwd_shape(B, L, C);
@@ -149,7 +150,7 @@ def rules(tmp_path_factory):
     lib = ctypes.CDLL(str(lib))
 
     def call(name, *a):
-        out = (ctypes.c_int64 * 12)()
+        out = (ctypes.c_int64 * 16)()
         f = getattr(lib, name)
         f.argtypes = [ctypes.c_int] * (len(a) - (name != "block")) + [ctypes.c_size_t] * (name != "block") + [ctypes.c_void_p]
         f.restype = None
@@ -244,12 +245,13 @@ def test_pieces_cover_every_tile_once():
 
 
 def test_backward_split_fits_its_workspace(rules):
-    cuts = 0
+    cuts = key_cuts = 0
     for B, H, Hkv, Lq, Lk in _shapes():
         for docs in (0, 1):
             for causal in (0, 1):
-                (runs, quantum, delta, nlse, empty, counts, part, least, floats, pieces, slot_rows,
-                 cut) = rules("bwd", B, H, Hkv, Lq, Lk, docs, causal, 256, ALL)
+                lens = (B + Lk) % 2
+                (runs, quantum, delta, nlse, empty, counts, part, least, floats, pieces, slot_rows, cut, kpieces, krows, kcut,
+                 _) = rules("bwd", B, H, Hkv, Lq, Lk, docs, causal, lens, 256, ALL)
                 doc = B * (4 * (-(-Lk // 64) + -(-Lq // 64)) + -(-Lk // 256) + -(-Lq // 256)) if docs else 0
                 rows = B * H * Lq
                 assert doc <= delta and delta + rows <= nlse and nlse + rows <= empty
@@ -262,16 +264,21 @@ def test_backward_split_fits_its_workspace(rules):
                     assert not docs and pieces <= 256 and slot_rows == min(256, -(-Lq // 32) * 32)
                     assert cut == part + 2 * pieces * slot_rows * 128
                     need = max(need, cut + 2 * B * H * -(-Lq // 256))
+                if kpieces:
+                    key_cuts += 1
+                    assert not docs and runs == 1 and kpieces <= 256 and krows == min(256, -(-Lk // 32) * 32)
+                    assert kcut == part + 2 * kpieces * krows * 256
+                    need = max(need, kcut + 2 * B * Hkv * -(-Lk // 256))
                 assert 1 <= runs <= 16 and floats == need
                 assert runs == 1 or 2 * runs * B * Lk * Hkv * 128 <= 96 << 20
                 if not docs:  # the longest stream's runs cover it
                     longest = H // Hkv * (-(-Lq // 64) - (max(Lq - Lk, 0) // 64 if causal else 0))
                     assert runs * quantum >= longest
-                one = rules("bwd", B, H, Hkv, Lq, Lk, docs, causal, 256, least)
-                assert one[0] == 1 and one[8] == least and one[9] == 0
-    assert cuts > 20
+                one = rules("bwd", B, H, Hkv, Lq, Lk, docs, causal, lens, 256, least)
+                assert one[0] == 1 and one[8] == least and one[9] == one[12] == 0
+    assert cuts > 20 and key_cuts > 20
     for B, H, Hkv, Lq, Lk, mask in PIECES:
-        assert rules("bwd", B, H, Hkv, Lq, Lk, 0, mask != "all", 256, ALL)[9] > 0
+        assert rules("bwd", B, H, Hkv, Lq, Lk, 0, mask not in ("all", "valid"), mask not in ("all", "causal"), 256, ALL)[9] > 0
 
 
 def test_block_runs_cover_every_token(rules):

@@ -523,22 +523,27 @@ __global__ __launch_bounds__(1024) void mod_order_kernel(OrderArgs a) {
   for (int i = wave; i < n; i += 16) {
     const int b = i / tiles, t = i - b * tiles;
     const Batch bt = batch_of(c, b);
-    Docs d{0x7fffffff, 0, false};
-    for (int j = 0; j < 8; ++j)
-      if (8 * t + j < own_r) d = mod::join(d, docs_of(own[(size_t)b * own_r + 8 * t + j]));
+    Docs d{0x7fffffff, 0, false};  // (lanes l, l + 8, .. the tile's range l)
+    if (8 * t + (lane & 7) < own_r) d = docs_of(own[(size_t)b * own_r + 8 * t + (lane & 7)]);
+#pragma unroll
+    for (int m = 1; m < 8; m <<= 1) d = mod::join(d, Docs{__shfl_xor(d.lo, m), __shfl_xor(d.hi, m), false});
     // the part of the other side that the limits leave: keys [0, to), queries [from, ..)
     const int last = min((t + 1) * BM, own_len) - 1;
     const int to = isq ? key_limit(bt, c.s.causal, bt.start + last) : other_len;
     const int from = !isq && c.s.causal && t * BM >= bt.prefix ? max(t * BM - bt.start, 0) : 0;
     int w = 0;
-    for (int o = 0; o < to; o += 4096) {
-      const int g = o / 64 + lane;
-      bool v = g * 64 < to && g * 64 + 63 >= from;
-      if (v) {
-        const int4 r = *reinterpret_cast<const int4*>(other + (size_t)b * other_r + 2 * g);
-        v = meet(d, mod::join(docs_of(make_int2(r.x, r.y)), docs_of(make_int2(r.z, r.w))));
+    for (int o = 0; o < to; o += 4 * 4096) {  // (four loads in flight)
+      int4 r[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        r[u] = *reinterpret_cast<const int4*>(other + (size_t)b * other_r + 2 * min(o / 64 + 64 * u + lane, other_r / 2 - 1));
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int g = o / 64 + 64 * u + lane;
+        const bool v = g * 64 < to && g * 64 + 63 >= from &&
+                       meet(d, mod::join(docs_of(make_int2(r[u].x, r[u].y)), docs_of(make_int2(r[u].z, r[u].w))));
+        w += __builtin_popcountll(__builtin_amdgcn_ballot_w64(v));
       }
-      w += __builtin_popcountll(__builtin_amdgcn_ballot_w64(v));
     }
     if (lane == 0) work[i] = w;
   }

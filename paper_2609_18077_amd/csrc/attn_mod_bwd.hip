@@ -93,13 +93,12 @@ __device__ __forceinline__ void each_hidden(int from, int to, const int* ids, in
 // The 4-byte values of 64-row tile t (of L rows at base; zero behind) into LDS, one wave.
 template <typename T>
 __device__ __forceinline__ void copy_row(const T* base, int t, int L, T* dst, int lane) {
-  const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-      (void*)(base + (size_t)t * BN), (short)0, __builtin_amdgcn_readfirstlane(min(L - t * BN, BN) * 4), kBufferFlags);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)dst, 4, lane * 4, 0, 0, 0);
+  const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, L * 4, kBufferFlags);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)dst, 4, (t * BN + lane) * 4, 0, 0, 0);
 }
-// 64-row tile `t` of rows [0, limit) of a buffer: later rows read as zero.
+// 64-row tile `t` of rows [0, limit) of a buffer (one at least): later rows read as zero.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const uint16_t* base, int t, int limit, int tok) {
-  const int nbytes = __builtin_amdgcn_readfirstlane(min(max(limit - t * BN, 0), BN) * tok * 2);
+  const int nbytes = min(limit - t * BN, BN) * tok * 2;
   return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (size_t)t * BN * tok), (short)0, nbytes, kBufferFlags);
 }
 

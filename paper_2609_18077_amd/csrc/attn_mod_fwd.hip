@@ -178,7 +178,7 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
   const int vr = vrow + 16 * (wave >> 1);  // blocks 2 wave and 2 wave + 1 are of one key step
   const int vg0 = vr * kbytes + 2 * (vd + 32 * (2 * wave & 3)), vg1 = vg0 + 64;
   auto tile_rsrc = [&](const uint16_t* base, int t) __attribute__((always_inline)) {
-    const int nbytes = __builtin_amdgcn_readfirstlane(min(max(gmax - t * BN, 0), BN) * kbytes);
+    const int nbytes = min(gmax - t * BN, BN) * kbytes;  // (t is below ntiles)
     return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (size_t)t * BN * ktok), (short)0, nbytes, kBufferFlags);
   };
   auto dma_k = [&](int t, uint16_t* buf) __attribute__((always_inline)) {
@@ -406,10 +406,9 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
   // ids of a tile's keys, in LDS for the step that masks it
   auto dma_ids = [&](const Tile& t, int* dst) __attribute__((always_inline)) {
     if (!docs || t.one() || wave != 0) return;
-    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)(c.s.k_doc + (size_t)b * c.Lk + t.t * BN), (short)0,
-        __builtin_amdgcn_readfirstlane(min(c.Lk - t.t * BN, BN) * 4), kBufferFlags);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)dst, 4, lane * 4, 0, 0, 0);
+    const __amdgpu_buffer_rsrc_t rs =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(c.s.k_doc + (size_t)b * c.Lk), (short)0, c.Lk * 4, kBufferFlags);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)dst, 4, (t.t * BN + lane) * 4, 0, 0, 0);
   };
   dma_ids(cur, Kd[0]);
   dma_k(cur.t, K0);
@@ -556,7 +555,8 @@ __global__ __launch_bounds__(1024) void mod_order_kernel(OrderArgs a) {
   }
 }
 
-// Joins the parts of the tiles that pieces have cut: 16 rows a workgroup, a wave four.
+// Joins the parts of the tiles that pieces have cut: 16 rows a workgroup, 8 values of a
+// row a thread.
 struct PieceJoinArgs {
   const float *po, *pl;
   uint16_t* o;
@@ -569,30 +569,35 @@ __global__ __launch_bounds__(256) void mod_piece_join_kernel(PieceJoinArgs a) {
   const int p0 = __builtin_amdgcn_readfirstlane(a.pieces.cut[2 * tile]);
   if (p0 < 0) return;
   const int p1 = __builtin_amdgcn_readfirstlane(a.pieces.cut[2 * tile + 1]);
-  const int bh = tile / a.ntile, row0 = (tile - bh * a.ntile) * BM + 16 * sub + 4 * (threadIdx.x >> 6);
-  const int b = bh / a.H, h = bh - b * a.H, lane = threadIdx.x & 63;
-  for (int i = row0; i < min(row0 + 4, a.Lq); ++i) {
-    auto at = [&](int p) { return (size_t)(2 * p + (p == p0)) * a.pieces.slot_rows + (i & (BM - 1)); };
-    float m = -INFINITY;
+  const int bh = tile / a.ntile, r = 16 * sub + (threadIdx.x >> 4), i = (tile - bh * a.ntile) * BM + r;
+  if (i >= a.Lq) return;
+  const int b = bh / a.H, h = bh - b * a.H, ch = 8 * (threadIdx.x & 15);
+  // o = sum_p 2^(lse_p - max) o_p / sum_p 2^(lse_p - max); a part that saw nothing
+  // wrote zeros: weight 0
+  auto at = [&](int p) { return (size_t)(2 * p + (p == p0)) * a.pieces.slot_rows + r; };
+  float m = -INFINITY;
 #pragma unroll 4
-    for (int p = p0; p <= p1; ++p) m = fmaxf(m, a.pl[at(p)]);
-    float x = 0.f, y = 0.f, l = 0.f;
-    if (m > -INFINITY) {
+  for (int p = p0; p <= p1; ++p) m = fmaxf(m, a.pl[at(p)]);
+  const float ref = m > -INFINITY ? m : 0.f;
+  float4 x0 = make_float4(0.f, 0.f, 0.f, 0.f), x1 = x0;
+  float l = 0.f;
 #pragma unroll 4
-      for (int p = p0; p <= p1; ++p) {
-        const float w = __builtin_amdgcn_exp2f(a.pl[at(p)] - m);
-        const float2 v = *reinterpret_cast<const float2*>(a.po + at(p) * D + 2 * lane);
-        l += w;  // (a part that saw nothing wrote zeros: weight 0)
-        x = fmaf(w, v.x, x);
-        y = fmaf(w, v.y, y);
-      }
-      const float inv = 1.0f / l;
-      x *= inv;
-      y *= inv;
-    }
-    *reinterpret_cast<uint32_t*>(a.o + (((size_t)b * a.Lq + i) * a.H + h) * D + 2 * lane) = pack_bf16x2(x, y);
-    if (a.lse && lane == 0) a.lse[(size_t)bh * a.Lq + i] = m > -INFINITY ? (m + __log2f(l)) * kLn2 : -INFINITY;
+  for (int p = p0; p <= p1; ++p) {
+    const float w = __builtin_amdgcn_exp2f(a.pl[at(p)] - ref);
+    const float4 u = *reinterpret_cast<const float4*>(a.po + at(p) * D + ch);
+    const float4 v = *reinterpret_cast<const float4*>(a.po + at(p) * D + ch + 4);
+    l += w;
+    x0.x = fmaf(w, u.x, x0.x); x0.y = fmaf(w, u.y, x0.y); x0.z = fmaf(w, u.z, x0.z); x0.w = fmaf(w, u.w, x0.w);
+    x1.x = fmaf(w, v.x, x1.x); x1.y = fmaf(w, v.y, x1.y); x1.z = fmaf(w, v.z, x1.z); x1.w = fmaf(w, v.w, x1.w);
   }
+  const float inv = l > 0.f ? 1.0f / l : 0.f;
+  uint4 o;
+  o.x = pack_bf16x2(x0.x * inv, x0.y * inv);
+  o.y = pack_bf16x2(x0.z * inv, x0.w * inv);
+  o.z = pack_bf16x2(x1.x * inv, x1.y * inv);
+  o.w = pack_bf16x2(x1.z * inv, x1.w * inv);
+  *reinterpret_cast<uint4*>(a.o + (((size_t)b * a.Lq + i) * a.H + h) * D + ch) = o;
+  if (a.lse && ch == 0) a.lse[(size_t)bh * a.Lq + i] = l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
 }
 
 // Joins the runs of every (batch, head, query): a wave a row, lane l its

@@ -93,7 +93,7 @@ inline int64_t mod_key_tiles(int Lq, int Lk, bool causal) {
   return n;
 }
 
-// Pieces, one a compute unit and 16 visited tiles at least: 16 us to find and
+// Pieces, one a compute unit and 16 visited tiles at least: 12 us to find and
 // start them and for the joining launch, and the partial rows' (of `row` floats) bytes
 // at 5 TB/s.  A workgroup finds its own by going over the tiles' weights, 64 at a time:
 // not where they are too many for that to be short.  Pieces of a head read its keys at
@@ -117,7 +117,7 @@ inline ModPieces mod_pieces(int B, int heads, int own, int other, F&& visits, in
   p.cut = first + (size_t)2 * n * p.slot_rows * row;
   p.floats = p.cut + 2 * (size_t)wgs;
   const int64_t parts = n + (wgs < n ? wgs : n);
-  p.us = (double)all / n / 4 * tile_us * (other > 8192 ? 1.15 : 1.0) + 16.0 + (double)parts * p.slot_rows * row * 8 / 5e6;
+  p.us = (double)all / n / 4 * tile_us * (other > 8192 ? 1.15 : 1.0) + 12.0 + (double)parts * p.slot_rows * row * 8 / 5e6;
   return p;
 }
 
@@ -301,15 +301,15 @@ inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool doc
       r.floats = p.floats;
     }
   }
-  // Query side: 256-row workgroups with all of their keys (as in the forward, 2 us a
-  // tile and 4 to start and end), or pieces.
+  // Query side: 256-row workgroups with all of their keys (as in the forward; 2.6 us
+  // a tile and 4 to start and end), or pieces.
   const int64_t qt = (int64_t)mod_tiles(Lq), wgs = qt * B * H;
   if (docs || qt > 4096) return r;
   const int64_t tiles = ((int64_t)Lk + kModKeys - 1) / kModKeys, rounds = (wgs + cus - 1) / cus;
   const double mean = 1.05 * (double)mod_key_tiles(Lq, Lk, causal) * B * H / cus;
   const double load = causal ? (mean > tiles ? mean : tiles) : (double)rounds * tiles;
-  const ModPieces p = mod_pieces(B, H, Lq, Lk, [&](int64_t t) { return mod_row_tiles(t, Lq, Lk, causal); }, cus, r.part, 128, 2.0);
-  if (p.n && p.floats <= max_floats && p.us < load * 2.0 + rounds * 4.0) {
+  const ModPieces p = mod_pieces(B, H, Lq, Lk, [&](int64_t t) { return mod_row_tiles(t, Lq, Lk, causal); }, cus, r.part, 128, 2.6);
+  if (p.n && p.floats <= max_floats && p.us < load * 2.6 + rounds * 4.0) {
     r.dq = p;
     if (p.floats > r.floats) r.floats = p.floats;
   }

@@ -303,6 +303,7 @@ vidax_status vidax_qkv_proj(const void* x, const void* w, const float* bias, con
  *                                             a negative id belongs to none),
  *   j <= p_i  or  j < prefix_len[b]           with causal.
  * A query that sees no key gives o = 0, lse = -inf and passes no gradient.
+ * Distances |p_i - j| are fp32 (exact up to 2^24).
  * All pointers are device pointers, 4-byte aligned, NULL where absent.
  */
 typedef struct vidax_score_desc {

@@ -117,13 +117,20 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
   const int ntiles = PIECES ? part.hi : (gmax + BN - 1) / BN, tile0 = PIECES ? part.lo : 0;
 
   // ---- the next tile to visit: a group of 64 tiles is looked at together, lane
-  // l at tile 64 g + l.
-  int grp = tile0 >> 6, left = INT32_MAX;  // group; tiles left of this run
+  // l at tile 64 g + l.  With a bias from the rows' own positions (tile `home`) down,
+  // then from the last tile down to there: the rows meet the keys next to them first,
+  // and the reference that those set holds (upwards, steep slopes raised it in every
+  // tile: 1560 rows on 32760 keys, causal, 12 heads, slopes 2^-2/3 .. 2^-8: 414 us, so
+  // 334).
+  constexpr bool DOWN = BIAS;
+  const int home = min(max((bt.start + glast) / BN, tile0), ntiles - 1);
+  bool above = false;  // behind home
+  int grp = DOWN ? home >> 6 : tile0 >> 6, left = INT32_MAX;  // group; tiles left of this run
   uint64_t visit = 0;             // tiles that some row of the workgroup may see
   int fl = 0, id = 0;             // of the lane's tile
   auto look = [&](int g) __attribute__((always_inline)) {
     const int t = 64 * g + lane;
-    bool v = t >= tile0 && t < ntiles;
+    bool v = t >= tile0 && t < ntiles && (!DOWN || (t > home) == above);
     fl = (t * BN < wmax ? Tile::kMine : 0) | (t * BN + BN <= wmin ? Tile::kWhole : 0) | Tile::kOne;
     if (docs && v) {
       const int4 r = *reinterpret_cast<const int4*>(a.r.k + (size_t)b * a.kr + 2 * t);
@@ -135,14 +142,30 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
     }
     visit = __builtin_amdgcn_ballot_w64(v);
   };
-  auto next = [&]() __attribute__((always_inline)) {
-    while (visit == 0) {
-      if (64 * (grp + 1) >= ntiles) return Tile{-1, 0, 0};
-      look(++grp);
+  auto first = [&]() __attribute__((always_inline)) {  // out of visit
+    const int i = DOWN ? 63 - __builtin_clzll(visit) : __builtin_ctzll(visit);
+    visit &= DOWN ? ~(1ull << i) : visit - 1;
+    return i;
+  };
+  auto more = [&]() __attribute__((always_inline)) {  // the next group; false: none left
+    if (!DOWN) {
+      if (64 * (grp + 1) >= ntiles) return false;
+      ++grp;
+    } else if (64 * grp > (above ? home + 1 : tile0)) {
+      --grp;
+    } else {
+      if (above || home + 1 >= ntiles) return false;
+      above = true;
+      grp = (ntiles - 1) >> 6;
     }
+    look(grp);
+    return true;
+  };
+  auto next = [&]() __attribute__((always_inline)) {
+    while (visit == 0)
+      if (!more()) return Tile{-1, 0, 0};
     if (left-- <= 0) return Tile{-1, 0, 0};
-    const int i = __builtin_ctzll(visit);
-    visit &= visit - 1;
+    const int i = first();
     return Tile{64 * grp + i, __builtin_amdgcn_readlane(fl, i), __builtin_amdgcn_readlane(id, i)};
   };
 
@@ -214,30 +237,51 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
   float mref = -INFINITY;  // the row's reference, log2 units
   float nm = kUnset;       // -mref
   float lsum = 0.f;        // this lane half's sum
-  const float mul = a.sc.mul;
   const float slope = BIAS ? -c.s.slopes[h] * kLog2e : 0.f;
+  // Of the tile at hand: the factor of its scores, and the bias as a linear function of
+  // the key, slope |p - j| = lin - lin_slope (j - first key of the lane half).  A tile
+  // on both sides of the wave's positions (a few of a wave's) has what is missing added
+  // to its scores beforehand (straddle).
+  float mul = a.sc.mul, lin = 0.f, lin_slope = 0.f;
+  const int pmin = bt.start + wrow, pmax = bt.start + wrow + 31;
+  auto straddle = [&](f32x16 s[2], int t) __attribute__((always_inline)) {
+    const bool after = t * BN >= pmax, both = !after && t * BN + BN - 1 > pmin;  // uniform
+    lin_slope = after ? -slope : slope;
+    const float dist = (float)(bt.start + qrow - t * BN - 4 * hi);
+    lin = lin_slope * dist;
+    if (!CAP) mul = a.sc.mul;
+    if (!both) return;
+#pragma unroll
+    for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float y = CAP ? s[blk][i] : s[blk][i] * a.sc.mul;
+        s[blk][i] = fmaf(2.f * slope, fmaxf((float)(32 * blk + 8 * (i >> 2) + (i & 3)) - dist, 0.f), y);
+      }
+    if (!CAP) mul = 1.f;
+  };
 
-  // y + n of element i of a block; dist: position minus the block's first key of this lane half
-  auto logit = [&](float s, float n, float dist, int i) __attribute__((always_inline)) {
+  // y + n of element i of block blk; with a bias n holds lin
+  auto logit = [&](float s, float n, int blk, int i) __attribute__((always_inline)) {
     float y = CAP ? s + n : fmaf(s, mul, n);
-    if (BIAS) y = fmaf(slope, fabsf(dist - (float)(8 * (i >> 2) + (i & 3))), y);
+    if (BIAS) y = fmaf(lin_slope, -(float)(32 * blk + 8 * (i >> 2) + (i & 3)), y);
     return y;
   };
   // P of elements i, i + 1 of a block (one rounding of the weights, 2^-9 of each,
   // independent; the sum adds them before it)
-  auto exps = [&](const f32x16& s, int i, float dist, uint32_t pw[8], float& sum) __attribute__((always_inline)) {
-    const float p0 = __builtin_amdgcn_exp2f(logit(s[i], nm, dist, i));
-    const float p1 = __builtin_amdgcn_exp2f(logit(s[i + 1], nm, dist, i + 1));
+  auto exps = [&](const f32x16& s, int blk, int i, float n, uint32_t pw[8], float& sum) __attribute__((always_inline)) {
+    const float p0 = __builtin_amdgcn_exp2f(logit(s[i], n, blk, i));
+    const float p1 = __builtin_amdgcn_exp2f(logit(s[i + 1], n, blk, i + 1));
     pw[i >> 1] = pack_bf16x2(p0, p1);
     sum += p0;
     sum += p1;
   };
   // The block's sum is not below 2^64 for some row: new references, the output and
   // sum rescaled, the block's weights formed again
-  auto reset = [&](const f32x16& s, float dist, uint32_t pw[8], float& sum) __attribute__((always_inline)) {
-    float m = logit(s[0], 0.f, dist, 0);
+  auto reset = [&](const f32x16& s, int blk, uint32_t pw[8], float& sum) __attribute__((always_inline)) {
+    float m = logit(s[0], lin, blk, 0);
 #pragma unroll
-    for (int i = 1; i < 16; ++i) m = fmaxf(m, logit(s[i], 0.f, dist, i));
+    for (int i = 1; i < 16; ++i) m = fmaxf(m, logit(s[i], lin, blk, i));
     const float mnew = fmaxf(mref, wave_half_max(m));
     const bool set = mnew > -INFINITY;
     const float alpha = set ? __builtin_amdgcn_exp2f(mref - mnew) : 1.f;
@@ -250,13 +294,12 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
     nm = set ? -mnew : kUnset;
     sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) exps(s, i, dist, pw, sum);
+    for (int i = 0; i < 16; i += 2) exps(s, blk, i, nm + lin, pw, sum);
   };
   // The scores of the next tile (K in kb) and the softmax and PV of this one (V in
   // vb), hand-scheduled: a slot a product, each also issuing the operand reads of
   // the product three slots on and its share of the exponentials.
-  auto products = [&](f32x16 s[2], f32x16 sn[2], const uint16_t* kb, const uint16_t* vb, int t) __attribute__((always_inline)) {
-    const float dist = BIAS ? (float)(bt.start + qrow - t * BN - 4 * hi) : 0.f;
+  auto products = [&](f32x16 s[2], f32x16 sn[2], const uint16_t* kb, const uint16_t* vb) __attribute__((always_inline)) {
     bf16x8 op[32];
     auto read_op = [&](auto N) __attribute__((always_inline)) {
       constexpr int n = decltype(N)::value;
@@ -273,26 +316,28 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
     auto p_op = [&](int blk, int k2) __attribute__((always_inline)) {
       return __builtin_bit_cast(bf16x8, make_uint4(pw[blk][4 * k2], pw[blk][4 * k2 + 1], pw[blk][4 * k2 + 2], pw[blk][4 * k2 + 3]));
     };
+    float n0 = BIAS ? nm + lin : nm;
     for_slots<3>(read_op);
     SLOT();
     for_slots<16>([&](auto N) __attribute__((always_inline)) {  // scores; exponentials of block 0
       constexpr int n = decltype(N)::value;
       sn[n & 1] = mfma32(op[n], qreg[n >> 1], n < 2 ? f32x16{} : sn[n & 1]);
       read_op(std::integral_constant<int, n + 3>());
-      if constexpr ((n & 1) == 0) exps(s[0], n, dist, pw[0], sum[0]);
+      if constexpr ((n & 1) == 0) exps(s[0], 0, n, n0, pw[0], sum[0]);
       SLOT();
     });
-    if (__builtin_amdgcn_ballot_w64(!(sum[0] < kSumLimit)) != 0) reset(s[0], dist, pw[0], sum[0]);
+    if (__builtin_amdgcn_ballot_w64(!(sum[0] < kSumLimit)) != 0) reset(s[0], 0, pw[0], sum[0]);
     lsum += sum[0];
+    n0 = BIAS ? nm + lin : nm;
     SLOT();
     for_slots<8>([&](auto N) __attribute__((always_inline)) {  // PV of block 0; exponentials of block 1
       constexpr int n = decltype(N)::value;
       oacc[n & 3] = mfma32(op[16 + n], p_op(0, n >> 2), oacc[n & 3]);
       read_op(std::integral_constant<int, n + 19>());
-      exps(s[1], 2 * n, dist - 32.f, pw[1], sum[1]);
+      exps(s[1], 1, 2 * n, n0, pw[1], sum[1]);
       SLOT();
     });
-    if (__builtin_amdgcn_ballot_w64(!(sum[1] < kSumLimit)) != 0) reset(s[1], dist - 32.f, pw[1], sum[1]);
+    if (__builtin_amdgcn_ballot_w64(!(sum[1] < kSumLimit)) != 0) reset(s[1], 1, pw[1], sum[1]);
     lsum += sum[1];
     SLOT();
     for_slots<8>([&](auto N) __attribute__((always_inline)) {  // PV of block 1
@@ -376,21 +421,22 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
       int n = ntiles;
       if (docs) {
         n = 0;
-        for (int g = 0; 64 * g < ntiles; ++g) {
-          look(g);
-          n += __builtin_popcountll(visit);
-        }
+        look(grp);
+        do n += __builtin_popcountll(visit);
+        while (more());
+        above = false;
+        grp = DOWN ? home >> 6 : 0;
       }
       int skip = (int)((int64_t)n * run / a.runs);
       left = (int)((int64_t)n * (run + 1) / a.runs) - skip;
-      look(0);
+      look(grp);
       while (left > 0 && skip >= __builtin_popcountll(visit)) {
         skip -= __builtin_popcountll(visit);
-        look(++grp);
+        more();
       }
-      for (; left > 0 && skip > 0; --skip) visit &= visit - 1;
+      for (; left > 0 && skip > 0; --skip) first();
     } else {
-      look(0);
+      look(grp);
     }
     cur = next();
     nxt = next();
@@ -435,8 +481,9 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
         cap16_log2(scur[0], a.sc);
         cap16_log2(scur[1], a.sc);
       }
+      if (BIAS) straddle(scur, cur.t);
       if (!(cur.mine() && cur.whole())) mask(scur, cur, Kd[P]);
-      products(scur, snext, P ? K0 : K1, P ? V1 : V0, cur.t);
+      products(scur, snext, P ? K0 : K1, P ? V1 : V0);
     }
     cur = nxt;
     nxt = aft;

@@ -414,20 +414,29 @@ def attn_fwd_naive(q, k, v, scale=None, kv_valid_len=None, rope: Rope | None = N
 
 
 # The calls below are short enough on the device (5 us) for the binding to count:
-# plain addresses instead of pointer objects, the raw stream instead of a Stream.
+# torch looked up once, plain addresses instead of pointer objects, the raw stream
+# instead of a Stream, device numbers instead of devices.
+
+_torch = _raw_stream = _current_device = None
 
 
-def _call(fn: str, device, stream, *args):
-    """fn(*args, stream) with the tensors' device current and, by default, on that device's current stream."""
+def _load_torch():
+    global _torch, _raw_stream, _current_device
     import torch
 
-    i = device.index
-    s = torch._C._cuda_getCurrentRawStream(i) if stream is None else stream.cuda_stream
+    _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    _torch = torch
+    return torch
+
+
+def _call(fn: str, i: int, stream, *args):
+    """fn(*args, stream) with device i current and, by default, on that device's current stream."""
+    s = _raw_stream(i) if stream is None else stream.cuda_stream
     f = getattr(_lib or lib(), fn)
-    if i == torch._C._cuda_getDevice():
+    if i == _current_device():
         st = f(*args, s)
     else:
-        with torch.cuda.device(device):
+        with _torch.cuda.device(i):
             st = f(*args, s)
     if st != VIDAX_OK:
         raise VidaxError(fn, st)
@@ -436,9 +445,7 @@ def _call(fn: str, device, stream, *args):
 @functools.lru_cache(maxsize=1024)
 def _floats(fn: str, device: int, *sizes) -> int:
     """Workspace size by a function of the library (of the sizes and the device alone)."""
-    import torch
-
-    with torch.cuda.device(device):
+    with _torch.cuda.device(device):
         return getattr(lib(), fn)(*sizes)
 
 
@@ -446,9 +453,10 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-def _check_dense(name, t, dtype, shape, device):
-    if t.dtype != dtype or t.device != device or not t.is_contiguous() or t.shape != shape:
-        raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} tensor on {device}")
+def _check_dense(name, t, dtype, shape, i):
+    """t: contiguous, of this type and shape, on device i (-1: the CPU)."""
+    if t.dtype is not dtype or t.get_device() != i or not t.is_contiguous() or t.shape != shape:
+        raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} tensor on device {i}")
 
 
 # ------------------------------------- attention with score modifiers ----
@@ -458,41 +466,54 @@ _SCALE_128 = 0.08838834764831845  # 1 / sqrt(128), rounded to fp32 at the call
 
 def _score_desc(score, q, Lk):
     """Descriptor of a Score for queries q [B, Lq, H, d] against Lk keys."""
-    import torch
-
-    if score is None:
+    s = score
+    if s is None:
         return ScoreDesc()
-    s, device, i32 = score, q.device, torch.int32
+    torch = _torch or _load_torch()
+    i, f32, i32 = q.get_device(), torch.float32, torch.int32
     B, Lq, H, _ = q.shape
     if (s.q_doc is None) != (s.k_doc is None):
         raise ValueError("q_doc and k_doc come together")
     d = ScoreDesc(s.causal, s.cap)
-    for n, t, dtype, shape in (("slopes", s.slopes, torch.float32, (H,)), ("q_doc", s.q_doc, i32, (B, Lq)),
-                               ("k_doc", s.k_doc, i32, (B, Lk)), ("kv_valid_len", s.kv_valid_len, i32, (B,)),
-                               ("prefix_len", s.prefix_len, i32, (B,)), ("q_start", s.q_start, i32, (B,))):
-        if t is not None:
-            _check_dense(n, t, dtype, shape, device)
-            setattr(d, n, t.data_ptr())
+    if s.slopes is not None:
+        _check_dense("slopes", s.slopes, f32, (H,), i)
+        d.slopes = s.slopes.data_ptr()
+    if s.q_doc is not None:
+        _check_dense("q_doc", s.q_doc, i32, (B, Lq), i)
+        _check_dense("k_doc", s.k_doc, i32, (B, Lk), i)
+        d.q_doc, d.k_doc = s.q_doc.data_ptr(), s.k_doc.data_ptr()
+    if s.kv_valid_len is not None:
+        _check_dense("kv_valid_len", s.kv_valid_len, i32, (B,), i)
+        d.kv_valid_len = s.kv_valid_len.data_ptr()
+    if s.prefix_len is not None:
+        _check_dense("prefix_len", s.prefix_len, i32, (B,), i)
+        d.prefix_len = s.prefix_len.data_ptr()
+    if s.q_start is not None:
+        _check_dense("q_start", s.q_start, i32, (B,), i)
+        d.q_start = s.q_start.data_ptr()
     return d
 
 
 def _check_mod_qkv(q, k, v):
-    for n, t in (("q", q), ("k", k), ("v", v)):
-        _check_bshd(n, t)
-    if k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
+    """The device number of q, k and v."""
+    bf16 = (_torch or _load_torch()).bfloat16
+    i, qs, ks = q.get_device(), q.shape, k.shape
+    if (q.dtype is not bf16 or k.dtype is not bf16 or v.dtype is not bf16 or i < 0 or len(qs) != 4 or len(ks) != 4
+            or not q.is_contiguous() or not k.is_contiguous() or not v.is_contiguous()):
+        raise ValueError("q, k and v must be contiguous bfloat16 [B, L, H, d] device tensors")
+    if ks != v.shape or ks[0] != qs[0] or ks[3] != qs[3]:
         raise ValueError("k and v must be [B, Lk, Hkv, d] matching q's B and d")
-    if k.device != q.device or v.device != q.device:
+    if k.get_device() != i or v.get_device() != i:
         raise ValueError("q, k and v must be on one device")
+    return i
 
 
-def _workspace(workspace, need, device):
+def _workspace(workspace, need, i):
     """The caller's float32 workspace, checked, or a new one of `need` values (None for 0)."""
-    import torch
-
     if workspace is None:
-        return torch.empty((need,), dtype=torch.float32, device=device) if need else None
-    if workspace.dtype != torch.float32 or workspace.device != device or not workspace.is_contiguous():
-        raise ValueError(f"workspace must be a contiguous float32 tensor on {device}")
+        return _torch.empty((need,), dtype=_torch.float32, device=i) if need else None
+    if workspace.dtype is not _torch.float32 or workspace.get_device() != i or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous float32 tensor on device {i}")
     return workspace
 
 
@@ -502,21 +523,21 @@ def attn_mod_fwd(q, k, v, score: Score | None = None, scale=None, return_lse=Fal
     k, v bf16 [B, Lk, Hkv, 128], Hkv a divisor of H.  `workspace`: a contiguous
     float32 device tensor (by default one of vidax_attn_mod_fwd_workspace_floats
     values is allocated where the call needs one)."""
-    import torch
-
-    _check_mod_qkv(q, k, v)
+    i = _check_mod_qkv(q, k, v)
     B, Lq, H, d = q.shape
-    Lk, Hkv = k.shape[1], k.shape[2]
+    _, Lk, Hkv, _ = k.shape
     desc = _score_desc(score, q, Lk)
-    o = torch.empty_like(q) if out is None else out
-    if out is not None:
-        _check_dense("out", o, q.dtype, q.shape, q.device)
-    lse = torch.empty((B, H, Lq), dtype=torch.float32, device=q.device) if return_lse else None
+    if out is None:
+        o = _torch.empty_like(q)
+    else:
+        o = out
+        _check_dense("out", o, q.dtype, q.shape, i)
+    lse = _torch.empty((B, H, Lq), dtype=_torch.float32, device=i) if return_lse else None
     need = 0
     if workspace is None:
-        need = _floats("vidax_attn_mod_fwd_workspace_floats", q.device.index, B, H, Hkv, Lq, Lk, d, desc.k_doc is not None)
-    ws = _workspace(workspace, need, q.device)
-    _call("vidax_attn_mod_fwd", q.device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _addr(lse), B, H,
+        need = _floats("vidax_attn_mod_fwd_workspace_floats", i, B, H, Hkv, Lq, Lk, d, desc.k_doc is not None)
+    ws = None if workspace is None and not need else _workspace(workspace, need, i)
+    _call("vidax_attn_mod_fwd", i, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _addr(lse), B, H,
           Hkv, Lq, Lk, d, _SCALE_128 if scale is None else scale, ctypes.byref(desc), _addr(ws),
           0 if ws is None else ws.numel())
     return (o, lse) if return_lse else o
@@ -527,26 +548,25 @@ def attn_mod_bwd(q, k, v, o, dout, lse, score: Score | None = None, scale=None, 
     the query heads of a K/V head.  `out` = tensors to write into; `workspace`: a
     contiguous float32 device tensor (by default one of
     vidax_attn_mod_bwd_workspace_floats values is allocated)."""
-    import torch
-
-    _check_mod_qkv(q, k, v)
+    i = _check_mod_qkv(q, k, v)
+    torch = _torch
     B, Lq, H, d = q.shape
-    Lk, Hkv = k.shape[1], k.shape[2]
-    for n, t in (("o", o), ("dout", dout)):
-        _check_dense(n, t, q.dtype, q.shape, q.device)
-    _check_dense("lse", lse, torch.float32, (B, H, Lq), q.device)
+    _, Lk, Hkv, _ = k.shape
+    _check_dense("o", o, q.dtype, q.shape, i)
+    _check_dense("dout", dout, q.dtype, q.shape, i)
+    _check_dense("lse", lse, torch.float32, (B, H, Lq), i)
     desc = _score_desc(score, q, Lk)
     if out is None:
         dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
     else:
         dq, dk, dv = out
         for n, t, ref in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
-            _check_dense(n, t, ref.dtype, ref.shape, q.device)
+            _check_dense(n, t, ref.dtype, ref.shape, i)
     need = 0
     if workspace is None:
-        need = _floats("vidax_attn_mod_bwd_workspace_floats", q.device.index, B, H, Hkv, Lq, Lk, d, desc.k_doc is not None)
-    ws = _workspace(workspace, need, q.device)
-    _call("vidax_attn_mod_bwd", q.device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), dout.data_ptr(),
+        need = _floats("vidax_attn_mod_bwd_workspace_floats", i, B, H, Hkv, Lq, Lk, d, desc.k_doc is not None)
+    ws = _workspace(workspace, need, i)
+    _call("vidax_attn_mod_bwd", i, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), dout.data_ptr(),
           lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, H, Hkv, Lq, Lk, d,
           _SCALE_128 if scale is None else scale, ctypes.byref(desc), _addr(ws), 0 if ws is None else ws.numel())
     return dq, dk, dv
@@ -557,13 +577,11 @@ def attn_mod_bwd(q, k, v, o, dout, lse, score: Score | None = None, scale=None, 
 _NORMS = {None: 0, "layer": 1, "rms": 2}
 
 
-def _block_mod(name, m, t, B, L, C, device):
+def _block_mod(name, m, t, B, L, C, i):
     """Fills the BlockMod m from a modulation [B, C], [B, 1, C] or [B, L, C]; True: one row a token."""
-    import torch
-
     shape, stride = t.shape, t.stride()
-    if t.dtype != torch.float32 or t.device != device or (C > 1 and stride[-1] != 1):
-        raise ValueError(f"{name} must be a float32 tensor on {device} with dense channels")
+    if t.dtype is not _torch.float32 or t.get_device() != i or (C > 1 and stride[-1] != 1):
+        raise ValueError(f"{name} must be a float32 tensor on device {i} with dense channels")
     n = len(shape)
     if not (n == 2 or (n == 3 and shape[1] in (1, L))) or shape[0] != B or shape[-1] != C:
         raise ValueError(f"{name} must be [B, C], [B, 1, C] or [B, L, C]")
@@ -575,27 +593,32 @@ def _block_mod(name, m, t, B, L, C, device):
 
 
 def _block_desc(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha):
-    """(descriptor, whether the modulations are one row a token: a set)"""
-    import torch
-
-    if x.dim() != 3 or not x.is_cuda or x.dtype not in (torch.bfloat16, torch.float32) or not x.is_contiguous():
+    """(device number, descriptor, whether the modulations are one row a token: a set)"""
+    torch = _torch or _load_torch()
+    i, shape, dtype = x.get_device(), x.shape, x.dtype
+    wide = dtype is torch.float32
+    if len(shape) != 3 or i < 0 or not (wide or dtype is torch.bfloat16) or not x.is_contiguous():
         raise ValueError("x must be a contiguous bfloat16 or float32 [B, L, C] device tensor")
     if norm not in ("layer", "rms") or post not in _NORMS:
         raise ValueError("norm must be 'layer' or 'rms', post one of them or None")
-    B, L, C = x.shape
-    device = x.device
+    B, L, C = shape
     if y is not None:
-        _check_dense("y", y, torch.bfloat16, x.shape, device)
-    d = BlockNormDesc(x.dtype == torch.float32, _NORMS[norm], _NORMS[post], 0, eps, alpha)
-    for n, t in (("gain", gain), ("post_gain", post_gain)):
-        if t is not None:
-            _check_dense(n, t, torch.float32, (C,), device)
-            setattr(d, n, t.data_ptr())
+        _check_dense("y", y, torch.bfloat16, shape, i)
+    d = BlockNormDesc(wide, _NORMS[norm], _NORMS[post], 0, eps, alpha)
+    if gain is not None:
+        _check_dense("gain", gain, torch.float32, (C,), i)
+        d.gain = gain.data_ptr()
+    if post_gain is not None:
+        _check_dense("post_gain", post_gain, torch.float32, (C,), i)
+        d.post_gain = post_gain.data_ptr()
     token = set()
-    for n, t in (("gate", gate), ("scale", scale), ("shift", shift)):
-        if t is not None:
-            token.add(_block_mod(n, getattr(d, n), t, B, L, C, device))
-    return d, token
+    if gate is not None:
+        token.add(_block_mod("gate", d.gate, gate, B, L, C, i))
+    if scale is not None:
+        token.add(_block_mod("scale", d.scale, scale, B, L, C, i))
+    if shift is not None:
+        token.add(_block_mod("shift", d.shift, shift, B, L, C, i))
+    return i, d, token
 
 
 def block_norm_fwd(x, y=None, gate=None, scale=None, shift=None, gain=None, post_gain=None, norm: str = "layer",
@@ -609,22 +632,21 @@ def block_norm_fwd(x, y=None, gate=None, scale=None, shift=None, gain=None, post
     are multiples of 4 (slices of one modulation table); gain, post_gain: fp32
     [C].  norm: "layer" or "rms"; post: the norm on the branch, or None.  h is
     bf16.  `out` = (x', h) tensors to write into; x' may be x (in place)."""
-    import torch
-
-    d, _ = _block_desc(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha)
+    i, d, _ = _block_desc(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha)
+    torch, bf16 = _torch, _torch.bfloat16
     same = y is None and alpha == 1.0
     if out is None:
         xo = None if same else torch.empty_like(x)
-        h = torch.empty_like(x, dtype=torch.bfloat16)
+        h = torch.empty_like(x) if x.dtype is bf16 else torch.empty_like(x, dtype=bf16)
     else:
         xo, h = out
         if xo is not None:
-            _check_dense("out[0]", xo, x.dtype, x.shape, x.device)
+            _check_dense("out[0]", xo, x.dtype, x.shape, i)
         elif not same:
             raise ValueError("out[0] may be None only where x' is x")
-        _check_dense("out[1]", h, torch.bfloat16, x.shape, x.device)
+        _check_dense("out[1]", h, bf16, x.shape, i)
     B, L, C = x.shape
-    _call("vidax_block_norm_fwd", x.device, stream, x.data_ptr(), _addr(y), _addr(xo), h.data_ptr(), B, L, C,
+    _call("vidax_block_norm_fwd", i, stream, x.data_ptr(), _addr(y), _addr(xo), h.data_ptr(), B, L, C,
           ctypes.byref(d))
     return (x if xo is None else xo), h
 
@@ -641,28 +663,27 @@ def block_norm_bwd(dh, dx, x, y=None, gate=None, scale=None, shift=None, gain=No
     for the forward (gate, scale and shift are all per sample or all per token).
     `workspace`: a contiguous float32 device tensor of at least
     vidax_block_norm_bwd_workspace_floats values (by default one is allocated)."""
-    import torch
-
-    d, token = _block_desc(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha)
+    i, d, token = _block_desc(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha)
+    torch = _torch
     if len(token) > 1:
         raise ValueError("gate, scale and shift must all be per sample or all per token")
     d.per_token = int(True in token)
     B, L, C = x.shape
-    _check_dense("dh", dh, torch.bfloat16, x.shape, x.device)
+    _check_dense("dh", dh, torch.bfloat16, x.shape, i)
     if dx is not None:
-        _check_dense("dx", dx, x.dtype, x.shape, x.device)
+        _check_dense("dx", dx, x.dtype, x.shape, i)
     got = {"dx": torch.empty_like(x)}
     if y is not None:
         got["dy"] = torch.empty_like(y)
     for n, t in (("dgate", gate), ("dscale", scale), ("dshift", shift), ("dgain", gain), ("dpost_gain", post_gain)):
         if t is not None:
-            got[n] = torch.empty(t.shape, dtype=torch.float32, device=x.device)
+            got[n] = torch.empty(t.shape, dtype=torch.float32, device=i)
     g = BlockNormGrads(*(got[n].data_ptr() if n in got else None for n, _ in BlockNormGrads._fields_))
     sums = (not d.per_token and len(token) > 0) or gain is not None or post_gain is not None
     need = 0
     if sums and workspace is None:
-        need = _floats("vidax_block_norm_bwd_workspace_floats", x.device.index, B, L, C)
-    ws = _workspace(workspace, need, x.device)
-    _call("vidax_block_norm_bwd", x.device, stream, dh.data_ptr(), _addr(dx), x.data_ptr(), _addr(y), got["dx"].data_ptr(),
+        need = _floats("vidax_block_norm_bwd_workspace_floats", i, B, L, C)
+    ws = _workspace(workspace, need, i)
+    _call("vidax_block_norm_bwd", i, stream, dh.data_ptr(), _addr(dx), x.data_ptr(), _addr(y), got["dx"].data_ptr(),
           _addr(got.get("dy")), ctypes.byref(g), _addr(ws), 0 if ws is None else ws.numel(), B, L, C, ctypes.byref(d))
     return got

@@ -578,18 +578,19 @@ _NORMS = {None: 0, "layer": 1, "rms": 2}
 
 
 def _block_mod(name, m, t, B, L, C, i):
-    """Fills the BlockMod m from a modulation [B, C], [B, 1, C] or [B, L, C]; True: one row a token."""
+    """Fills the empty BlockMod m from a modulation [B, C], [B, 1, C] or [B, L, C]; True: one row a token."""
     shape, stride = t.shape, t.stride()
-    if t.dtype is not _torch.float32 or t.get_device() != i or (C > 1 and stride[-1] != 1):
+    if not shape or t.dtype is not _torch.float32 or t.get_device() != i or (C > 1 and stride[-1] != 1):
         raise ValueError(f"{name} must be a float32 tensor on device {i} with dense channels")
-    n = len(shape)
-    if not (n == 2 or (n == 3 and shape[1] in (1, L))) or shape[0] != B or shape[-1] != C:
-        raise ValueError(f"{name} must be [B, C], [B, 1, C] or [B, L, C]")
-    token = n == 3 and shape[1] > 1
     m.p = t.data_ptr()
-    m.batch_stride = stride[0] if B > 1 else 0
-    m.token_stride = stride[1] if token else 0
-    return token
+    if B > 1:
+        m.batch_stride = stride[0]
+    if shape == (B, C) or shape == (B, 1, C):
+        return False
+    if shape != (B, L, C):
+        raise ValueError(f"{name} must be [B, C], [B, 1, C] or [B, L, C]")
+    m.token_stride = stride[1]
+    return True
 
 
 def _block_desc(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha):

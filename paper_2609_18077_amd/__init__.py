@@ -429,9 +429,17 @@ def _load_torch():
     return torch
 
 
-def _call(fn: str, i: int, stream, *args):
-    """fn(*args, stream) with device i current and, by default, on that device's current stream."""
-    s = _raw_stream(i) if stream is None else stream.cuda_stream
+def _on(stream, t):
+    """Context in which `stream`, of t's device, is current: outputs and workspaces then belong to it."""
+    torch = _torch or _load_torch()
+    if stream.device_index != t.get_device():
+        raise ValueError("stream must be of the tensors' device")
+    return torch.cuda.stream(stream)
+
+
+def _call(fn: str, i: int, *args):
+    """fn(*args, stream) with device i current, on that device's current stream."""
+    s = _raw_stream(i)
     f = getattr(_lib or lib(), fn)
     if i == _current_device():
         st = f(*args, s)
@@ -523,6 +531,9 @@ def attn_mod_fwd(q, k, v, score: Score | None = None, scale=None, return_lse=Fal
     k, v bf16 [B, Lk, Hkv, 128], Hkv a divisor of H.  `workspace`: a contiguous
     float32 device tensor (by default one of vidax_attn_mod_fwd_workspace_floats
     values is allocated where the call needs one)."""
+    if stream is not None:
+        with _on(stream, q):
+            return attn_mod_fwd(q, k, v, score, scale, return_lse, out, workspace)
     i = _check_mod_qkv(q, k, v)
     B, Lq, H, d = q.shape
     _, Lk, Hkv, _ = k.shape
@@ -537,7 +548,7 @@ def attn_mod_fwd(q, k, v, score: Score | None = None, scale=None, return_lse=Fal
     if workspace is None:
         need = _floats("vidax_attn_mod_fwd_workspace_floats", i, B, H, Hkv, Lq, Lk, d, desc.k_doc is not None)
     ws = None if workspace is None and not need else _workspace(workspace, need, i)
-    _call("vidax_attn_mod_fwd", i, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _addr(lse), B, H,
+    _call("vidax_attn_mod_fwd", i, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _addr(lse), B, H,
           Hkv, Lq, Lk, d, _SCALE_128 if scale is None else scale, ctypes.byref(desc), _addr(ws),
           0 if ws is None else ws.numel())
     return (o, lse) if return_lse else o
@@ -548,6 +559,9 @@ def attn_mod_bwd(q, k, v, o, dout, lse, score: Score | None = None, scale=None, 
     the query heads of a K/V head.  `out` = tensors to write into; `workspace`: a
     contiguous float32 device tensor (by default one of
     vidax_attn_mod_bwd_workspace_floats values is allocated)."""
+    if stream is not None:
+        with _on(stream, q):
+            return attn_mod_bwd(q, k, v, o, dout, lse, score, scale, out, workspace)
     i = _check_mod_qkv(q, k, v)
     torch = _torch
     B, Lq, H, d = q.shape
@@ -566,7 +580,7 @@ def attn_mod_bwd(q, k, v, o, dout, lse, score: Score | None = None, scale=None, 
     if workspace is None:
         need = _floats("vidax_attn_mod_bwd_workspace_floats", i, B, H, Hkv, Lq, Lk, d, desc.k_doc is not None)
     ws = _workspace(workspace, need, i)
-    _call("vidax_attn_mod_bwd", i, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), dout.data_ptr(),
+    _call("vidax_attn_mod_bwd", i, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), dout.data_ptr(),
           lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, H, Hkv, Lq, Lk, d,
           _SCALE_128 if scale is None else scale, ctypes.byref(desc), _addr(ws), 0 if ws is None else ws.numel())
     return dq, dk, dv
@@ -633,6 +647,9 @@ def block_norm_fwd(x, y=None, gate=None, scale=None, shift=None, gain=None, post
     are multiples of 4 (slices of one modulation table); gain, post_gain: fp32
     [C].  norm: "layer" or "rms"; post: the norm on the branch, or None.  h is
     bf16.  `out` = (x', h) tensors to write into; x' may be x (in place)."""
+    if stream is not None:
+        with _on(stream, x):
+            return block_norm_fwd(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha, out)
     i, d, _ = _block_desc(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha)
     torch, bf16 = _torch, _torch.bfloat16
     same = y is None and alpha == 1.0
@@ -647,7 +664,7 @@ def block_norm_fwd(x, y=None, gate=None, scale=None, shift=None, gain=None, post
             raise ValueError("out[0] may be None only where x' is x")
         _check_dense("out[1]", h, bf16, x.shape, i)
     B, L, C = x.shape
-    _call("vidax_block_norm_fwd", i, stream, x.data_ptr(), _addr(y), _addr(xo), h.data_ptr(), B, L, C,
+    _call("vidax_block_norm_fwd", i, x.data_ptr(), _addr(y), _addr(xo), h.data_ptr(), B, L, C,
           ctypes.byref(d))
     return (x if xo is None else xo), h
 
@@ -664,6 +681,9 @@ def block_norm_bwd(dh, dx, x, y=None, gate=None, scale=None, shift=None, gain=No
     for the forward (gate, scale and shift are all per sample or all per token).
     `workspace`: a contiguous float32 device tensor of at least
     vidax_block_norm_bwd_workspace_floats values (by default one is allocated)."""
+    if stream is not None:
+        with _on(stream, x):
+            return block_norm_bwd(dh, dx, x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha, workspace)
     i, d, token = _block_desc(x, y, gate, scale, shift, gain, post_gain, norm, post, eps, alpha)
     torch = _torch
     if len(token) > 1:
@@ -685,6 +705,6 @@ def block_norm_bwd(dh, dx, x, y=None, gate=None, scale=None, shift=None, gain=No
     if sums and workspace is None:
         need = _floats("vidax_block_norm_bwd_workspace_floats", i, B, L, C)
     ws = _workspace(workspace, need, i)
-    _call("vidax_block_norm_bwd", i, stream, dh.data_ptr(), _addr(dx), x.data_ptr(), _addr(y), got["dx"].data_ptr(),
+    _call("vidax_block_norm_bwd", i, dh.data_ptr(), _addr(dx), x.data_ptr(), _addr(y), got["dx"].data_ptr(),
           _addr(got.get("dy")), ctypes.byref(g), _addr(ws), 0 if ws is None else ws.numel(), B, L, C, ctypes.byref(d))
     return got

@@ -227,19 +227,43 @@ __device__ __forceinline__ void each_part(const ModCall& c, int pieces, int p, F
   auto unit = [&](int t) { return key_weight(min(len - t * kModRows, kModRows)); };
   auto tile_weight = [&](const Batch& bt, int t) { return kTileStart + Side::visits(c, bt, t) * unit(t); };
   const bool lens = c.s.kv_valid_len || c.s.q_start || c.s.prefix_len;
+  auto wave_sum = [&](int x) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+    return __builtin_amdgcn_readfirstlane(x);
+  };
+  auto scan = [&](int x) {  // with the lane's own
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const int y = __shfl_up(x, m);
+      if (lane >= m) x += y;
+    }
+    return x;
+  };
   auto head_weight = [&](const Batch& bt) {
     int w = 0;
     for (int t = lane; t < nt; t += 64) w += tile_weight(bt, t);
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) w += __shfl_xor(w, m);
-    return __builtin_amdgcn_readfirstlane(w);
+    return wave_sum(w);
   };
-  Batch bt = batch_of(c, 0);
-  int hw = head_weight(bt);
-  int64_t total = (int64_t)hw * heads * c.B;
-  if (lens) {
-    total = (int64_t)hw * heads;
-    for (int b = 1; b < c.B; ++b) total += (int64_t)head_weight(batch_of(c, b)) * heads;
+  // the whole sequence (all weights of a head fit in 31 bits: mod_pieces)
+  Batch bt;
+  int hw = 0, lane_w = 0;  // of a head: of batch b, of batch `lane`
+  int64_t total = 0;
+  if (!lens) {
+    bt = batch_of(c, 0);
+    hw = head_weight(bt);
+    total = (int64_t)hw * c.B * heads;
+  } else if (nt <= kLaneTiles) {
+    const Batch mine = batch_of_lane(c, min(lane, c.B - 1));
+    if (lane < c.B)
+      for (int t = 0; t < nt; ++t) lane_w += tile_weight(mine, t);
+    total = (int64_t)wave_sum(lane_w) * heads;
+  } else {
+    for (int b = 0; b < c.B; ++b) {
+      const int w = head_weight(batch_of(c, b));
+      if (lane == b) lane_w = w;
+      total += (int64_t)w * heads;
+    }
   }
   int64_t per = (total + pieces - 1) / pieces;
   if (per < kLeastPiece) per = kLeastPiece;
@@ -249,16 +273,15 @@ __device__ __forceinline__ void each_part(const ModCall& c, int pieces, int p, F
   int64_t S = 0;  // where the tile begins
   int b = 0;
   if (lens) {
-    while (pos >= S + (int64_t)hw * heads) {  // (ends: pos < total)
-      S += (int64_t)hw * heads;
-      bt = batch_of(c, ++b);
-      hw = head_weight(bt);
-    }
+    const int to = scan(lane_w);
+    b = __builtin_ctzll(__builtin_amdgcn_ballot_w64((int64_t)to * heads > pos));  // (pos < total)
+    hw = __builtin_amdgcn_readlane(lane_w, b);
+    S = (int64_t)__builtin_amdgcn_readlane(to - lane_w, b) * heads;
   } else {
     b = (int)(pos / ((int64_t)hw * heads));
-    bt = batch_of(c, b);
     S = (int64_t)hw * heads * b;
   }
+  bt = batch_of(c, b);
   int h = (int)((pos - S) / hw);
   S += (int64_t)h * hw;
   int t = 0;
@@ -267,12 +290,7 @@ __device__ __forceinline__ void each_part(const ModCall& c, int pieces, int p, F
     int before = 0;
     for (int t0 = 0; t0 < nt; t0 += 64) {
       const int w = t0 + lane < nt ? tile_weight(bt, t0 + lane) : 0;
-      int x = w;
-#pragma unroll
-      for (int m = 1; m < 64; m <<= 1) {
-        const int y = __shfl_up(x, m);
-        if (lane >= m) x += y;
-      }
+      const int x = scan(w);
       const uint64_t over = __builtin_amdgcn_ballot_w64(before + x > rem);
       if (over != 0) {
         const int i = __builtin_ctzll(over);

@@ -71,6 +71,8 @@ constexpr int kTileStart = 8;  // weight of starting and ending a query tile; se
 __host__ __device__ inline int key_weight(int rows) { return rows > 128 ? 4 : 3; }
 // Four key tiles: every piece between a tile's first and last then holds some of it.
 constexpr int kLeastPiece = 16;
+// Tiles of a head up to which a lane adds up those of a batch with lengths of its own.
+constexpr int kLaneTiles = 16;
 
 struct ModPieces {
   int n;          // 0: a workgroup takes a tile (or one of its runs)
@@ -95,23 +97,26 @@ inline int64_t mod_key_tiles(int Lq, int Lk, bool causal) {
 
 // Pieces, one a compute unit and 16 visited tiles at least: 12 us to find and
 // start them and for the joining launch, and the partial rows' (of `row` floats) bytes
-// at 5 TB/s.  A workgroup finds its own by going over the tiles' weights, 64 at a time:
-// not where they are too many for that to be short.  Pieces of a head read its keys at
+// at 5 TB/s.  A workgroup finds its own by going over the tiles' weights, 64 at a time
+// (with lengths those of every batch): not where they are too many for that to be
+// short.  Pieces of a head read its keys at
 // different places; where K and V of a head are more than an L2 (4 MB) that costs 15 %.
 // (Forward, 12 heads, 6144 plain: seven runs 303 us, pieces 260; causal 177 and 154;
 // 1560 rows on 32760 keys: three runs 346, pieces 413.)
 // `own` rows in tiles of 256, of which tile t visits visits(t) tiles of `other` rows.
 template <typename F>
-inline ModPieces mod_pieces(int B, int heads, int own, int other, F&& visits, int cus, size_t first, int row, double tile_us) {
+inline ModPieces mod_pieces(int B, int heads, int own, int other, int64_t most_visits, F&& visits, bool lengths, int cus, size_t first,
+                            int row, double tile_us) {
   ModPieces p{0, 0, 0, 0, 0.0};
   const int64_t nt = (int64_t)mod_tiles(own), wgs = nt * B * heads;
-  if ((nt + 63) / 64 * B > 64) return p;
+  if (lengths ? B > 64 || (nt > kLaneTiles && (nt + 63) / 64 * B > 16) : nt > 4096) return p;
+  if ((__int128)nt * B * (kTileStart + 4 * most_visits) > INT32_MAX) return p;  // (32-bit sums)
   int64_t weight = 0;  // of a head
   for (int64_t t = 0; t < nt; ++t)
     weight += kTileStart + visits(t) * key_weight((int)(own - t * kModRows < kModRows ? own - t * kModRows : kModRows));
   const int64_t all = weight * B * heads, most = all / (4 * kLeastPiece);
   const int n = (int)(most < cus ? most : cus);
-  if (n < 2 || weight > INT32_MAX) return p;
+  if (n < 2) return p;
   p.n = n;
   p.slot_rows = (own < kModRows ? own + 31 : kModRows) / 32 * 32;
   p.cut = first + (size_t)2 * n * p.slot_rows * row;
@@ -191,7 +196,8 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
     }
   }
   if (docs) return r;
-  const ModPieces p = mod_pieces(B, H, Lq, Lk, [&](int64_t t) { return mod_row_tiles(t, Lq, Lk, causal); }, cus, r.part, 129, 2.0);
+  const ModPieces p = mod_pieces(B, H, Lq, Lk, tiles, [&](int64_t t) { return mod_row_tiles(t, Lq, Lk, causal); }, lengths, cus,
+                                 r.part, 129, 2.0);
   if (p.n && p.floats <= max_floats && p.us < best) {
     r.runs = 1;
     r.pieces = p;
@@ -293,7 +299,8 @@ inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool doc
     // are made for streams that are not there, and end unevenly.  (Both with the joining
     // launch; 2 x 4001, 16 heads on 4, causal: runs 301 us, pieces 278; with prefixes of
     // 1000 and 2300: 531 and 321; 2 x 2049 causal: 105 and 116.)
-    ModPieces p = mod_pieces(B, Hkv, Lk, Lq, [&](int64_t t) { return mod_stream((int)t, H / Hkv, Lq, Lk, causal); }, cus, r.part, 256, 4.0);
+    const ModPieces p = mod_pieces(B, Hkv, Lk, Lq, mod_stream(0, H / Hkv, Lq, Lk, false),
+                                   [&](int64_t t) { return mod_stream((int)t, H / Hkv, Lq, Lk, causal); }, lengths, cus, r.part, 256, 4.0);
     if (p.n && p.floats <= max_floats && p.us < best * 4.0 * (lengths ? 1.3 : 0.95)) {
       r.dkdv = p;
       r.runs = 1;
@@ -308,7 +315,8 @@ inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool doc
   const int64_t tiles = ((int64_t)Lk + kModKeys - 1) / kModKeys, rounds = (wgs + cus - 1) / cus;
   const double mean = 1.05 * (double)mod_key_tiles(Lq, Lk, causal) * B * H / cus;
   const double load = causal ? (mean > tiles ? mean : tiles) : (double)rounds * tiles;
-  const ModPieces p = mod_pieces(B, H, Lq, Lk, [&](int64_t t) { return mod_row_tiles(t, Lq, Lk, causal); }, cus, r.part, 128, 2.6);
+  const ModPieces p = mod_pieces(B, H, Lq, Lk, tiles, [&](int64_t t) { return mod_row_tiles(t, Lq, Lk, causal); }, lengths, cus,
+                                 r.part, 128, 2.6);
   if (p.n && p.floats <= max_floats && p.us < load * 2.6 + rounds * 4.0) {
     r.dq = p;
     if (p.floats > r.floats) r.floats = p.floats;

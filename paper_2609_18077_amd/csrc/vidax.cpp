@@ -534,9 +534,12 @@ size_t vidax_attn_mod_fwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, in
   Buf s[6];
   if (mod_common(B, H, Hkv, Lq, Lk, d, 1.0f, nullptr, &c, s) != VIDAX_OK || B == 0 || H == 0 || Lq == 0) return 0;
   const int cus = vidax::device_cu_count();
-  const size_t x = vidax::mod_fwd_split(B, H, Hkv, Lq, Lk, docs != 0 && Lk > 0, false, true, cus, SIZE_MAX).floats;
-  const size_t y = vidax::mod_fwd_split(B, H, Hkv, Lq, Lk, docs != 0 && Lk > 0, true, true, cus, SIZE_MAX).floats;
-  return x > y ? x : y;  // (causal or not)
+  size_t most = 0;
+  for (int i = 0; i < 4; ++i) {  // (causal or not, lengths or not)
+    const size_t n = vidax::mod_fwd_split(B, H, Hkv, Lq, Lk, docs != 0 && Lk > 0, i & 1, i & 2, cus, SIZE_MAX).floats;
+    if (n > most) most = n;
+  }
+  return most;
 }
 
 vidax_status vidax_block_norm_fwd(const void* x, const void* y, void* xo, void* h, int32_t B, int32_t L, int32_t C,

@@ -289,7 +289,8 @@ def test_runs_of_keys_are_joined(Lq, Lk):
 
 # Sizes whose query tiles are cut into pieces of equal weight on 256 compute units
 PIECES = [(3, 16, 4, 296, 3993, "all"), (3, 16, 4, 532, 2375, "valid"), (2, 8, 2, 2814, 2526, "causal"),
-          (1, 8, 2, 4001, 4001, "prefix"), (3, 4, 1, 2934, 5374, "lengths")]
+          (1, 8, 2, 4001, 4001, "prefix"), (3, 4, 1, 2934, 5374, "lengths"),
+          (20, 5, 1, 7, 3100, "lengths"), (2, 3, 1, 4500, 3000, "lengths")]
 
 
 def piece_score(B, H, Lq, Lk, mask):
@@ -304,7 +305,8 @@ def piece_score(B, H, Lq, Lk, mask):
     if mask == "prefix":
         s["prefix_len"] = [1500]
     if mask == "lengths":
-        s |= dict(q_start=[-1000, 300, Lk - Lq], kv_valid_len=[1900, 3000, Lk], prefix_len=[0, 900, 70])
+        s |= {n: [x[b % 3] for b in range(B)] for n, x in (("q_start", (-1000, 300, Lk - Lq)), ("kv_valid_len", (1900, 3000, Lk)),
+                                                           ("prefix_len", (0, 900, 70)))}
     return s, np.asarray(s["slopes"], np.float32).astype(np.float64) if "slopes" in s else None
 
 
@@ -323,6 +325,28 @@ def test_pieces_of_tiles_are_joined(B, H, Hkv, Lq, Lk, mask):
         hs, ks = slice(h, h + 1), slice(h * Hkv // H, h * Hkv // H + 1)
         one = oracle.ScoreSpec(**{**s, "slopes": slopes[hs] if slopes is not None else None})
         compare(o[:, :, hs], lse[:, hs], q[:, :, hs], k[:, :, ks], v[:, :, ks], SCALE, one, f"pieces {Lq}x{Lk} {mask} head {h}")
+
+
+def test_on_a_stream_beside_the_current_one():
+    """Outputs and workspace belong to the stream given: nothing that the current stream still runs or takes next is
+    touched, nor the other way round."""
+    import torch
+
+    q, k, v = make(1, 8, 2, 4001, 4001, 6)
+    score, _ = dev_score(causal=True)
+    ref, lse = vx.attn_mod_fwd(q, k, v, score, return_lse=True)
+    grads = vx.attn_mod_bwd(q, k, v, ref, q, lse, score)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for n in range(4):
+        got = vx.attn_mod_fwd(q, k, v, score, return_lse=True, stream=side)
+        dgot = vx.attn_mod_bwd(q, k, v, *got[:1], q, got[1], score, stream=side)
+        for size in (1 << 24, 1 << 25):  # the sizes of what the calls have just let go
+            torch.empty(size, device="cuda").fill_(float("nan"))
+        side.synchronize()
+        assert torch.equal(got[0], ref) and torch.equal(got[1], lse), n
+        assert all(torch.equal(a, b) for a, b in zip(dgot, grads)), n
+    torch.cuda.synchronize()
 
 
 def test_pieces_in_a_graph():

@@ -19,6 +19,11 @@
  *                   (Lk = text length, no rotation) and joint video+text
  *                   attention (rotation on the video prefix only).
  *
+ * Beside these: the gradient of the attention, the Q/K prologue and the Q/K/V
+ * projection, neighbourhood attention, attention with score modifiers
+ * (vidax_attn_mod_fwd and _bwd: documents, causality, cap, distance bias, shared
+ * K/V heads) and the step between two sublayers (vidax_block_norm_fwd and _bwd).
+ *
  * Conventions shared by every entry point
  *   Layout    dense B x L x H x d ("BSHD"): element (b, n, h, c) sits at
  *             ((b * L + n) * H + h) * d + c, bfloat16 storage.  Offsets are

@@ -18,13 +18,15 @@ constexpr int kStartLimit = 1 << 30;  // positions stay within +- 2^30 + L
 // log2 e, ku = |scale| / cap).
 struct Scores {
   float mul, ku;
-  float poly[5], limit; // capped, the forward's form of y (cap16_log2)
+  float tanh_poly[4], poly[4], limit;  // capped: t, and the forward's form of y (cap16_log2)
   uint32_t qxor, qand;  // applied to q's bf16 pairs: sign of scale, zero where it is 0
 };
 
-// tanh(u) = u (1 + k1 u^2 + ... + k4 u^8) up to 1.2e-7 of itself for |u| <= 1/2
-// (least squares on Chebyshev points).
-constexpr float kTanh[5] = {1.f, -3.333331048e-1f, 1.333051324e-1f, -5.339105427e-2f, 1.799921878e-2f};
+// tanh(u) = u (k0 + k1 u^2 + k2 u^4 + k3 u^6) up to 3.2e-7 of itself for |u| <= 0.45
+// (weighted least squares; five terms up to 1/2 are good to 1.2e-7 and cost a twelfth
+// of the capped forward's vector work).
+constexpr float kTanhMost = 0.45f;
+constexpr float kTanh[4] = {9.999997616e-1f, -3.332946599e-1f, 1.323636919e-1f, -4.602819309e-2f};
 
 inline Scores make_scores(const ModCall& c) {
   Scores s;
@@ -33,61 +35,53 @@ inline Scores make_scores(const ModCall& c) {
   s.qand = a == 0.f ? 0u : 0xffffffffu;
   s.ku = c.s.cap > 0.f ? a / c.s.cap : 0.f;
   s.mul = c.s.cap > 0.f ? c.s.cap * kLog2e : a == 0.f ? 1.f : a * kLog2e;
-  // mul tanh(ku x) = x (p0 + p1 x^2 + ...) for |x| <= limit; never where a factor could overflow
-  float k = s.mul * s.ku;
-  for (int i = 0; i < 5; ++i, k *= s.ku * s.ku) s.poly[i] = kTanh[i] * k;
-  s.limit = s.ku == 0.f ? INFINITY : s.ku < 100.f ? 0.5f / s.ku : -1.f;
+  // tanh(ku x) = x (p0 + p1 x^2 + ...) for |x| <= limit; never where a factor could overflow
+  float k = s.ku;
+  for (int i = 0; i < 4; ++i, k *= s.ku * s.ku) {
+    s.tanh_poly[i] = kTanh[i] * k;
+    s.poly[i] = s.mul * s.tanh_poly[i];
+  }
+  s.limit = s.ku == 0.f ? INFINITY : s.ku < 100.f && fabsf(s.poly[3]) < 1e30f ? kTanhMost / s.ku : -1.f;
   return s;
 }
 
-// tanh of 16 products times ku, in place.  The odd polynomial where the whole
-// wave's block stays within 1/2, else the exponential, whose absolute error of 1e-7
-// is then small against the block's largest score.
-__device__ __forceinline__ float tanh_small(float u) {
-  const float w = u * u;
-  float p = fmaf(w, kTanh[4], kTanh[3]);
-  p = fmaf(w, p, kTanh[2]);
-  p = fmaf(w, p, kTanh[1]);
-  p = fmaf(w, p, kTanh[0]);
-  return u * p;
+// tanh(ku x) of 16 products, in place.  The odd polynomial, ku folded in, where the
+// whole wave's block stays within its limit, else the exponential, whose absolute error
+// of 1e-7 is then small against the block's largest score.
+__device__ __forceinline__ float odd_poly(float x, const float p[4], float n) {  // + n
+  const float w = x * x;
+  float y = fmaf(w, p[3], p[2]);
+  y = fmaf(w, y, p[1]);
+  y = fmaf(w, y, p[0]);
+  return fmaf(x, y, n);
 }
 __device__ __forceinline__ float tanh_any(float u) {
   const float e = __builtin_amdgcn_exp2f(u * (2.f * kLog2e));
   return fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f);
 }
-__device__ __forceinline__ float largest16(const f32x16& s) {
+__device__ __forceinline__ bool within16(const f32x16& s, const Scores& c) {  // (uniform)
   float m = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(s[i]));
-  return m;
+  return __builtin_amdgcn_ballot_w64(!(m <= c.limit)) == 0;
 }
-__device__ __forceinline__ void cap16(f32x16& s, float ku) {
+__device__ __forceinline__ void cap16(f32x16& s, const Scores& c) {
+  if (within16(s, c)) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s[i] *= ku;
-  if (__builtin_amdgcn_ballot_w64(!(largest16(s) <= 0.5f)) == 0) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = tanh_small(s[i]);
+    for (int i = 0; i < 16; ++i) s[i] = odd_poly(s[i], c.tanh_poly, 0.f);
   } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = tanh_any(s[i]);
+    for (int i = 0; i < 16; ++i) s[i] = tanh_any(s[i] * c.ku);
   }
 }
-// The same as y = mul tanh(ku x), the factors folded into the polynomial: six
-// operations a score where tanh and its factors take eight.
-__device__ __forceinline__ void cap16_log2(f32x16& s, const Scores& c) {
-  if (__builtin_amdgcn_ballot_w64(!(largest16(s) <= c.limit)) == 0) {
+// y + n = mul tanh(ku x) + n, all factors folded in: five operations a score.
+__device__ __forceinline__ void cap16_log2(f32x16& s, const Scores& c, float n) {
+  if (within16(s, c)) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float w = s[i] * s[i];
-      float p = fmaf(w, c.poly[4], c.poly[3]);
-      p = fmaf(w, p, c.poly[2]);
-      p = fmaf(w, p, c.poly[1]);
-      p = fmaf(w, p, c.poly[0]);
-      s[i] *= p;
-    }
+    for (int i = 0; i < 16; ++i) s[i] = odd_poly(s[i], c.poly, n);
   } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = c.mul * tanh_any(s[i] * c.ku);
+    for (int i = 0; i < 16; ++i) s[i] = fmaf(c.mul, tanh_any(s[i] * c.ku), n);
   }
 }
 

@@ -307,7 +307,7 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a, const Part& part) {
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
 
-  const float mul = a.sc.mul, ku = a.sc.ku;
+  const float mul = a.sc.mul;
   const float slope = BIAS ? -c.s.slopes[h] * kLog2e : 0.f;
   // One tile, one slot a product, as in the dense backward: each slot issues the
   // operand reads of the product three slots on and its share of the vector work.
@@ -388,8 +388,8 @@ __device__ __forceinline__ void dq_body(const BwdArgs& a, const Part& part) {
         read_op(std::integral_constant<int, decltype(N)::value + 3>());
         SLOT();
       });
-      cap16(sc[0], ku);
-      cap16(sc[1], ku);
+      cap16(sc[0], a.sc);
+      cap16(sc[1], a.sc);
       if (!t.whole()) {
         hidden(0, sc[0]);
         hidden(1, sc[1]);
@@ -671,7 +671,7 @@ __device__ __forceinline__ void dkdv_body(const BwdArgs& a, const Part& part) {
     if (wave == 2 && docs && !t.one()) copy_row(c.s.q_doc + (size_t)b * c.Lq, t.t, c.Lq, Qd[buf], lane);
   };
   const RowOffsets off = row_offsets(lane);
-  const float mul = a.sc.mul, ku = a.sc.ku;
+  const float mul = a.sc.mul;
   // One 32-query block of a tile, one slot a product (as in the dense backward).
   // Without a cap P is formed beside dP; with one the scores' tanh comes first.
   auto block = [&](int blk, auto par, const Tile& t, const uint16_t* qt, const uint16_t* ot, float slope)
@@ -731,7 +731,7 @@ __device__ __forceinline__ void dkdv_body(const BwdArgs& a, const Part& part) {
       SLOT();
     }
     if (CAP) {
-      cap16(s, ku);
+      cap16(s, a.sc);
       if (!t.whole()) hidden(s);
     }
 #pragma unroll

@@ -201,7 +201,7 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_mod_few_kernel(FewArgs a) {
     f32x16 s = f32x16{};
 #pragma unroll
     for (int st = 0; st < 8; ++st) s = mfma32(read_row(kb, off.row, st), qop[st], s);
-    if (a.c.s.cap > 0.f) cap16_log2(s, a.sc);  // uniform
+    if (a.c.s.cap > 0.f) cap16_log2(s, a.sc, 0.f);  // uniform
     // y; -inf for what the row does not see
     const float dist = (float)(pos - t.t * BN - 4 * hi);
     const int left = lim - t.t * BN - 4 * hi;

@@ -20,8 +20,9 @@
 //     sum of 0: o = 0, lse = -inf.  Keys that no row may see (past
 //     the valid length or the last row's position, or of a negative document) are
 //     read as zeros, so that nothing that lies there reaches the output.
-//   Sums add the fp32 probabilities, not their bf16 roundings: the log-sum-exp is
-//     then good to fp32, and costs eight additions a block more.
+//   Sums: of the bf16 roundings of the weights (which the output is divided by) and,
+//     where the log-sum-exps are wanted, of the weights: good to fp32, a sixteenth
+//     more vector work (16384 x 12 heads: 1483 us without, 1550 with).
 //   Few tiles of rows, or uneven ones: the keys are cut into runs, or all tiles'
 //     keys into pieces of equal weight (attn_mod.hpp), a workgroup each, whose
 //     normalised fp32 outputs and log-sum-exps a second launch joins.
@@ -42,6 +43,7 @@ constexpr int NT = NW * 64;
 constexpr int TILE = BN * D;  // elements of a K or V tile
 constexpr int BLK = 512;      // elements of an operand block
 constexpr float kUnset = 1e30f;
+constexpr float kFoldMost = 80.f;  // a row of scores at -cap has weights of 2^-80
 
 struct FwdArgs {
   ModCall c;
@@ -60,8 +62,9 @@ struct FwdArgs {
   int kr, qr;      // document ranges a batch
 };
 
-// CAP, BIAS: the scores' modifiers.  PIECES: the part of a query tile's keys given.
-template <bool CAP, bool BIAS, bool PIECES>
+// CAP, BIAS: the scores' modifiers.  LSE: the log-sum-exps are wanted.  PIECES: the part
+// of a query tile's keys given.
+template <bool CAP, bool BIAS, bool LSE, bool PIECES>
 __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
   __shared__ __attribute__((aligned(16))) uint16_t K0[TILE], K1[TILE], V0[TILE], V1[TILE];
   __shared__ __attribute__((aligned(16))) int Kd[2][BN];  // ids of the tiles' keys, where they differ
@@ -234,10 +237,15 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
   f32x16 oacc[4];
 #pragma unroll
   for (int mb = 0; mb < 4; ++mb) oacc[mb] = f32x16{};
-  float mref = -INFINITY;  // the row's reference, log2 units
-  float nm = kUnset;       // -mref
-  float lsum = 0.f;        // this lane half's sum
-  const float slope = BIAS ? -c.s.slopes[h] * kLog2e : 0.f;
+  // Capped scores without a bias lie within +-mul; up to kFoldMost of it they need no
+  // reference of their own: it starts at 0 and is added with the cap (one operation a
+  // score less); a sum that grows beyond the limit still moves it.
+  constexpr bool FOLD = CAP && !BIAS;
+  float mref = FOLD ? 0.f : -INFINITY;  // the row's reference, log2 units
+  float nm = FOLD ? 0.f : kUnset;       // -mref
+  float lsum = 0.f;        // this lane half's sum of the weights
+  float wsum = 0.f;        // and of their roundings
+  const float slope = BIAS && c.s.slopes ? -c.s.slopes[h] * kLog2e : 0.f;
   // Of the tile at hand: the factor of its scores, and the bias as a linear function of
   // the key, slope |p - j| = lin - lin_slope (j - first key of the lane half).  A tile
   // on both sides of the wave's positions (a few of a wave's) has what is missing added
@@ -263,38 +271,50 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
 
   // y + n of element i of block blk; with a bias n holds lin
   auto logit = [&](float s, float n, int blk, int i) __attribute__((always_inline)) {
+    if (FOLD) return s;
     float y = CAP ? s + n : fmaf(s, mul, n);
     if (BIAS) y = fmaf(lin_slope, -(float)(32 * blk + 8 * (i >> 2) + (i & 3)), y);
     return y;
   };
   // P of elements i, i + 1 of a block (one rounding of the weights, 2^-9 of each,
-  // independent; the sum adds them before it)
-  auto exps = [&](const f32x16& s, int blk, int i, float n, uint32_t pw[8], float& sum) __attribute__((always_inline)) {
+  // independent).  The output is divided by the sum of the rounded weights, so that the
+  // rounding of one that carries a row cancels; the log-sum-exp is of the sum before.
+  auto exps = [&](const f32x16& s, int blk, int i, float n, uint32_t pw[8], float sum[2]) __attribute__((always_inline)) {
     const float p0 = __builtin_amdgcn_exp2f(logit(s[i], n, blk, i));
     const float p1 = __builtin_amdgcn_exp2f(logit(s[i + 1], n, blk, i + 1));
     pw[i >> 1] = pack_bf16x2(p0, p1);
-    sum += p0;
-    sum += p1;
+    sum[1] = dot2(pw[i >> 1], 0x3f803f80u, sum[1]);
+    if (LSE) {
+      sum[0] += p0;
+      sum[0] += p1;
+    }
   };
   // The block's sum is not below 2^64 for some row: new references, the output and
   // sum rescaled, the block's weights formed again
-  auto reset = [&](const f32x16& s, int blk, uint32_t pw[8], float& sum) __attribute__((always_inline)) {
-    float m = logit(s[0], lin, blk, 0);
+  auto reset = [&](f32x16 s[2], int blk, uint32_t pw[8], float sum[2]) __attribute__((always_inline)) {
+    float m = logit(s[blk][0], lin, blk, 0);
 #pragma unroll
-    for (int i = 1; i < 16; ++i) m = fmaxf(m, logit(s[i], lin, blk, i));
-    const float mnew = fmaxf(mref, wave_half_max(m));
+    for (int i = 1; i < 16; ++i) m = fmaxf(m, logit(s[blk][i], lin, blk, i));
+    const float mnew = fmaxf(mref, wave_half_max(m) - (FOLD ? nm : 0.f));
     const bool set = mnew > -INFINITY;
     const float alpha = set ? __builtin_amdgcn_exp2f(mref - mnew) : 1.f;
     lsum *= alpha;
+    wsum *= alpha;
 #pragma unroll
     for (int mb = 0; mb < 4; ++mb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
+    if (FOLD) {  // what the tile's scores already hold
+#pragma unroll
+      for (int z = blk; z < 2; ++z)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[z][i] -= mnew + nm;
+    }
     mref = mnew;
     nm = set ? -mnew : kUnset;
-    sum = 0.f;
+    sum[0] = sum[1] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) exps(s, blk, i, nm + lin, pw, sum);
+    for (int i = 0; i < 16; i += 2) exps(s[blk], blk, i, nm + lin, pw, sum);
   };
   // The scores of the next tile (K in kb) and the softmax and PV of this one (V in
   // vb), hand-scheduled: a slot a product, each also issuing the operand reads of
@@ -312,7 +332,7 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
       }
     };
     uint32_t pw[2][8];
-    float sum[2] = {0.f, 0.f};
+    float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
     auto p_op = [&](int blk, int k2) __attribute__((always_inline)) {
       return __builtin_bit_cast(bf16x8, make_uint4(pw[blk][4 * k2], pw[blk][4 * k2 + 1], pw[blk][4 * k2 + 2], pw[blk][4 * k2 + 3]));
     };
@@ -326,8 +346,9 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
       if constexpr ((n & 1) == 0) exps(s[0], 0, n, n0, pw[0], sum[0]);
       SLOT();
     });
-    if (__builtin_amdgcn_ballot_w64(!(sum[0] < kSumLimit)) != 0) reset(s[0], 0, pw[0], sum[0]);
-    lsum += sum[0];
+    if (__builtin_amdgcn_ballot_w64(!(sum[0][1] < kSumLimit)) != 0) reset(s, 0, pw[0], sum[0]);
+    lsum += sum[0][0];
+    wsum += sum[0][1];
     n0 = BIAS ? nm + lin : nm;
     SLOT();
     for_slots<8>([&](auto N) __attribute__((always_inline)) {  // PV of block 0; exponentials of block 1
@@ -337,8 +358,9 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
       exps(s[1], 1, 2 * n, n0, pw[1], sum[1]);
       SLOT();
     });
-    if (__builtin_amdgcn_ballot_w64(!(sum[1] < kSumLimit)) != 0) reset(s[1], 1, pw[1], sum[1]);
-    lsum += sum[1];
+    if (__builtin_amdgcn_ballot_w64(!(sum[1][1] < kSumLimit)) != 0) reset(s, 1, pw[1], sum[1]);
+    lsum += sum[1][0];
+    wsum += sum[1][1];
     SLOT();
     for_slots<8>([&](auto N) __attribute__((always_inline)) {  // PV of block 1
       constexpr int n = decltype(N)::value;
@@ -372,8 +394,8 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
   // ---- output, whole rows through the staging area; empty rows: o = 0, lse = -inf
   const size_t nrow = (size_t)c.B * c.H * c.Lq, orow = ((size_t)b * c.H + h) * c.Lq;
   auto store_o = [&]() __attribute__((always_inline)) {
-    const float l = wave_half_sum(lsum);
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const float w = wave_half_sum(wsum), l = LSE ? wave_half_sum(lsum) : w;
+    const float inv = w == 0.f ? 0.f : 1.0f / w;
     const float lse2 = l == 0.f ? -INFINITY : mref + __log2f(l);
     if (PIECES ? !part.whole() : a.po != nullptr) {  // fp32 rows of this run or part
       if (qlive) {
@@ -478,8 +500,8 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
     // (at the ends of what it sees) does the other on whatever is there, unseen.
     if (cur.mine() || nxt.mine()) {
       if (CAP) {
-        cap16_log2(scur[0], a.sc);
-        cap16_log2(scur[1], a.sc);
+        cap16_log2(scur[0], a.sc, FOLD ? nm : 0.f);
+        cap16_log2(scur[1], a.sc, FOLD ? nm : 0.f);
       }
       if (BIAS) straddle(scur, cur.t);
       if (!(cur.mine() && cur.whole())) mask(scur, cur, Kd[P]);
@@ -497,21 +519,21 @@ __device__ __forceinline__ void fwd_body(const FwdArgs& a, const Part& part) {
   store_o();
 }
 
-template <bool CAP, bool BIAS>
+template <bool CAP, bool BIAS, bool LSE>
 __global__ __launch_bounds__(NT) void attn_mod_fwd_kernel(FwdArgs a) {
-  fwd_body<CAP, BIAS, false>(a, Part{});
+  fwd_body<CAP, BIAS, LSE, false>(a, Part{});
 }
-template <bool CAP, bool BIAS>
+template <bool CAP, bool BIAS, bool LSE>
 __device__ __forceinline__ void pieces_body(const FwdArgs& a) {
   each_part<QuerySide>(a.c, a.pieces.n, piece_of(blockIdx.x, a.pieces.n), [&](const Part& part) __attribute__((always_inline)) {
     if (threadIdx.x == 0) note_cut<QuerySide>(a.pieces, a.c, part);
-    fwd_body<CAP, BIAS, true>(a, part);
+    fwd_body<CAP, BIAS, LSE, true>(a, part);
     __syncthreads();  // (the staging areas)
   });
 }
-template <bool CAP, bool BIAS>
+template <bool CAP, bool BIAS, bool LSE>
 __global__ __launch_bounds__(NT) void attn_mod_pieces_kernel(FwdArgs a) {
-  pieces_body<CAP, BIAS>(a);
+  pieces_body<CAP, BIAS, LSE>(a);
 }
 
 // Ranges of document ids of every 32 tokens: a wave takes 64 tokens of a batch.
@@ -733,6 +755,12 @@ hipError_t launch_mod_join(const ModFwd& f, const ModSplit& s, hipStream_t strea
 }  // namespace
 
 hipError_t launch_attn_mod_fwd(const ModFwd& f, hipStream_t stream) {
+#define LAUNCH_LSE(kernel, grid, CAP, BIAS)                                                       \
+  (a.lse ? launch_kernel(kernel<CAP, BIAS, true>, grid, (unsigned)NT, stream, a)                  \
+         : launch_kernel(kernel<CAP, BIAS, false>, grid, (unsigned)NT, stream, a))
+#define LAUNCH(kernel, grid)                                                                      \
+  (cap ? (bias ? LAUNCH_LSE(kernel, grid, true, true) : LAUNCH_LSE(kernel, grid, true, false))    \
+       : (bias ? LAUNCH_LSE(kernel, grid, false, true) : LAUNCH_LSE(kernel, grid, false, false)))
   const ModCall& c = f.c;
   const ModSplit s = mod_fwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr, c.s.causal != 0,
                                    c.s.kv_valid_len || c.s.q_start, device_cu_count(), f.ws_floats);
@@ -756,27 +784,23 @@ hipError_t launch_attn_mod_fwd(const ModFwd& f, hipStream_t stream) {
   hipError_t e = launch_mod_ranges(c, f.ws, !s.few && a.sorted, false, &a.r, stream);
   if (e != hipSuccess) return e;
   if (s.few) return launch_mod_few(f, s, a.r, stream);
+  // (a cap too large to fold its reference: the kernel with a bias, which is then 0)
+  const bool cap = c.s.cap > 0.f, bias = c.s.slopes || (cap && a.sc.mul > kFoldMost);
   if (s.pieces.n) {
     a.po = f.ws + s.part;
     a.pl = a.po + (size_t)2 * s.pieces.n * s.pieces.slot_rows * D;
     a.pieces = Pieces{s.pieces.n, s.pieces.slot_rows, reinterpret_cast<int32_t*>(f.ws + s.pieces.cut)};
-    const bool cap = c.s.cap > 0.f, bias = c.s.slopes != nullptr;
-    e = cap ? (bias ? launch_kernel(attn_mod_pieces_kernel<true, true>, (unsigned)s.pieces.n, (unsigned)NT, stream, a)
-                    : launch_kernel(attn_mod_pieces_kernel<true, false>, (unsigned)s.pieces.n, (unsigned)NT, stream, a))
-            : (bias ? launch_kernel(attn_mod_pieces_kernel<false, true>, (unsigned)s.pieces.n, (unsigned)NT, stream, a)
-                    : launch_kernel(attn_mod_pieces_kernel<false, false>, (unsigned)s.pieces.n, (unsigned)NT, stream, a));
+    e = LAUNCH(attn_mod_pieces_kernel, (unsigned)s.pieces.n);
     if (e != hipSuccess) return e;
     const PieceJoinArgs j{a.po, a.pl, f.o, f.lse, a.pieces, c.H, c.Lq, a.ntile};
     return launch_kernel(mod_piece_join_kernel, (unsigned)(a.ntile * c.B * c.H * 16), 256u, stream, j);
   }
   for (int r = 0; r < kMostRuns; ++r) a.in_run[r] = a.r.q_order ? a.ntile * c.B : a.ntile;
-  const bool cap = c.s.cap > 0.f, bias = c.s.slopes != nullptr;
-  e = cap ? (bias ? launch_kernel(attn_mod_fwd_kernel<true, true>, (unsigned)a.nwg, (unsigned)NT, stream, a)
-                  : launch_kernel(attn_mod_fwd_kernel<true, false>, (unsigned)a.nwg, (unsigned)NT, stream, a))
-          : (bias ? launch_kernel(attn_mod_fwd_kernel<false, true>, (unsigned)a.nwg, (unsigned)NT, stream, a)
-                  : launch_kernel(attn_mod_fwd_kernel<false, false>, (unsigned)a.nwg, (unsigned)NT, stream, a));
+  e = LAUNCH(attn_mod_fwd_kernel, (unsigned)a.nwg);
   if (e != hipSuccess || s.runs == 1) return e;
   return launch_mod_join(f, s, stream);
+#undef LAUNCH
+#undef LAUNCH_LSE
 }
 
 }  // namespace vidax

@@ -624,6 +624,40 @@ __global__ __launch_bounds__(1024) void mod_order_kernel(OrderArgs a) {
   }
 }
 
+// Eight values of a row from its partial results p0 .. p1, row at(p) each: sum_p
+// 2^(lse_p - max) o_p / sum_p 2^(lse_p - max).  A part that saw nothing wrote zeros:
+// weight 0.
+struct Joined {
+  uint4 o;
+  float lse;  // natural
+};
+template <typename At>
+__device__ __forceinline__ Joined join_parts(const float* po, const float* pl, int p0, int p1, At&& at) {
+  float m = -INFINITY;
+#pragma unroll 4
+  for (int p = p0; p <= p1; ++p) m = fmaxf(m, pl[at(p)]);
+  const float ref = m > -INFINITY ? m : 0.f;
+  float4 x0 = make_float4(0.f, 0.f, 0.f, 0.f), x1 = x0;
+  float l = 0.f;
+#pragma unroll 4
+  for (int p = p0; p <= p1; ++p) {
+    const float w = __builtin_amdgcn_exp2f(pl[at(p)] - ref);
+    const float4 u = *reinterpret_cast<const float4*>(po + at(p) * D);
+    const float4 v = *reinterpret_cast<const float4*>(po + at(p) * D + 4);
+    l += w;
+    x0.x = fmaf(w, u.x, x0.x); x0.y = fmaf(w, u.y, x0.y); x0.z = fmaf(w, u.z, x0.z); x0.w = fmaf(w, u.w, x0.w);
+    x1.x = fmaf(w, v.x, x1.x); x1.y = fmaf(w, v.y, x1.y); x1.z = fmaf(w, v.z, x1.z); x1.w = fmaf(w, v.w, x1.w);
+  }
+  const float inv = l > 0.f ? 1.0f / l : 0.f;
+  Joined y;
+  y.o.x = pack_bf16x2(x0.x * inv, x0.y * inv);
+  y.o.y = pack_bf16x2(x0.z * inv, x0.w * inv);
+  y.o.z = pack_bf16x2(x1.x * inv, x1.y * inv);
+  y.o.w = pack_bf16x2(x1.z * inv, x1.w * inv);
+  y.lse = l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
+  return y;
+}
+
 // Joins the parts of the tiles that pieces have cut: 16 rows a workgroup, 8 values of a
 // row a thread.
 struct PieceJoinArgs {
@@ -641,36 +675,14 @@ __global__ __launch_bounds__(256) void mod_piece_join_kernel(PieceJoinArgs a) {
   const int bh = tile / a.ntile, r = 16 * sub + (threadIdx.x >> 4), i = (tile - bh * a.ntile) * BM + r;
   if (i >= a.Lq) return;
   const int b = bh / a.H, h = bh - b * a.H, ch = 8 * (threadIdx.x & 15);
-  // o = sum_p 2^(lse_p - max) o_p / sum_p 2^(lse_p - max); a part that saw nothing
-  // wrote zeros: weight 0
-  auto at = [&](int p) { return (size_t)(2 * p + (p == p0)) * a.pieces.slot_rows + r; };
-  float m = -INFINITY;
-#pragma unroll 4
-  for (int p = p0; p <= p1; ++p) m = fmaxf(m, a.pl[at(p)]);
-  const float ref = m > -INFINITY ? m : 0.f;
-  float4 x0 = make_float4(0.f, 0.f, 0.f, 0.f), x1 = x0;
-  float l = 0.f;
-#pragma unroll 4
-  for (int p = p0; p <= p1; ++p) {
-    const float w = __builtin_amdgcn_exp2f(a.pl[at(p)] - ref);
-    const float4 u = *reinterpret_cast<const float4*>(a.po + at(p) * D + ch);
-    const float4 v = *reinterpret_cast<const float4*>(a.po + at(p) * D + ch + 4);
-    l += w;
-    x0.x = fmaf(w, u.x, x0.x); x0.y = fmaf(w, u.y, x0.y); x0.z = fmaf(w, u.z, x0.z); x0.w = fmaf(w, u.w, x0.w);
-    x1.x = fmaf(w, v.x, x1.x); x1.y = fmaf(w, v.y, x1.y); x1.z = fmaf(w, v.z, x1.z); x1.w = fmaf(w, v.w, x1.w);
-  }
-  const float inv = l > 0.f ? 1.0f / l : 0.f;
-  uint4 o;
-  o.x = pack_bf16x2(x0.x * inv, x0.y * inv);
-  o.y = pack_bf16x2(x0.z * inv, x0.w * inv);
-  o.z = pack_bf16x2(x1.x * inv, x1.y * inv);
-  o.w = pack_bf16x2(x1.z * inv, x1.w * inv);
-  *reinterpret_cast<uint4*>(a.o + (((size_t)b * a.Lq + i) * a.H + h) * D + ch) = o;
-  if (a.lse && ch == 0) a.lse[(size_t)bh * a.Lq + i] = l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
+  const Joined y = join_parts(a.po + ch, a.pl, p0, p1,
+                              [&](int p) { return (size_t)(2 * p + (p == p0)) * a.pieces.slot_rows + r; });
+  *reinterpret_cast<uint4*>(a.o + (((size_t)b * a.Lq + i) * a.H + h) * D + ch) = y.o;
+  if (a.lse && ch == 0) a.lse[(size_t)bh * a.Lq + i] = y.lse;
 }
 
-// Joins the runs of every (batch, head, query): a wave a row, lane l its
-// channels 2 l, 2 l + 1.  o = sum_r 2^(lse_r - max) o_r / sum_r 2^(lse_r - max).
+// Joins the runs of every (batch, head, query): 16 rows a workgroup, 8 values of a row a
+// thread.  o = sum_r 2^(lse_r - max) o_r / sum_r 2^(lse_r - max).
 struct JoinArgs {
   const float *po, *pl;
   uint16_t* o;
@@ -679,28 +691,13 @@ struct JoinArgs {
 };
 __global__ __launch_bounds__(256) void mod_join_kernel(JoinArgs a) {
   const size_t nrow = (size_t)a.B * a.H * a.Lq;
-  const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // (b, h, i)
+  const size_t row = (size_t)blockIdx.x * 16 + (threadIdx.x >> 4);  // (b, h, i)
   if (row >= nrow) return;
-  const int lane = threadIdx.x & 63;
-  float m = -INFINITY;
-  for (int r = 0; r < a.runs; ++r) m = fmaxf(m, a.pl[r * nrow + row]);
-  float x = 0.f, y = 0.f, l = 0.f;
-  if (m > -INFINITY) {
-#pragma unroll 4
-    for (int r = 0; r < a.runs; ++r) {
-      const float w = __builtin_amdgcn_exp2f(a.pl[r * nrow + row] - m);
-      const float2 v = *reinterpret_cast<const float2*>(a.po + (r * nrow + row) * D + 2 * lane);
-      l += w;  // (a run that saw nothing wrote zeros: weight 0)
-      x = fmaf(w, v.x, x);
-      y = fmaf(w, v.y, y);
-    }
-    const float inv = 1.0f / l;
-    x *= inv;
-    y *= inv;
-  }
   const size_t i = row % a.Lq, bh = row / a.Lq, b = bh / a.H, h = bh % a.H;
-  *reinterpret_cast<uint32_t*>(a.o + ((b * a.Lq + i) * a.H + h) * D + 2 * lane) = pack_bf16x2(x, y);
-  if (a.lse && lane == 0) a.lse[row] = m > -INFINITY ? (m + __log2f(l)) * kLn2 : -INFINITY;
+  const int ch = 8 * (threadIdx.x & 15);
+  const Joined y = join_parts(a.po + ch, a.pl, 0, a.runs - 1, [&](int r) { return r * nrow + row; });
+  *reinterpret_cast<uint4*>(a.o + ((b * a.Lq + i) * a.H + h) * D + ch) = y.o;
+  if (a.lse && ch == 0) a.lse[row] = y.lse;
 }
 
 }  // namespace
@@ -750,7 +747,7 @@ hipError_t launch_mod_join(const ModFwd& f, const ModSplit& s, hipStream_t strea
   a.H = f.c.H;
   a.Lq = f.c.Lq;
   a.runs = s.runs;
-  return launch_kernel(mod_join_kernel, (unsigned)((nrow + 3) / 4), 256u, stream, a);
+  return launch_kernel(mod_join_kernel, (unsigned)((nrow + 15) / 16), 256u, stream, a);
 }
 }  // namespace
 

@@ -86,7 +86,10 @@ def check(q, k, v, scale=None, what="", workspace=None, **s):
 
     score, spec = dev_score(**s)
     o, lse = vx.attn_mod_fwd(q, k, v, score, scale=scale, return_lse=True, workspace=workspace)
+    alone = vx.attn_mod_fwd(q, k, v, score, scale=scale, workspace=workspace)
     torch.cuda.synchronize()
+    # without the log-sum-exps: the same but for the weights of parts that are joined, good to a rounding of the sums
+    assert (alone.double() - o.double()).norm() <= 2.0 ** -9 * o.double().norm(), what
     return compare(o, lse, q, k, v, SCALE if scale is None else float(np.float32(scale)), spec, what)
 
 
@@ -290,7 +293,7 @@ def test_runs_of_keys_are_joined(Lq, Lk):
 # Sizes whose query tiles are cut into pieces of equal weight on 256 compute units
 PIECES = [(3, 16, 4, 296, 3993, "all"), (3, 16, 4, 532, 2375, "valid"), (2, 8, 2, 2814, 2526, "causal"),
           (1, 8, 2, 4001, 4001, "prefix"), (3, 4, 1, 2934, 5374, "lengths"),
-          (20, 5, 1, 7, 3100, "lengths"), (2, 3, 1, 4500, 3000, "lengths")]
+          (20, 5, 1, 7, 3100, "lengths"), (2, 3, 1, 4500, 3000, "lengths"), (1, 8, 2, 4001, 4001, "capped")]
 
 
 def piece_score(B, H, Lq, Lk, mask):
@@ -298,6 +301,8 @@ def piece_score(B, H, Lq, Lk, mask):
     s = {}
     if mask in ("lengths", "prefix"):
         s = dict(cap=20.0, slopes=list(0.01 * np.arange(H)))
+    if mask == "capped":
+        s = dict(cap=20.0)
     if mask not in ("all", "valid"):
         s["causal"] = True
     if mask == "valid":

@@ -532,7 +532,7 @@ __device__ __forceinline__ void dkdv_body(const BwdArgs& a, const Part& part) {
   auto look = [&](int s) __attribute__((always_inline)) {
     const int t = 64 * s + lane;
     bool v = t >= qa && t < qb;
-    fl = (wlive && t * BN + BN - 1 >= wrmin ? Tile::kMine : 0) | (t * BN >= wrmax ? Tile::kWhole : 0) | Tile::kOne;
+    fl = (wlive && t * BN + BN - 1 >= wrmin ? Tile::kMine : 0) | (t * BN >= wrmax && t * BN + BN <= c.Lq ? Tile::kWhole : 0) | Tile::kOne;
     if (v) {
       const int2 e = *reinterpret_cast<const int2*>(a.empty + (size_t)b * a.qr + 2 * t);
       if (e.x != 0 || (t * BN + 32 < c.Lq && e.y != 0)) fl |= Tile::kZero;
@@ -650,7 +650,8 @@ __device__ __forceinline__ void dkdv_body(const BwdArgs& a, const Part& part) {
     }
   }
   const size_t qbase = (size_t)b * c.Lq * qtok;
-  // (rows past Lq: zeros everywhere, which add nothing)
+  // (rows past Lq: zeros everywhere, and never seen: a bias that grows with the
+  // distance would make weights of them that overflow)
   auto copies = [&](const Tile& t, uint16_t* qs, uint16_t* os, int buf) __attribute__((always_inline)) {
     const size_t hoff = qbase + (size_t)(hk * rep + head) * D;
     const size_t lbase = ((size_t)b * c.H + hk * rep + head) * c.Lq;
@@ -679,7 +680,7 @@ __device__ __forceinline__ void dkdv_body(const BwdArgs& a, const Part& part) {
     constexpr int P = decltype(par)::value;
     auto hidden = [&](f32x16& x) __attribute__((always_inline)) {
       each_hidden(rmin == INT32_MIN ? INT32_MIN : rmin - t.t * BN - 4 * hi - 32 * blk,
-                  docs && t.one() && kd != t.id ? INT32_MIN : INT32_MAX,
+                  docs && t.one() && kd != t.id ? INT32_MIN : c.Lq - t.t * BN - 4 * hi - 32 * blk,
                   docs && !t.one() ? &Qd[P][32 * blk + 4 * hi] : nullptr, kd,
                   [&](int i) __attribute__((always_inline)) { x[i] = -INFINITY; });
     };

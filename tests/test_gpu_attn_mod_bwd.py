@@ -18,6 +18,7 @@ import pytest
 import oracle
 import paper_2609_18077_amd as vx
 from tests.gpu_util import log
+from tests.test_gpu_attn_mod import check as fwd_check
 from tests.test_gpu_attn_mod import D, HALF, MASKS, PIECES, RMS, SCALE, deltas, dev_score, f64, make, masks, piece_score
 
 pytestmark = pytest.mark.gpu
@@ -188,6 +189,30 @@ def test_empty_calls():
         lse = torch.full((B, H, Lq), -float("inf"), device="cuda")
         for x in vx.attn_mod_bwd(q, k, k, q, q, lse, vx.Score(causal=True)):
             assert not x.any()
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_calls(seed):
+    """Seeded sizes, heads and modifiers of every kind together, lengths and positions past their ends among them."""
+    rng = np.random.default_rng(1000 + seed)
+    Hkv = int(rng.integers(1, 4))
+    B, H = int(rng.integers(1, 4)), Hkv * int(rng.integers(1, 4))
+    Lq, Lk = (int(np.exp(rng.uniform(0, 6.3))) for _ in range(2))
+    s = dict(causal=bool(rng.integers(2)), cap=float(rng.choice([0.0, 0.0, 3.0, 30.0, 200.0])))
+    if rng.integers(2):
+        s["slopes"] = list(rng.normal(0, 0.1, H))
+    if rng.integers(2):
+        s["q_doc"], s["k_doc"] = (np.sort(rng.integers(-1, 4, (B, L)), axis=1) if rng.integers(2) else rng.integers(-1, 3, (B, L))
+                                  for L in (Lq, Lk))
+    if rng.integers(2):
+        s["kv_valid_len"] = rng.integers(-3, Lk + 9, B)
+    if s["causal"] and rng.integers(2):
+        s["prefix_len"] = rng.integers(-3, Lk + 9, B)
+    if rng.integers(2):
+        s["q_start"] = rng.integers(-Lq, Lk + 50, B)
+    q, k, v = make(B, H, Hkv, Lq, Lk, seed)
+    check(q, k, v, what=f"random {seed}: {B}x{H}/{Hkv} {Lq}x{Lk} {sorted(s)}", **s)
+    fwd_check(q, k, v, what=f"random {seed}", **s)
 
 
 def test_differences():

@@ -1,9 +1,11 @@
 """Attention with score modifiers (vidax_attn_mod_fwd) against the float64
 reference.
 
-Tolerances, per element.  A weight p is rounded to bf16 once (off by at most
-2^-8 of itself) and rests on a score that is off by at most delta, so an output
-is off by at most (2^-8 + 2 delta) sum_j p_j |v_j| and its own rounding, 2^-8.
+Tolerances, per element.  A weight p is rounded to bf16 once, to p (1 + e) with
+|e| <= 2^-8, and the output is divided by the sum of the rounded weights: with
+sum_j p_j = 1 it is off by sum_j p_j e_j (v_j - o) / (1 + sum_j p_j e_j), at most
+2^-8 / (1 - 2^-8) (sum_j p_j |v_j| + |o|).  Its scores are off by at most delta,
+which adds 2 delta sum_j p_j |v_j|, and its own rounding 2^-8 of all that.
 delta: the fp32 dot product of 128 terms, 128 * 2^-24 of scale * sum |q k|, and
 eight roundings (2^-24 each, 2^-22 for the hardware exponential and reciprocal)
 of the magnitudes that y passes through: the cap, the bias, the reference.  The
@@ -101,7 +103,8 @@ def compare(o, lse, q, k, v, sc, spec, what):
     delta = deltas(qn, kn, sc, spec)
     got, gl = f64(o), f64(lse)
     assert np.isfinite(got).all(), what
-    tol = (HALF + 2 * delta[..., None]) * mag + HALF * (np.abs(ro) + (HALF + 2 * delta[..., None]) * mag)
+    off = HALF / (1 - HALF) * (mag + np.abs(ro)) + 2 * delta[..., None] * mag
+    tol = off + HALF * (np.abs(ro) + off)
     err = np.abs(got - ro)
     empty = np.isneginf(rl)
     assert np.array_equal(np.isneginf(gl), empty), what

@@ -8,7 +8,9 @@ rounds the result once.  With delta the error of a score (as for the forward),
 P is off by 2 delta of itself and ds by 4 delta of P (|dP| + |D|) and the fp32
 errors of dP and D, 130 * 2^-24 of their terms.  So, with A the same sums taken
 over absolute values, an element is off by at most (2^-8 + E) A and 2^-8 of
-itself, E = 4 delta + 300 * 2^-24.  Beside that the relative RMS error of a
+itself, E = 4 delta + 300 * 2^-24.  A weight below 2^-126 may count as zero, also
+in a product with bf16: 2^-126 of the other factors, at most |dP| + |D| <= 256
+max|dout| max|v| and |q| or |k| a row or key.  Beside that the relative RMS error of a
 tensor is held to 2^-7.5, two independent roundings.
 """
 
@@ -62,10 +64,12 @@ def compare(got, o, dout, q, k, v, sc, spec, what):
     ref = oracle.attn_mod_bwd_ref(*args, f64(dout), sc, spec, o_saved=f64(o))
     mags = _absolute(*args, f64(o), f64(dout), sc, spec)
     E = 4 * deltas(*args[:2], sc, spec).max(initial=0) + 300 * 2.0 ** -24
+    most = lambda *a: float(np.prod([np.abs(t).max(initial=0) + 1 for t in a]))
+    under = 2.0 ** -126 * 256 * (args[0].shape[1] * args[0].shape[2] + args[1].shape[1]) * most(f64(dout), *args)
     for n, x, r, m in zip(("dq", "dk", "dv"), got, ref, mags):
         x = f64(x)
         assert np.isfinite(x).all(), (what, n)
-        tol = (HALF + E) * m + HALF * (np.abs(r) + (HALF + E) * m)
+        tol = (HALF + E) * m + HALF * (np.abs(r) + (HALF + E) * m) + under
         err = np.abs(x - r)
         norm = np.sqrt((r ** 2).sum())
         rms = np.sqrt((err ** 2).sum()) / norm if norm else 0.0
@@ -191,13 +195,13 @@ def test_empty_calls():
             assert not x.any()
 
 
-@pytest.mark.parametrize("seed", range(12))
+@pytest.mark.parametrize("seed", range(18))
 def test_random_calls(seed):
     """Seeded sizes, heads and modifiers of every kind together, lengths and positions past their ends among them."""
     rng = np.random.default_rng(1000 + seed)
     Hkv = int(rng.integers(1, 4))
     B, H = int(rng.integers(1, 4)), Hkv * int(rng.integers(1, 4))
-    Lq, Lk = (int(np.exp(rng.uniform(0, 6.3))) for _ in range(2))
+    Lq, Lk = (int(np.exp(rng.uniform(*((0, 6.3) if seed < 12 else (4.5, 7.8))))) for _ in range(2))
     s = dict(causal=bool(rng.integers(2)), cap=float(rng.choice([0.0, 0.0, 3.0, 30.0, 200.0])))
     if rng.integers(2):
         s["slopes"] = list(rng.normal(0, 0.1, H))

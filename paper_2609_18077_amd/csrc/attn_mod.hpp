@@ -220,7 +220,7 @@ __device__ __forceinline__ void each_part(const ModCall& c, int pieces, int p, F
   const int lane = threadIdx.x & 63, len = Side::length(c), heads = Side::heads(c), nt = (int)mod_tiles(len);
   auto unit = [&](int t) { return key_weight(min(len - t * kModRows, kModRows)); };
   auto tile_weight = [&](const Batch& bt, int t) { return kTileStart + Side::visits(c, bt, t) * unit(t); };
-  const bool lens = c.s.kv_valid_len || c.s.q_start || c.s.prefix_len;
+  const bool lens = mod_own_lengths(c.s);  // (B <= kLaneBatches then: mod_pieces)
   auto wave_sum = [&](int x) {
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);

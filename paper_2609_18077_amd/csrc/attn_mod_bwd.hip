@@ -893,8 +893,7 @@ __global__ __launch_bounds__(256) void mod_reduce_kernel(BwdArgs a) {
 hipError_t launch_attn_mod_bwd(const ModBwd& f, hipStream_t stream) {
   const ModCall& c = f.c;
   const int cus = device_cu_count();
-  const ModBwdSplit s = mod_bwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr, c.s.causal != 0,
-                                      c.s.kv_valid_len || c.s.prefix_len || c.s.q_start, cus, f.ws_floats);
+  const ModBwdSplit s = mod_bwd_split(c, cus, f.ws_floats);
   BwdArgs a;
   a.c = c;
   a.sc = make_scores(c);

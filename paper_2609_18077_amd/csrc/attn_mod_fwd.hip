@@ -759,8 +759,7 @@ hipError_t launch_attn_mod_fwd(const ModFwd& f, hipStream_t stream) {
   (cap ? (bias ? LAUNCH_LSE(kernel, grid, true, true) : LAUNCH_LSE(kernel, grid, true, false))    \
        : (bias ? LAUNCH_LSE(kernel, grid, false, true) : LAUNCH_LSE(kernel, grid, false, false)))
   const ModCall& c = f.c;
-  const ModSplit s = mod_fwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr, c.s.causal != 0,
-                                   c.s.kv_valid_len || c.s.q_start, device_cu_count(), f.ws_floats);
+  const ModSplit s = mod_fwd_split(c, device_cu_count(), f.ws_floats);
   FwdArgs a;
   a.c = c;
   a.sc = make_scores(c);

@@ -27,6 +27,10 @@ struct ModCall {
   ModScore s;
 };
 
+// Whether the batches may visit tiles of their own: valid lengths, positions or prefixes.
+// (One answer for the launch rules and the device's walk over the pieces.)
+__host__ __device__ inline bool mod_own_lengths(const ModScore& s) { return s.kv_valid_len || s.q_start || s.prefix_len; }
+
 struct ModFwd {
   ModCall c;
   const uint16_t *q, *k, *v;
@@ -63,6 +67,7 @@ inline size_t mod_doc_floats(int B, int Lq, int Lk, bool docs) {
 constexpr int kModKeys = 64;
 constexpr int kFewRows = 32;
 constexpr int kMostRuns = 16;
+inline bool mod_few(int H, int Hkv, int Lq) { return Hkv > 0 && (int64_t)(H / Hkv) * Lq <= kFewRows; }
 
 // Or all key tiles of all query tiles are cut into `pieces` of equal weight
 // (attn_mod.hpp): tiles of unequal work, or not a whole number of rounds of them.
@@ -73,6 +78,8 @@ __host__ __device__ inline int key_weight(int rows) { return rows > 128 ? 4 : 3;
 constexpr int kLeastPiece = 16;
 // Tiles of a head up to which a lane adds up those of a batch with lengths of its own.
 constexpr int kLaneTiles = 16;
+// Batches with lengths of their own in pieces: a lane each.
+constexpr int kLaneBatches = 64;
 
 struct ModPieces {
   int n;          // 0: a workgroup takes a tile (or one of its runs)
@@ -109,7 +116,7 @@ inline ModPieces mod_pieces(int B, int heads, int own, int other, int64_t most_v
                             int row, double tile_us) {
   ModPieces p{0, 0, 0, 0, 0.0};
   const int64_t nt = (int64_t)mod_tiles(own), wgs = nt * B * heads;
-  if (lengths ? B > 64 || (nt > kLaneTiles && (nt + 63) / 64 * B > 16) : nt > 4096) return p;
+  if (lengths ? B > kLaneBatches || (nt > kLaneTiles && (nt + 63) / 64 * B > 16) : nt > 4096) return p;
   if ((__int128)nt * B * (kTileStart + 4 * most_visits) > INT32_MAX) return p;  // (32-bit sums)
   int64_t weight = 0;  // of a head
   for (int64_t t = 0; t < nt; ++t)
@@ -143,7 +150,7 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
   r.pieces.n = 0;
   r.floats = mod_doc_floats(B, Lq, Lk, docs);
   r.part = (r.floats + 63) / 64 * 64;
-  r.few = Hkv > 0 && (int64_t)(H / Hkv) * Lq <= kFewRows;
+  r.few = mod_few(H, Hkv, Lq);
   const int64_t rows = (int64_t)B * H * Lq;
   if (rows == 0 || Lk == 0) return r;
   if (r.few) {
@@ -204,6 +211,13 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
     r.floats = p.floats;
   }
   return r;
+}
+
+// For a call.  (Few rows: a prefix alone leaves every batch the same keys, those up to
+// its last query.)
+inline ModSplit mod_fwd_split(const ModCall& c, int cus, size_t max_floats) {
+  const bool own = mod_few(c.H, c.Hkv, c.Lq) ? c.s.kv_valid_len || c.s.q_start : mod_own_lengths(c.s);
+  return mod_fwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr, c.s.causal != 0, own, cus, max_floats);
 }
 
 // ---- backward ----
@@ -322,6 +336,10 @@ inline ModBwdSplit mod_bwd_split(int B, int H, int Hkv, int Lq, int Lk, bool doc
     if (p.floats > r.floats) r.floats = p.floats;
   }
   return r;
+}
+
+inline ModBwdSplit mod_bwd_split(const ModCall& c, int cus, size_t max_floats) {
+  return mod_bwd_split(c.B, c.H, c.Hkv, c.Lq, c.Lk, c.s.k_doc != nullptr, c.s.causal != 0, mod_own_lengths(c.s), cus, max_floats);
 }
 
 __attribute__((weak)) hipError_t launch_attn_mod_fwd(const ModFwd& a, hipStream_t stream);

@@ -344,7 +344,9 @@ typedef struct vidax_score_desc {
  * rounded to bf16 before the product with v.  Requires d == 128; device pointers
  * 16-byte aligned; outputs and workspace must not overlap each other or an
  * input.  One batch of q, Lq * H * d * 2 bytes, and 64 tokens of k must stay
- * below 2 GiB - 4 KiB (VIDAX_ERR_UNSUPPORTED beyond).  scale finite.
+ * below 2 GiB - 4 KiB, B H Lq below 2^31, B H (ceil(Lq / 128) + ceil(Lk / 128)) below
+ * 2^25 and, with more than 32 rows a K/V head (H / Hkv * Lq), B H ceil(Lq / 256) below
+ * 2^23 (VIDAX_ERR_UNSUPPORTED beyond).  scale finite.
  */
 vidax_status vidax_attn_mod_fwd(const void* q, const void* k, const void* v, void* o, float* lse, int32_t B, int32_t H,
                                 int32_t Hkv, int32_t Lq, int32_t Lk, int32_t d, float scale,
@@ -378,7 +380,8 @@ size_t vidax_attn_mod_fwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, in
  *              documents, those of the forward more.
  * Same call, same bits: no atomics.  Products on bf16 inputs (P and ds rounded to
  * bf16) with fp32 accumulation.  Pointers, sizes and overlap as for the forward
- * (lse 4-byte aligned).
+ * (lse 4-byte aligned; B H ceil(Lq / 256) and B Hkv ceil(Lk / 256) below 2^23 for any
+ * number of rows).
  */
 vidax_status vidax_attn_mod_bwd(const void* q, const void* k, const void* v, const void* o, const void* dout,
                                 const float* lse, void* dq, void* dk, void* dv, int32_t B, int32_t H, int32_t Hkv,

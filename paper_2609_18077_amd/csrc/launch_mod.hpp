@@ -81,6 +81,19 @@ constexpr int kLaneTiles = 16;
 // Batches with lengths of their own in pieces: a lane each.
 constexpr int kLaneBatches = 64;
 
+// A launch takes fewer than 2^32 threads: workgroups of 512 for the tiles (and for each
+// of the runs of their keys), of 256 for few rows, ranges and joins.  What a call cannot
+// do without has to fit (the calls beyond are refused), runs and pieces are not taken
+// where they or their joins would not.
+constexpr int64_t kMostTiles = ((int64_t)1 << 23) - 1;
+constexpr int64_t kMostSmall = ((int64_t)1 << 24) - 1;
+inline bool mod_launches_fit(int B, int H, int Hkv, int Lq, int Lk, bool docs, bool backward) {
+  const __int128 q = (__int128)mod_tiles(Lq) * B * H, k = (__int128)mod_tiles(Lk) * B * Hkv;
+  if (docs && (__int128)B * (mod_ranges(Lq) + mod_ranges(Lk)) / 8 >= kMostSmall) return false;
+  if (backward) return q <= kMostTiles && k <= kMostTiles;
+  return mod_few(H, Hkv, Lq) ? (__int128)B * Hkv <= kMostSmall : q <= kMostTiles;
+}
+
 struct ModPieces {
   int n;          // 0: a workgroup takes a tile (or one of its runs)
   int slot_rows;  // rows of a partial result
@@ -118,6 +131,7 @@ inline ModPieces mod_pieces(int B, int heads, int own, int other, int64_t most_v
   const int64_t nt = (int64_t)mod_tiles(own), wgs = nt * B * heads;
   if (lengths ? B > kLaneBatches || (nt > kLaneTiles && (nt + 63) / 64 * B > 16) : nt > 4096) return p;
   if ((__int128)nt * B * (kTileStart + 4 * most_visits) > INT32_MAX) return p;  // (32-bit sums)
+  if (wgs * 32 > kMostSmall) return p;                                          // (the joins: up to 32 workgroups a tile)
   int64_t weight = 0;  // of a head
   for (int64_t t = 0; t < nt; ++t)
     weight += kTileStart + visits(t) * key_weight((int)(own - t * kModRows < kModRows ? own - t * kModRows : kModRows));
@@ -168,7 +182,7 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
       return rounds * (3.0 + (per + 3) / 4 * step);
     };
     const size_t need = r.part + (size_t)(u + B) * H * Lq * 129;
-    if (u > 0 && need <= max_floats && us(u * Hkv, (B * tiles * (lengths && B > 1 ? 2 : 3) / 3 + u - 1) / u) + 5.0 < us(wgs, tiles)) {
+    if (u > 0 && need <= max_floats && rows / 4 < kMostSmall && us(u * Hkv, (B * tiles * (lengths && B > 1 ? 2 : 3) / 3 + u - 1) / u) + 5.0 < us(wgs, tiles)) {
       r.units = (int)u;
       r.floats = need;
     }
@@ -195,7 +209,7 @@ inline ModSplit mod_fwd_split(int B, int H, int Hkv, int Lq, int Lk, bool docs, 
   // one.
   for (int s = 2; s <= kMostRuns && s <= tiles && (!docs || wgs * s <= cus); ++s) {
     const size_t need = r.part + (size_t)s * rows * 129;  // a run's rows: 128 outputs and a log-sum-exp each
-    if (need > max_floats) break;
+    if (need > max_floats || wgs * s > kMostTiles || rows / 16 >= kMostSmall) break;
     if (direct(s) < best) {
       best = direct(s);
       r.runs = s;

@@ -226,7 +226,7 @@ bool any_overlap(const Buf (&outs)[NO], const Buf (&ins)[NI], int io_out = -1, i
 // The checks that attention with score modifiers shares between forward and
 // backward; bufs: the descriptor's arrays.
 vidax_status mod_common(int32_t B, int32_t H, int32_t Hkv, int32_t Lq, int32_t Lk, int32_t d, float scale,
-                        const vidax_score_desc* s, vidax::ModCall* c, Buf (&bufs)[6]) {
+                        const vidax_score_desc* s, bool backward, vidax::ModCall* c, Buf (&bufs)[6]) {
   if (B < 0 || H < 0 || Hkv < 0 || Lq < 0 || Lk < 0 || d < 0) return VIDAX_ERR_INVALID_ARG;
   if ((Hkv == 0) != (H == 0) || (Hkv > 0 && H % Hkv != 0)) return VIDAX_ERR_INVALID_ARG;
   if (numel4(B, Lq, H, d) < 0 || numel4(B, Lk, Hkv, d) < 0) return VIDAX_ERR_INVALID_ARG;
@@ -250,10 +250,12 @@ vidax_status mod_common(int32_t B, int32_t H, int32_t Hkv, int32_t Lq, int32_t L
   if ((int64_t)Lq * H * d * 2 > INT32_MAX - 4096 || (int64_t)64 * Hkv * d * 2 > INT32_MAX - 4096 ||
       (int64_t)64 * H * d * 2 > INT32_MAX - 4096 || Lk > (1 << 28) || Lq > (1 << 28))
     return VIDAX_ERR_UNSUPPORTED;
-  // launch sizes: the forward's tiles in up to 64 runs, the joining launch, the ranges
-  const int64_t tiles = ((int64_t)Lq + 127) / 128 + ((int64_t)Lk + 127) / 128;
-  if ((__int128)tiles * B * H * 64 > INT32_MAX || (__int128)B * H * Lq > INT32_MAX) return VIDAX_ERR_UNSUPPORTED;
+  // launch sizes, and 32-bit numbers of tiles and rows
   const bool docs = s->q_doc && s->k_doc;
+  const int64_t tiles = ((int64_t)Lq + 127) / 128 + ((int64_t)Lk + 127) / 128;
+  if ((__int128)tiles * B * H * 64 > INT32_MAX || (__int128)B * H * Lq > INT32_MAX ||
+      !vidax::mod_launches_fit(B, H, Hkv, Lq, Lk, docs, backward))
+    return VIDAX_ERR_UNSUPPORTED;
   *c = vidax::ModCall{B, H, Hkv, Lq, Lk, scale,
                       vidax::ModScore{s->causal, s->cap > 1e30f ? 0.0f : s->cap,  // (tanh is then the identity in fp32)
                                       s->slopes, docs ? s->q_doc : nullptr, docs ? s->k_doc : nullptr, s->kv_valid_len,
@@ -453,7 +455,7 @@ vidax_status vidax_attn_mod_fwd(const void* q, const void* k, const void* v, voi
                                 hipStream_t stream) {
   vidax::ModFwd a;
   Buf s[6];
-  const vidax_status st = mod_common(B, H, Hkv, Lq, Lk, d, scale, score, &a.c, s);
+  const vidax_status st = mod_common(B, H, Hkv, Lq, Lk, d, scale, score, false, &a.c, s);
   if (st == VIDAX_ERR_INVALID_ARG) return st;
   const uint64_t nq = (uint64_t)B * Lq * H * d, nk = (uint64_t)B * Lk * Hkv * d;
   if ((nq > 0 && (!q || !o)) || (nq > 0 && nk > 0 && (!k || !v))) return VIDAX_ERR_INVALID_ARG;
@@ -483,7 +485,7 @@ vidax_status vidax_attn_mod_bwd(const void* q, const void* k, const void* v, con
                                 float* workspace, size_t workspace_floats, hipStream_t stream) {
   vidax::ModBwd a;
   Buf s[6];
-  const vidax_status st = mod_common(B, H, Hkv, Lq, Lk, d, scale, score, &a.c, s);
+  const vidax_status st = mod_common(B, H, Hkv, Lq, Lk, d, scale, score, true, &a.c, s);
   if (st == VIDAX_ERR_INVALID_ARG) return st;
   const uint64_t nq = (uint64_t)B * Lq * H * d, nk = (uint64_t)B * Lk * Hkv * d, nr = (uint64_t)B * H * Lq;
   if ((nq > 0 && (!q || !o || !dout || !dq || !lse)) || (nk > 0 && (!dk || !dv)) || (nq > 0 && nk > 0 && (!k || !v)))
@@ -518,7 +520,7 @@ size_t vidax_attn_mod_bwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, in
                                            int32_t docs) {
   vidax::ModCall c;
   Buf s[6];
-  if (mod_common(B, H, Hkv, Lq, Lk, d, 1.0f, nullptr, &c, s) != VIDAX_OK) return 0;
+  if (mod_common(B, H, Hkv, Lq, Lk, d, 1.0f, nullptr, true, &c, s) != VIDAX_OK) return 0;
   const int cus = vidax::device_cu_count();
   size_t most = 0;
   for (int i = 0; i < 4; ++i) {
@@ -532,7 +534,7 @@ size_t vidax_attn_mod_fwd_workspace_floats(int32_t B, int32_t H, int32_t Hkv, in
                                            int32_t docs) {
   vidax::ModCall c;
   Buf s[6];
-  if (mod_common(B, H, Hkv, Lq, Lk, d, 1.0f, nullptr, &c, s) != VIDAX_OK || B == 0 || H == 0 || Lq == 0) return 0;
+  if (mod_common(B, H, Hkv, Lq, Lk, d, 1.0f, nullptr, false, &c, s) != VIDAX_OK || B == 0 || H == 0 || Lq == 0) return 0;
   const int cus = vidax::device_cu_count();
   size_t most = 0;
   for (int i = 0; i < 4; ++i) {  // (causal or not, lengths or not)

@@ -11,6 +11,8 @@ import subprocess
 import numpy as np
 import pytest
 
+import paper_2609_18077_amd as vx
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
 CUS, ALL = 256, 1 << 62
@@ -35,6 +37,8 @@ extern "C" void cut(int B, int H, int Hkv, int Lq, int Lk, int causal, int valid
   o[0] = mod_own_lengths(c.s);
   o[1] = f.few; o[2] = f.units; o[3] = f.pieces.n; o[4] = f.floats;
   o[5] = b.dq.n; o[6] = b.dkdv.n; o[7] = b.floats;
+  o[8] = f.runs; o[9] = b.runs;
+  o[10] = mod_launches_fit(B, H, Hkv, Lq, Lk, false, false); o[11] = mod_launches_fit(B, H, Hkv, Lq, Lk, true, true);
 }
 """
 
@@ -55,9 +59,10 @@ def cut(tmp_path_factory):
     f.restype = None
 
     def call(B, H, Hkv, Lq, Lk, causal, valid, prefix, start, most=ALL):
-        out = (ctypes.c_int64 * 8)()
+        out = (ctypes.c_int64 * 12)()
         f(B, H, Hkv, Lq, Lk, causal, valid, prefix, start, CUS, most, out)
-        return dict(zip(("own", "few", "units", "fwd", "fwd_floats", "dq", "dkdv", "bwd_floats"), out))
+        return dict(zip(("own", "few", "units", "fwd", "fwd_floats", "dq", "dkdv", "bwd_floats", "runs", "bwd_runs",
+                         "fwd_fits", "bwd_fits"), out))
 
     return call
 
@@ -112,3 +117,51 @@ def test_few_rows_take_a_prefix_for_no_length_of_a_cache(cut):
     for B, H, Hkv, Lq, Lk in ((16, 32, 8, 1, 16384), (130, 8, 2, 4, 700), (3, 4, 2, 3, 2100)):
         with_prefix, without = cut(B, H, Hkv, Lq, Lk, 1, 0, 1, 0), cut(B, H, Hkv, Lq, Lk, 1, 0, 0, 0)
         assert without["few"] and all(with_prefix[n] == without[n] for n in ("few", "units", "fwd_floats"))
+
+
+def test_launches_stay_below_two_to_the_32_threads(cut):
+    """Whatever is not refused: tiles in workgroups of 512, few rows, joins and ranges in workgroups of 256."""
+    rng = np.random.default_rng(75)
+    shapes = [(32000, 33, 1, 1, 20), (131072, 8, 8, 40, 40), (40000, 16, 16, 2, 2), (260000, 33, 1, 1, 1)]
+    for _ in range(3000):
+        Hkv = int(rng.integers(1, 40))
+        shapes.append((int(np.exp(rng.uniform(5, 16.6))), Hkv * int(rng.integers(1, 40)), Hkv, int(np.exp(rng.uniform(0, 6.5))),
+                       int(np.exp(rng.uniform(0, 6.5)))))
+    small = 2 ** 24 - 1  # workgroups of 256
+    fit = refused = 0
+    for B, H, Hkv, Lq, Lk in shapes:
+        tiles = -(-Lq // 128) - (-Lk // 128)
+        if tiles * B * H * 64 >= 2 ** 31 or B * H * Lq >= 2 ** 31:
+            continue
+        qt, kt = -(-Lq // 256) * B * H, -(-Lk // 256) * B * Hkv
+        for s in ((0, 0, 0, 0), (1, 0, 0, 0), (1, 1, 0, 1)):
+            got = cut(B, H, Hkv, Lq, Lk, *s)
+            what = (B, H, Hkv, Lq, Lk, s, got)
+            fit += got["fwd_fits"]
+            refused += not got["bwd_fits"]
+            if got["fwd_fits"]:
+                if got["few"]:
+                    assert B * Hkv <= small and (not got["units"] or -(-B * H * Lq // 4) <= small), what
+                elif got["fwd"]:
+                    assert qt * 16 <= small, what
+                else:
+                    assert qt * got["runs"] * 512 < 2 ** 32 and (got["runs"] == 1 or -(-B * H * Lq // 16) <= small), what
+            else:
+                assert qt * 512 >= 2 ** 32, what
+            if got["bwd_fits"]:
+                assert qt * 16 <= small if got["dq"] else qt * 512 < 2 ** 32, what
+                assert kt * 32 <= small if got["dkdv"] else kt * got["bwd_runs"] * 512 < 2 ** 32, what
+                assert B * (-(-Lq // 64) - (-Lk // 64)) <= 4 * small, what
+    assert fit > 1000 and refused > 10
+
+
+def test_calls_of_too_many_tiles_are_refused():
+    P, UNS = 1 << 40, 2
+    p = [ctypes.c_void_p(i * P) for i in range(1, 11)]
+    for n in ((260000, 33, 1, 1, 1), (1 << 23, 1, 1, 33, 1)):
+        assert vx.lib().vidax_attn_mod_fwd(*p[:4], None, *n, 128, 0.1, None, None, 0, None) == UNS
+    for n in ((260000, 33, 1, 1, 1), (1 << 23, 1, 1, 1, 1), (1 << 22, 2, 2, 1, 33)):
+        assert vx.lib().vidax_attn_mod_bwd(*p[:9], *n, 128, 0.1, None, p[9], 1 << 40, None) == UNS
+        assert vx.lib().vidax_attn_mod_bwd_workspace_floats(*n, 128, 0) == 0
+    # single tokens of as many requests: a workgroup a K/V head
+    assert vx.lib().vidax_attn_mod_fwd_workspace_floats(1 << 22, 2, 2, 1, 33, 128, 1) > 0

@@ -50,3 +50,22 @@ def test_batches_with_lengths_of_their_own(B, H, Hkv, Lq, Lk, what):
         compare_grads([grads[0][bs, :, hs], grads[1][bs, :, ks], grads[2][bs, :, ks]], o[bs, :, hs], dout[bs, :, hs], *args)
     for t in (o, *grads):
         assert torch.isfinite(t).all()
+
+
+@pytest.mark.parametrize("B,H,Hkv,Lq,Lk", [(32000, 33, 1, 1, 20), (40000, 16, 16, 2, 2), (20000, 33, 1, 1, 33)])
+def test_a_million_tiles(B, H, Hkv, Lq, Lk):
+    """Short sequences by the thousand: more tiles than a launch that joins pieces of them could hold."""
+    import torch
+
+    q, k, v = make(B, H, Hkv, Lq, Lk, 53)
+    dout = make(B, H, Hkv, Lq, 1, 54)[0]
+    score = vx.Score(causal=True)
+    o, lse = vx.attn_mod_fwd(q, k, v, score, return_lse=True)
+    grads = vx.attn_mod_bwd(q, k, v, o, dout, lse, score)
+    for b in (0, B // 2, B - 2):
+        bs = slice(b, b + 2)
+        args = q[bs], k[bs], v[bs], SCALE, oracle.ScoreSpec(causal=True), f"batch {b} of {B}"
+        compare(o[bs], lse[bs], *args)
+        compare_grads([t[bs] for t in grads], o[bs], dout[bs], *args)
+    for t in (o, *grads):
+        assert torch.isfinite(t).all()

@@ -432,8 +432,9 @@ typedef struct vidax_block_norm_desc {
  * and post_gain must then be absent); xo (x'): as x, may be x itself (in place),
  * NULL allowed without a branch where alpha is 1 (x' is x); h: bf16 [B, L, C].
  * All device pointers 16-byte aligned; outputs must not overlap each other or
- * an input (x itself apart).  Requires C a multiple of 8 and C <= 16384
- * (VIDAX_ERR_UNSUPPORTED otherwise); zero-sized calls are no-ops.  `desc` is a
+ * an input (x itself apart).  Requires C a multiple of 8 and C <= 16384, and no more
+ * tokens than one launch takes (2^22 in any shape, more of few channels or long
+ * sequences; VIDAX_ERR_UNSUPPORTED otherwise); zero-sized calls are no-ops.  `desc` is a
  * host pointer.  HBM-bound: x and y are read once, x' and h written once.
  */
 vidax_status vidax_block_norm_fwd(const void* x, const void* y, void* xo, void* h, int32_t B, int32_t L, int32_t C,

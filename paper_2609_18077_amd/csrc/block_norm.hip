@@ -25,7 +25,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // Waves of a workgroup: 8, so that a lane may hold 256 registers; 10 where it
 // needs few (168 then): a row of 5120 channels with one chunk a lane.
 constexpr int kMaxWaves = 10;
-constexpr int kWaves = 8;
+constexpr int kWaves = kBlockWaves;
 
 // Eight values of the stream (bf16: 16 bytes, fp32: 32) as they lie in memory.
 template <bool F32>
@@ -593,22 +593,6 @@ hipError_t launch(void (*kernel)(A), unsigned grid, unsigned block, hipStream_t 
   return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(grid), dim3(block), args, 0, stream);
 }
 
-// Waves a row and chunks a lane: the fewest idle lanes, then the fewest waves.
-void fwd_row(int C, int& chunks, int& waves) {
-  const int n = C / 8;
-  int best = 1 << 30;
-  for (int nc = 4; nc >= 1; --nc) {
-    const int w = (n + 64 * nc - 1) / (64 * nc);
-    if (w > kWaves || (nc == 4 && n <= 64 * 3 * kWaves)) continue;
-    const int idle = w * 64 * nc - n;
-    if (idle < best) {
-      best = idle;
-      chunks = nc;
-      waves = w;
-    }
-  }
-}
-
 template <bool F32, bool TOKEN>
 hipError_t launch_fwd(int nc, unsigned grid, unsigned block, hipStream_t stream, const FwdArgs& f) {
   switch (nc) {
@@ -634,18 +618,12 @@ hipError_t launch_block_norm_fwd(const BlockNormFwd& a, hipStream_t stream) {
   const BlockNorm& n = a.n;
   FwdArgs f;
   f.a = a;
-  int nc = 1;
-  fwd_row(n.C, nc, f.s.waves);
-  f.s.groups = f.s.waves >= 4 ? 1 : 4 / f.s.waves;
-  // runs of rows: about 16 waves a compute unit, 8 rows a group at most
-  int64_t per = (int64_t)n.B * n.L / (256 * 16 / f.s.waves);
-  per = per < 1 ? 1 : per > 8 ? 8 : per;
-  f.s.rows = (int)(per * f.s.groups);
-  f.s.runs = (int)(((int64_t)n.L + f.s.rows - 1) / f.s.rows);
-  const unsigned grid = (unsigned)(f.s.runs * n.B), block = 64u * f.s.waves * f.s.groups;
+  const BlockShape s = block_fwd_shape(n.B, n.L, n.C);
+  f.s = Shape{s.waves, s.groups, s.rows, s.runs};
+  const unsigned grid = (unsigned)s.runs * (unsigned)n.B, block = 64u * s.waves * s.groups;
   const bool token = (n.gate.p && n.gate.token) || (n.scale.p && n.scale.token) || (n.shift.p && n.shift.token);
-  if (n.fp32) return token ? launch_fwd<true, true>(nc, grid, block, stream, f) : launch_fwd<true, false>(nc, grid, block, stream, f);
-  return token ? launch_fwd<false, true>(nc, grid, block, stream, f) : launch_fwd<false, false>(nc, grid, block, stream, f);
+  if (n.fp32) return token ? launch_fwd<true, true>(s.chunks, grid, block, stream, f) : launch_fwd<true, false>(s.chunks, grid, block, stream, f);
+  return token ? launch_fwd<false, true>(s.chunks, grid, block, stream, f) : launch_fwd<false, false>(s.chunks, grid, block, stream, f);
 }
 
 hipError_t launch_block_norm_bwd(const BlockNormBwd& a, hipStream_t stream) {
@@ -655,7 +633,7 @@ hipError_t launch_block_norm_bwd(const BlockNormBwd& a, hipStream_t stream) {
   f.s = Shape{s.waves, s.groups, s.rows, s.runs};
   const bool sums = (!a.per_token && (a.dshift || a.dscale || a.dgate)) || a.dgain || a.dpost_gain;
   if (!sums) f.a.ws = nullptr;
-  const unsigned grid = (unsigned)(s.runs * a.n.B), block = 64u * s.waves * s.groups;
+  const unsigned grid = (unsigned)s.runs * (unsigned)a.n.B, block = 64u * s.waves * s.groups;
   hipError_t e = hipSuccess;
   if (grid == 0) f.s.runs = 0;  // no tokens: the sums alone, all zero
   else e =

@@ -47,6 +47,40 @@ struct BlockNormBwd {
   float* ws;      // column sums of every run of rows
 };
 
+struct BlockShape {
+  int chunks, waves, groups, rows, runs;
+};
+// A launch takes fewer than 2^32 threads.
+inline bool block_launch_fits(const BlockShape& s, int B) {
+  return (__int128)s.runs * B * 64 * s.waves * s.groups < ((int64_t)1 << 32);
+}
+
+// Shape of the forward: as below.  Waves a row and chunks a lane: the fewest idle
+// lanes, then the fewest waves; runs of rows: about 16 waves a compute unit, 8 rows a
+// group at most.
+constexpr int kBlockWaves = 8;  // of a workgroup
+inline BlockShape block_fwd_shape(int B, int L, int C) {
+  BlockShape s{1, 1, 1, 1, 0};
+  const int n = C / 8;
+  int best = 1 << 30;
+  for (int nc = 4; nc >= 1; --nc) {
+    const int w = (n + 64 * nc - 1) / (64 * nc);
+    if (w > kBlockWaves || (nc == 4 && n <= 64 * 3 * kBlockWaves)) continue;
+    const int idle = w * 64 * nc - n;
+    if (idle < best) {
+      best = idle;
+      s.chunks = nc;
+      s.waves = w;
+    }
+  }
+  s.groups = s.waves >= 4 ? 1 : 4 / s.waves;
+  int64_t per = (int64_t)B * L / (256 * 16 / s.waves);
+  per = per < 1 ? 1 : per > 8 ? 8 : per;
+  s.rows = (int)(per * s.groups);
+  s.runs = (int)(((int64_t)L + s.rows - 1) / s.rows);
+  return s;
+}
+
 // Shape of the backward: workgroups of `groups` groups of `waves` waves, a row
 // each at a time; a workgroup takes `rows` consecutive rows of a batch (a run),
 // `runs` of them a batch.
@@ -58,9 +92,6 @@ struct BlockNormBwd {
 // once by the reduction, 12 bytes a channel each way (512 runs against 65536
 // rows: 1.6 % of the bytes); at least 4 rows a group, so that the loads of one
 // row pass under the arithmetic of the one before.
-struct BlockShape {
-  int chunks, waves, groups, rows, runs;
-};
 inline BlockShape block_bwd_shape(int B, int L, int C) {
   BlockShape s;
   const int n = C / 8;

@@ -295,7 +295,7 @@ vidax_status block_norm_common(int32_t B, int32_t L, int32_t C, const vidax_bloc
   mods[3] = Buf{d->gain, (uint64_t)C * 4};
   mods[4] = Buf{d->post_gain, (uint64_t)C * 4};
   if (C % 8 != 0 || C > vidax::kBlockMaxC) return VIDAX_ERR_UNSUPPORTED;
-  if ((int64_t)B * L > INT32_MAX) return VIDAX_ERR_UNSUPPORTED;  // workgroups
+  if ((int64_t)B * L > INT32_MAX) return VIDAX_ERR_UNSUPPORTED;  // rows
   auto mod = [](const vidax_block_mod& x) { return vidax::BlockMod{x.p, x.batch_stride, x.token_stride}; };
   *n = vidax::BlockNorm{B, L, C, d->stream_fp32, d->norm, d->post, d->eps, d->alpha, d->gain, d->post_gain,
                         mod(d->gate), mod(d->scale), mod(d->shift)};
@@ -558,6 +558,7 @@ vidax_status vidax_block_norm_fwd(const void* x, const void* y, void* xo, void* 
   const Buf ins[7] = {{x, sb}, {y, n * 2}, mods[0], mods[1], mods[2], mods[3], mods[4]};
   if (any_overlap(outs, ins, 0, 0)) return VIDAX_ERR_INVALID_ARG;
   if (st != VIDAX_OK || n == 0) return st;
+  if (!vidax::block_launch_fits(vidax::block_fwd_shape(B, L, C), B)) return VIDAX_ERR_UNSUPPORTED;
   if (!vidax::launch_block_norm_fwd) return VIDAX_ERR_LAUNCH;
   a.x = x;
   a.y = (const uint16_t*)y;
@@ -568,7 +569,8 @@ vidax_status vidax_block_norm_fwd(const void* x, const void* y, void* xo, void* 
 
 size_t vidax_block_norm_bwd_workspace_floats(int32_t B, int32_t L, int32_t C) {
   if (B < 0 || L < 0 || C < 0 || C % 8 != 0 || C > vidax::kBlockMaxC || (int64_t)B * L > INT32_MAX) return 0;
-  return B && L && C ? vidax::block_bwd_floats(B, L, C) : 0;
+  if (B == 0 || L == 0 || C == 0 || !vidax::block_launch_fits(vidax::block_bwd_shape(B, L, C), B)) return 0;
+  return vidax::block_bwd_floats(B, L, C);
 }
 
 vidax_status vidax_block_norm_bwd(const void* dh, const void* dxo, const void* xo, const void* y, void* dx, void* dy,
@@ -602,6 +604,7 @@ vidax_status vidax_block_norm_bwd(const void* dh, const void* dxo, const void* x
   const Buf ins[8] = {{dxo, sb}, {dh, n * 2}, {xo, sb}, {y, n * 2}, mods[0], mods[1], mods[3], mods[4]};
   if (any_overlap(outs, ins, 0, 0)) return VIDAX_ERR_INVALID_ARG;
   if (st != VIDAX_OK) return st;
+  if (n > 0 && !vidax::block_launch_fits(vidax::block_bwd_shape(B, L, C), B)) return VIDAX_ERR_UNSUPPORTED;
   if (n > 0 && sums && (!workspace || workspace_floats < vidax::block_bwd_floats(B, L, C))) return VIDAX_ERR_INVALID_ARG;
   if (C == 0 || (n == 0 && !sums)) return VIDAX_OK;  // (without tokens the sums are zero)
   if (!vidax::launch_block_norm_bwd) return VIDAX_ERR_LAUNCH;

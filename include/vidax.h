@@ -334,14 +334,19 @@ typedef struct vidax_score_desc {
  *          values (VIDAX_ERR_INVALID_ARG below); otherwise NULL is allowed.  With at least
  *          vidax_attn_mod_fwd_workspace_floats(...) values, calls of few or uneven
  *          query tiles cut their keys into parts that work side by side, and join
- *          them in a further launch; with fewer they take the parts that fit.  The
- *          result differs by fp32 rounding only.
- * What lies in k and v where no query of the call can see it (past
- * kv_valid_len, behind the last query's position, at keys of negative documents)
- * never reaches an output, whatever it holds; k and v of the other keys must be
- * finite, also for queries that do not see them.
- * Products on bf16 inputs with fp32 accumulation, softmax in fp32, the weights
- * rounded to bf16 before the product with v.  Requires d == 128; device pointers
+ *          them in a further launch; with fewer they take the parts that fit.
+ * What lies in k and v at keys past kv_valid_len, behind every position and prefix
+ * of the batch's queries (causal) or of negative documents never reaches an output,
+ * whatever it holds.  k and v of all other keys must be finite, also for queries that
+ * do not see them and in documents that no query is of.
+ * Products on bf16 inputs with fp32 accumulation, softmax in fp32.  The weights are
+ * rounded to bf16 before the product with v: o is within 2^-8 / (1 - 2^-8) (sum_j p_j
+ * |v_j| + |o|), fp32 rounding and its own rounding to bf16 of the exact value.  Which way
+ * a weight is rounded, and whether o is divided by the sum of the weights or of their
+ * roundings, depends on how the keys are cut and on whether lse is wanted: outputs with
+ * another workspace, or with and without lse, differ within that bound; the same call
+ * gives the same bits.  With a cap, what else a tile holds may choose between two forms
+ * of the tanh that differ by fp32 rounding.  Requires d == 128; device pointers
  * 16-byte aligned; outputs and workspace must not overlap each other or an
  * input.  One batch of q, Lq * H * d * 2 bytes, and 64 tokens of k must stay
  * below 2 GiB - 4 KiB, B H Lq below 2^31, B H (ceil(Lq / 128) + ceil(Lk / 128)) below

@@ -96,7 +96,9 @@ class Score:
     |position - j| is subtracted; q_doc, k_doc: int32 [B, Lq] and [B, Lk], only
     keys of the query's own document are seen (a negative id belongs to none);
     kv_valid_len, prefix_len: int32 [B]; q_start: int32 [B], the position of
-    query 0 (default: Lk - Lq).  All tensors are device tensors."""
+    query 0 (default: Lk - Lq).  All tensors are device tensors.  Keys that hold
+    anything but numbers have to lie past kv_valid_len, behind all positions and
+    prefixes of a causal call, or in negative documents."""
 
     causal: bool = False
     cap: float = 0.0

@@ -7,7 +7,7 @@
 // of LDS: two buffers of K and two of V, filled by direct copies of whole rows;
 // no barrier until the waves' outputs are joined at the end.  Two tiles a wave
 // are on their way at any time, 128 KB a compute unit; 16 requests x 16384 keys x
-// 8 heads, 1.07 GB: 206 us = 5.2 TB/s.
+// 8 heads, 1.07 GB: 238 us = 4.5 TB/s, the joining launch with it.
 //   Split.  The tiles of all batches (those below the last key that a batch's
 // queries may see) are one sequence, cut into `units` equal pieces, a workgroup
 // and K/V head each; a piece may end one batch and begin the next.  Caches filled
@@ -257,6 +257,8 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_mod_few_kernel(FewArgs a) {
 #pragma unroll
       for (int mb = 0; mb < 4; ++mb) oacc[mb] = mfma32(read_tr(vb + 16 * ks * D, off.tr, mb), pop[ks], oacc[mb]);
   };
+  // (The output is divided by the sum of the weights before their rounding, where the
+  // 256-row form takes the roundings: either is within 2^-8 of the weights.)
   // One tile: its copies (older than the next tile's 16) are awaited; behind it,
   // when nothing reads its buffers any more, the tile after next is on its way.
   auto step = [&](auto parity) __attribute__((always_inline)) {

@@ -22,8 +22,9 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// Waves of a workgroup: 8, so that a lane may hold 256 registers; 10 where it
-// needs few (168 then): a row of 5120 channels with one chunk a lane.
+// Waves of a workgroup: 8, so that a lane may hold 256 registers; up to 10 in the
+// backward with one chunk a lane, which needs few (128 to 157; three waves a SIMD, so up
+// to twelve waves, leave 168).
 constexpr int kMaxWaves = 10;
 constexpr int kWaves = kBlockWaves;
 

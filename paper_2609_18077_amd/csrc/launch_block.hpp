@@ -84,10 +84,10 @@ inline BlockShape block_fwd_shape(int B, int L, int C) {
 // Shape of the backward: workgroups of `groups` groups of `waves` waves, a row
 // each at a time; a workgroup takes `rows` consecutive rows of a batch (a run),
 // `runs` of them a batch.
-//   One chunk of 8 channels a lane up to C = 5120 (ten waves), two up to 8192, four
-// beyond: a lane holds about ten values a channel (row, gradients, modulations,
-// column sums).  7803 tokens x 5120, fp32, modulations a token: two chunks, five
-// waves 475 us; one chunk, ten waves 309 us.
+//   One chunk of 8 channels a lane up to ten waves (C = 5120; the registers would
+// allow twelve), two up to 8192, four beyond: a lane holds about ten values a
+// channel (row, gradients, modulations, column sums).  7803 tokens x 5120, fp32,
+// modulations a token: two chunks, five waves 475 us; one chunk, ten waves 309 us.
 //   About 512 runs in all: the column sums of a run are written once and read
 // once by the reduction, 12 bytes a channel each way (512 runs against 65536
 // rows: 1.6 % of the bytes); at least 4 rows a group, so that the loads of one

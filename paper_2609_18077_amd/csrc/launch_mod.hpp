@@ -245,7 +245,7 @@ inline ModSplit mod_fwd_split(const ModCall& c, int cus, size_t max_floats) {
 // us): rounds of equal workgroups; one round of unequal ones, or the mean load and
 // half a run where they are more; 2 to start and end a workgroup; 2 for the further launch; the
 // partial sums written and read, 20 MB in a tile's time.  (2 x 2049 causal, 16 heads
-// on 4, cap and bias: three runs of every tile 184 + 14 us, up to eight 116 + 12.)
+// on 4, cap and bias: three runs of every tile 177 + 11 us, up to six 105 + 13.)
 struct ModBwdSplit {
   int runs, quantum;
   size_t delta, nlse, empty, counts, part;  // first values of these in the workspace (document ranges at 0)
